@@ -370,6 +370,117 @@ int nmt_op_adam(float* d_master32, float* d_m, float* d_v, const float* d_g32, f
 int nmt_op_dropout_mask(uint8_t* d_keep, int32_t rows, int32_t n_cols, const nmt_dropout* drop,
                         void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators for models beyond the step above: deeper ones (norms around a gated residual block), sparse ones (tokens
+ * sorted by expert and back) and larger ones (AdamW over many tensors, its states in 8 bits if wanted).
+ * Rows are fp16, bf16 or fp32; sums, statistics and norms are fp32.  Rows may lie any distance >= d apart (ld, in
+ * elements), and d and every address may be any that the type itself allows.  Nothing is atomic: the same inputs give the same bits.
+ * No rows and no tokens are a call like any other: sums over none are zero, ranges are empty.
+ * ------------------------------------------------------------------------------------------ */
+#define NMT_F16 0
+#define NMT_BF16 1
+#define NMT_F32 2
+#define NMT_NORM_LAYER 0 /* (a - mean) / sqrt(mean((a - mean)^2) + eps) */
+#define NMT_NORM_RMS 1   /* a / sqrt(mean(a^2) + eps)                     */
+
+/* The norms after one block and before the next, with the block's gate and the scale of its residual, row by row:
+ *   h = resid_scale * x + gate * post(y),  post(y) = norm(y) * post_gain + post_shift   (y itself if d_post_gain is NULL)
+ *   n = norm(h) * pre_gain + pre_shift                                              (not wanted if d_n is NULL)
+ * y: the block's output, x: the residual stream before it, n: the next block's input.  n is formed from h before h is
+ * rounded.  d_gate NULL: 1; otherwise row r takes row r / rows_per_gate of d_gate [ceil(rows / rows_per_gate), d] (rows_per_gate >= rows: one
+ * gate for all; 1: a gate for every element).  Shifts may be NULL (0).  Gains, shifts and gates are contiguous, of the rows' type.
+ * d_y NULL: the norm before the first block, n = norm(x) * pre_gain + pre_shift; d_h, d_post_gain, d_gate are then NULL too.
+ * d_stats: fp32 [rows, 4] = mean and 1 / sqrt(.) of y, then of h (0 and 1 where there is no norm; RMS: mean 0), for the backward call; may be
+ * NULL.  d_h may be d_x, and d_n may be d_y, with the same distance between rows; otherwise what is written overlaps nothing else.
+ * d <= 16384, rows < 2^31 - 65536. */
+typedef struct nmt_gated_norm {
+  int32_t rows, d, type, kind; /* type: NMT_F16 / NMT_BF16 / NMT_F32; kind: NMT_NORM_LAYER / NMT_NORM_RMS */
+  float eps, resid_scale;
+  int32_t rows_per_gate;
+  int64_t ld_x, ld_y, ld_h, ld_n;
+  const void *d_x, *d_y;
+  const void *d_post_gain, *d_post_shift, *d_gate, *d_pre_gain, *d_pre_shift;
+  void *d_h, *d_n;
+  float* d_stats;
+} nmt_gated_norm;
+int nmt_op_gated_norm_fwd(const nmt_gated_norm* a /*host*/, void* stream);
+
+/* Backward of the above.  Read from `a`: rows, d, type, kind, resid_scale, rows_per_gate, the gains, shifts and gate, d_y, d_h (without d_y: the x
+ * of the forward call), ld_y, ld_h and d_stats; its x, n and eps are not used.  d_dh: gradient that reaches h from elsewhere (NULL: none);
+ * d_dn: gradient at n (NULL: none); one of the two is there, and d_pre_gain with d_dn.  Written: d_dx (resid_scale times the gradient at h) and, with d_y, d_dy, of the
+ * rows' type, and the gradients of gains, shifts and gate (sums over the rows in fp32, rounded once to the rows' type; each may be NULL).  d_dx may be d_dh and
+ * d_dy may be d_dn with the same distance between rows.
+ * d_scratch: 16-byte aligned, of nmt_op_gated_norm_bwd_scratch(rows, d, rows_per_gate) floats. */
+typedef struct nmt_gated_norm_grad {
+  int64_t ld_dh, ld_dn, ld_dx, ld_dy;
+  const void *d_dh, *d_dn;
+  void *d_dx, *d_dy;
+  void *d_dpost_gain, *d_dpost_shift, *d_dgate, *d_dpre_gain, *d_dpre_shift;
+  float* d_scratch;
+  int64_t scratch_floats;
+} nmt_gated_norm_grad;
+int64_t nmt_op_gated_norm_bwd_scratch(int32_t rows, int32_t d, int32_t rows_per_gate);
+int nmt_op_gated_norm_bwd(const nmt_gated_norm* a /*host*/, const nmt_gated_norm_grad* g /*host*/, void* stream);
+
+/* Tokens to their experts.  d_expert [tokens, k]: the experts of every token (a value outside [0, experts) is none: the choice is
+ * dropped); the same expert twice takes two rows.  The choices are sorted by expert, those of one expert in the order of d_expert, and row
+ * d_slot[t, j] of d_rows becomes row t of d_x.
+ *   capacity == 0: the experts' rows lie back to back; d_rows has tokens * k rows, and those behind the last are left as they were.
+ *   capacity  > 0: expert e has the rows [e * capacity, (e + 1) * capacity) of d_rows, so that products of a size the host knows can be
+ *                  enqueued; choices beyond them are dropped, and rows without a token are set to zero.
+ * d_slot [tokens, k]: the row of every choice, -1 if it was dropped.  d_ranges [experts, 2]: first row and number of rows of every expert.
+ * d_x NULL: the lists alone (d_rows is then NULL too).  d_scratch: nmt_op_expert_dispatch_scratch int32 elements.
+ * k <= 64, experts <= 1024, tokens * k and experts * capacity <= 2^30. */
+int64_t nmt_op_expert_dispatch_scratch(int32_t tokens, int32_t k, int32_t experts);
+int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, int32_t k, int32_t experts, int32_t capacity, const void* d_x,
+                           int64_t ld_x, int32_t d, int32_t type, void* d_rows, int64_t ld_rows, int32_t* d_slot, int32_t* d_ranges,
+                           int32_t* d_scratch, void* stream);
+
+/* And back: out[t] = add[t] + sum over j of weights[t, j] * rows[slot[t, j]], in fp32 in the order of j, rounded once.  A choice whose slot lies
+ * outside [0, n_rows) adds nothing, whatever its weight.  d_weights fp32 [tokens, k], NULL: 1 (with the slots of nmt_op_expert_dispatch this is its
+ * gradient: d_x from d_rows).  d_add may be NULL, or d_out with the same distance between rows. */
+int nmt_op_expert_combine(const void* d_rows, int64_t ld_rows, int32_t n_rows, const int32_t* d_slot, const float* d_weights,
+                          const void* d_add, int64_t ld_add, void* d_out, int64_t ld_out, int32_t tokens, int32_t k, int32_t d,
+                          int32_t type, void* stream);
+/* Gradients of the above: d_drows[slot[t, j]] = weights[t, j] * dout[t] and d_dweights[t, j] = the inner product of dout[t] and rows[slot[t, j]]
+ * (0 for a dropped choice).  capacity and d_ranges as in nmt_op_expert_dispatch: rows without a token become zero where capacity > 0 and stay
+ * as they were otherwise (d_ranges may then be NULL).  d_weights NULL: 1.  d_rows and d_dweights may both be NULL.  d_drows may be d_rows with
+ * the same distance between rows; n_rows rows each.  The gradient of `add` is dout. */
+int nmt_op_expert_combine_bwd(const void* d_dout, int64_t ld_dout, const void* d_rows, int64_t ld_rows, int32_t n_rows,
+                              const int32_t* d_slot, const float* d_weights, void* d_drows, int64_t ld_drows, float* d_dweights,
+                              const int32_t* d_ranges, int32_t experts, int32_t capacity, int32_t tokens, int32_t k, int32_t d,
+                              int32_t type, void* stream);
+
+/* AdamW (Adam with decoupled weight decay) over many tensors in one launch:
+ *   g = grad * grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   master -= lr * lr_factor * (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay * master),  weights = master, rounded.
+ * state_bits 32: d_m, d_v fp32 [n].  state_bits 8: one byte each, in blocks of 256 elements counted from the tensor's first (the last may be
+ * shorter): m / m_scale and sqrt(v) / v_scale in OCP e4m3 (4 exponent and 3 mantissa bits), nearest, ties to even, the scale of a block being its
+ * largest magnitude / 448, fp32 [ceil(n / 256)]; a sqrt(v) that is not zero is never rounded to zero, so that no step is divided by eps alone.
+ * The step itself uses m and v before they are rounded.  Zeros everywhere are the states to start from.  What is inf or NaN stays so in its own element and
+ * does not reach its block's scale (in 8 bits both are NaN). */
+typedef struct nmt_adamw_tensor {
+  int64_t n;
+  float weight_decay, lr_factor;
+  float* d_master;
+  void *d_m, *d_v;
+  float *d_m_scale, *d_v_scale; /* state_bits 8 only */
+  const void* d_grad;           /* of type grad_type */
+  void* d_weights;              /* of type weights_type, or NULL: no copy of this tensor */
+} nmt_adamw_tensor;
+typedef struct nmt_adamw nmt_adamw;
+/* Bytes of the device table that nmt_adamw_create fills (host only). */
+int64_t nmt_adamw_table_bytes(int32_t n, const nmt_adamw_tensor* tensors /*host*/);
+/* Checks the tensors and writes the table of their pieces to d_table (16-byte aligned), which belongs to the handle until nmt_adamw_destroy.  Waits for the
+ * stream, so it cannot be captured.  `tensors` itself is not kept; the buffers it names must stay where they are.  No two tensors of a list overlap. */
+int nmt_adamw_create(int32_t n, const nmt_adamw_tensor* tensors /*host*/, int32_t state_bits, int32_t grad_type, int32_t weights_type,
+                     void* d_table, int64_t table_bytes, void* stream, nmt_adamw** out);
+void nmt_adamw_destroy(nmt_adamw* plan);
+/* One step of all tensors; t >= 1 is the number of this update.  If d_flag is not NULL and *d_flag != 0 the call changes nothing, as in
+ * nmt_adam_step.  lr, t and grad_scale are taken when the call is made: a captured graph repeats them. */
+int nmt_adamw_step(const nmt_adamw* plan, double lr, double beta1, double beta2, double eps, int32_t t, float grad_scale,
+                   const int32_t* d_flag, void* stream);
+
 #ifdef __cplusplus
 }
 #endif
