@@ -139,6 +139,7 @@ def load():
         for name, (res, args) in _SIGNATURES.items():
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = res, args
+        _torch_types()
         _lib = lib
     return _lib
 
@@ -428,100 +429,123 @@ def nmt_op_dropout_mask(keep, rows, n_cols, drop, stream=None):
 
 # ---- norms around a gated block, experts, AdamW ----------------------------------------------------
 # These take sizes, types and distances between rows from their tensors and refuse tensors that do not fit each other; the call goes
-# to the stream of the tensors' device.
+# to the stream of the tensors' device.  A small call is bound by what is done here, so nothing is looked up twice.
 NMT_F16, NMT_BF16, NMT_F32 = 0, 1, 2
 NMT_NORM_LAYER, NMT_NORM_RMS = 0, 1
 _KINDS = {"layer": NMT_NORM_LAYER, "rms": NMT_NORM_RMS}
+_TYPES = {}          # torch dtypes -> type codes; filled with _FLOAT and _INT when torch is there (load())
+_FLOAT = _INT = None
 
 
-def _refuse(msg):
-    raise NmtError(NMT_EINVAL, msg)
+def _torch_types():
+    global _FLOAT, _INT
+    import torch
+    _TYPES.update({torch.float16: NMT_F16, torch.bfloat16: NMT_BF16, torch.float32: NMT_F32})
+    _FLOAT, _INT = torch.float32, torch.int32
+
+
+def _refuse(msg, code=NMT_EINVAL):
+    raise NmtError(code, msg)
 
 
 def _type_code(dtype, who):
-    import torch
-    if dtype is torch.float16:
-        return NMT_F16
-    if dtype is torch.bfloat16:
-        return NMT_BF16
-    if dtype is torch.float32:
-        return NMT_F32
-    _refuse(f"{who}: rows of {dtype}: float16, bfloat16 or float32")
+    code = _TYPES.get(dtype)
+    if code is None:
+        _refuse(f"{who}: rows of {dtype}: float16, bfloat16 or float32")
+    return code
 
 
-def _matrix(t, rows, d, like, who, what):
-    """(address, distance between rows) of a [rows, d] tensor of the type and device of `like`; (None, 0) of None."""
-    if t is None:
-        return None, 0
-    if t.dtype is not like.dtype or t.device != like.device or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != d:
-        _refuse(f"{who}: {what} is {tuple(t.shape)} {t.dtype} on {t.device}, not ({rows}, {d}) {like.dtype} on {like.device}")
+def _rows_of(t, who, what):
+    """(rows, d, dtype, device) of the tensor that the others are held to."""
+    if t is None or t.dim() != 2:
+        _refuse(f"{who}: {what} is a two-dimensional tensor")
+    rows, d = t.shape
+    return rows, d, t.dtype, t.get_device()
+
+
+def _matrix(t, rows, d, dtype, device, what):
+    """Address of a [rows, d] tensor of that type on that device, and the distance between its rows."""
+    if t.dtype is not dtype or t.get_device() != device or t.shape != (rows, d):
+        _refuse(f"{what} is {tuple(t.shape)} {t.dtype} on {t.device}, not ({rows}, {d}) {dtype} on device {device}")
     ld, step = t.stride()
-    if (step != 1 and d > 1) or (ld < d and rows > 1):
-        _refuse(f"{who}: {what} has strides {(ld, step)}: rows whose elements lie side by side and that do not overlap are taken")
-    return t.data_ptr(), (ld if rows > 1 else d)
+    if rows <= 1:
+        ld = d
+    if (step != 1 and d > 1) or ld < d:
+        _refuse(f"{what} has strides {t.stride()}: rows whose elements lie side by side and that do not overlap are taken")
+    return t.data_ptr(), ld
 
 
-def _vector(t, n, dtype, like, who, what):
-    """Address of a contiguous tensor of n elements, or None."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.device != like.device or t.numel() != n or not t.is_contiguous():
-        _refuse(f"{who}: {what} is {tuple(t.shape)} {t.dtype} on {t.device}, not {n} contiguous elements of {dtype} on {like.device}")
+def _vector(t, n, dtype, device, what):
+    """Address of a contiguous tensor of n elements."""
+    if t.dtype is not dtype or t.get_device() != device or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{what} is {tuple(t.shape)} {t.dtype} on {t.device}, not {n} contiguous elements of {dtype} on device {device}")
     return t.data_ptr()
 
 
-def _on(like, stream, call, *args):
-    """call(*args, stream) with the device of `like` as the current one."""
+def _call(fn, device, stream, *args, out=None):
+    """fn(*args, stream[, address of out]) with `device` as the current one; its current stream if none is given."""
     import torch
-    device = like.device
-    if device.type != "cuda":
-        _refuse(f"the tensors are on {device}")
+    if device < 0:
+        _refuse(f"{fn.__name__}: the tensors are not on a GPU")
     if stream is None:
         stream = torch.cuda.current_stream(device).cuda_stream
-    if device.index == torch.cuda.current_device():
-        _check(call(*args, stream))
+    last = (stream,) if out is None else (stream, C.byref(out))
+    if device == torch.cuda.current_device():
+        rc = fn(*args, *last)
     else:
         with torch.cuda.device(device):
-            _check(call(*args, stream))
+            rc = fn(*args, *last)
+    if rc != NMT_OK:
+        _check(rc)
 
 
-def _pair(p):
-    return (None, None) if p is None else p
+def _gates(gate, rows, rows_per_gate, who):
+    """(rows of the gate, rows_per_gate)"""
+    if rows_per_gate is None or rows_per_gate >= rows:
+        return 1, max(rows, 1)
+    if rows_per_gate < 1:
+        _refuse(f"{who}: rows_per_gate must be at least 1")
+    return -(-rows // rows_per_gate), rows_per_gate
 
 
-def _gated_norm(who, first, x, y, h, n, stats, post, gate, pre, kind, rows_per_gate, resid_scale, eps):
-    if first is None or first.dim() != 2:
-        _refuse(f"{who}: the rows are [rows, d] tensors")
-    rows, d = first.shape
-    T = first.dtype
+def _norm_parts(a, rows, d, dtype, device, post, gate, pre, kind, rows_per_gate, resid_scale, who):
+    """What the forward and the backward call take alike."""
     if kind not in _KINDS:
         _refuse(f"{who}: kind {kind!r}: 'layer' or 'rms'")
-    gates = 0
+    a.rows, a.d, a.type, a.kind, a.resid_scale = rows, d, _type_code(dtype, who), _KINDS[kind], resid_scale
+    if post is not None:
+        gain, shift = post
+        a.d_post_gain = _vector(gain, d, dtype, device, "the gain after the block")
+        if shift is not None:
+            a.d_post_shift = _vector(shift, d, dtype, device, "the shift after the block")
     if gate is not None:
-        rows_per_gate = rows_per_gate or max(rows, 1)
-        if rows_per_gate < 1:
-            _refuse(f"{who}: rows_per_gate must be at least 1")
-        gates = 1 if rows_per_gate >= rows else -(-rows // rows_per_gate)
-    x_, ld_x = _matrix(x, rows, d, first, who, "x")
-    y_, ld_y = _matrix(y, rows, d, first, who, "y")
-    h_, ld_h = _matrix(h, rows, d, first, who, "h")
-    n_, ld_n = _matrix(n, rows, d, first, who, "n")
-    post_gain, post_shift = _pair(post)
-    pre_gain, pre_shift = _pair(pre)
-    import torch
-    return nmt_gated_norm(rows, d, _type_code(T, who), _KINDS[kind], eps, resid_scale, min(rows_per_gate or 1, 2 ** 31 - 1), ld_x, ld_y, ld_h, ld_n,
-                          x_, y_, _vector(post_gain, d, T, first, who, "the gain after the block"),
-                          _vector(post_shift, d, T, first, who, "the shift after the block"), _vector(gate, gates * d, T, first, who, "the gate"),
-                          _vector(pre_gain, d, T, first, who, "the gain before the next block"),
-                          _vector(pre_shift, d, T, first, who, "the shift before the next block"), h_, n_,
-                          _vector(stats, 4 * rows, torch.float32, first, who, "stats"))
+        gates, a.rows_per_gate = _gates(gate, rows, rows_per_gate, who)
+        a.d_gate = _vector(gate, gates * d, dtype, device, "the gate")
+    if pre is not None:
+        gain, shift = pre
+        a.d_pre_gain = _vector(gain, d, dtype, device, "the gain before the next block")
+        if shift is not None:
+            a.d_pre_shift = _vector(shift, d, dtype, device, "the shift before the next block")
 
 
 def nmt_op_gated_norm_fwd(x, y, h, n, stats=None, post=None, gate=None, pre=None, kind="layer", rows_per_gate=None, resid_scale=1.0, eps=1e-5,
                           stream=None):
     """h = resid_scale * x + gate * post(y), n = pre(h).  post, pre: (gain, shift or None) or None; rows_per_gate None: one gate for all rows."""
-    a = _gated_norm("nmt_op_gated_norm_fwd", x, x, y, h, n, stats, post, gate, pre, kind, rows_per_gate, resid_scale, eps)
-    _on(x, stream, load().nmt_op_gated_norm_fwd, C.byref(a))
+    lib = _lib or load()
+    rows, d, dtype, device = _rows_of(x, "nmt_op_gated_norm_fwd", "x")
+    a = nmt_gated_norm()
+    _norm_parts(a, rows, d, dtype, device, post, gate, pre, kind, rows_per_gate, resid_scale, "nmt_op_gated_norm_fwd")
+    a.eps = eps
+    a.d_x, a.ld_x = _matrix(x, rows, d, dtype, device, "x")
+    if y is not None:
+        a.d_y, a.ld_y = _matrix(y, rows, d, dtype, device, "y")
+    if h is not None:
+        a.d_h, a.ld_h = _matrix(h, rows, d, dtype, device, "h")
+    if n is not None:
+        a.d_n, a.ld_n = _matrix(n, rows, d, dtype, device, "n")
+    if stats is not None:
+        a.d_stats = _vector(stats, 4 * rows, _FLOAT, device, "stats")
+    _call(lib.nmt_op_gated_norm_fwd, device, stream, a)
 
 
 def nmt_op_gated_norm_bwd_scratch(rows, d, rows_per_gate=None):
@@ -534,23 +558,41 @@ def nmt_op_gated_norm_bwd_scratch(rows, d, rows_per_gate=None):
 def nmt_op_gated_norm_bwd(dh, dn, y, h, stats, dx, dy, scratch, post=None, gate=None, pre=None, dpost=None, dgate=None, dpre=None, kind="layer",
                           rows_per_gate=None, resid_scale=1.0, stream=None):
     """Gradients of nmt_op_gated_norm_fwd (h: its x where there is no y).  dpost, dpre: (of the gain, of the shift or None) or None."""
-    import torch
-    who = "nmt_op_gated_norm_bwd"
-    a = _gated_norm(who, dx, None, y, h, None, stats, post, gate, pre, kind, rows_per_gate, resid_scale, 1.0)
-    rows, d, T = a.rows, a.d, dx.dtype
-    (dh_, ld_dh), (dn_, ld_dn) = _matrix(dh, rows, d, dx, who, "dh"), _matrix(dn, rows, d, dx, who, "dn")
-    (dx_, ld_dx), (dy_, ld_dy) = _matrix(dx, rows, d, dx, who, "dx"), _matrix(dy, rows, d, dx, who, "dy")
-    dpost_gain, dpost_shift = _pair(dpost)
-    dpre_gain, dpre_shift = _pair(dpre)
-    vec = lambda t, what: _vector(t, d, T, dx, who, what)
-    g = nmt_gated_norm_grad(ld_dh, ld_dn, ld_dx, ld_dy, dh_, dn_, dx_, dy_, vec(dpost_gain, "the gradient of the gain after the block"),
-                            vec(dpost_shift, "the gradient of the shift after the block"),
-                            _vector(dgate, 0 if gate is None else gate.numel(), T, dx, who, "the gate's gradient"),
-                            vec(dpre_gain, "the gradient of the gain before the next block"),
-                            vec(dpre_shift, "the gradient of the shift before the next block"),
-                            None if scratch is None else _vector(scratch, scratch.numel(), torch.float32, dx, who, "scratch"),
-                            0 if scratch is None else scratch.numel())
-    _on(dx, stream, load().nmt_op_gated_norm_bwd, C.byref(a), C.byref(g))
+    lib = _lib or load()
+    rows, d, dtype, device = _rows_of(dx, "nmt_op_gated_norm_bwd", "dx")
+    a, g = nmt_gated_norm(), nmt_gated_norm_grad()
+    _norm_parts(a, rows, d, dtype, device, post, gate, pre, kind, rows_per_gate, resid_scale, "nmt_op_gated_norm_bwd")
+    g.d_dx, g.ld_dx = _matrix(dx, rows, d, dtype, device, "dx")
+    if y is not None:
+        a.d_y, a.ld_y = _matrix(y, rows, d, dtype, device, "y")
+    if h is not None:
+        a.d_h, a.ld_h = _matrix(h, rows, d, dtype, device, "h")
+    if dh is not None:
+        g.d_dh, g.ld_dh = _matrix(dh, rows, d, dtype, device, "dh")
+    if dn is not None:
+        g.d_dn, g.ld_dn = _matrix(dn, rows, d, dtype, device, "dn")
+    if dy is not None:
+        g.d_dy, g.ld_dy = _matrix(dy, rows, d, dtype, device, "dy")
+    if stats is not None:
+        a.d_stats = _vector(stats, 4 * rows, _FLOAT, device, "stats")
+    if dpost is not None:
+        gain, shift = dpost
+        if gain is not None:
+            g.d_dpost_gain = _vector(gain, d, dtype, device, "the gradient of the gain after the block")
+        if shift is not None:
+            g.d_dpost_shift = _vector(shift, d, dtype, device, "the gradient of the shift after the block")
+    if dgate is not None:
+        g.d_dgate = _vector(dgate, 0 if gate is None else gate.numel(), dtype, device, "the gate's gradient")
+    if dpre is not None:
+        gain, shift = dpre
+        if gain is not None:
+            g.d_dpre_gain = _vector(gain, d, dtype, device, "the gradient of the gain before the next block")
+        if shift is not None:
+            g.d_dpre_shift = _vector(shift, d, dtype, device, "the gradient of the shift before the next block")
+    if scratch is not None:
+        g.scratch_floats = scratch.numel()
+        g.d_scratch = _vector(scratch, g.scratch_floats, _FLOAT, device, "scratch")
+    _call(lib.nmt_op_gated_norm_bwd, device, stream, a, g)
 
 
 def nmt_op_expert_dispatch_scratch(tokens, k, experts):
@@ -561,74 +603,68 @@ def nmt_op_expert_dispatch_scratch(tokens, k, experts):
 
 
 def _lists(t, who, what):
-    import torch
-    if t is None or t.dim() != 2 or t.dtype is not torch.int32 or not t.is_contiguous():
+    if t is None or t.dim() != 2 or t.dtype is not _INT or not t.is_contiguous():
         _refuse(f"{who}: {what} is a contiguous [tokens, k] tensor of int32")
-    return t.shape
+    tokens, k = t.shape
+    return tokens, k, t.get_device()
 
 
 def nmt_op_expert_dispatch(expert, experts, capacity, x, rows, slot, ranges, scratch, stream=None):
     """expert [tokens, k] int32; x [tokens, d], rows: [experts * capacity, d], or [tokens * k, d] without a capacity (both None: the lists alone);
-    slot [tokens, k], ranges [experts, 2] int32."""
-    import torch
+    slot [tokens, k], ranges [experts, 2] int32; scratch: int32."""
+    lib = _lib or load()
     who = "nmt_op_expert_dispatch"
-    tokens, k = _lists(expert, who, "expert")
-    type_ = d = ld_x = ld_rows = 0
-    x_ = rows_ = None
-    if (x is None) != (rows is None):
+    tokens, k, device = _lists(expert, who, "expert")
+    d = code = ld_x = ld_rows = 0
+    x_ = rows_ = scratch_ = None
+    if x is not None and rows is not None:
+        _, d, dtype, _ = _rows_of(x, who, "x")
+        code = _type_code(dtype, who)
+        x_, ld_x = _matrix(x, tokens, d, dtype, device, "x")
+        rows_, ld_rows = _matrix(rows, experts * capacity if capacity else tokens * k, d, dtype, device, "rows")
+    elif x is not rows:
         _refuse(f"{who}: tokens and the experts' rows belong together")
-    if x is not None:
-        if x.dim() != 2:
-            _refuse(f"{who}: x is [tokens, d]")
-        d, type_ = x.shape[1], _type_code(x.dtype, who)
-        x_, ld_x = _matrix(x, tokens, d, x, who, "x")
-        rows_, ld_rows = _matrix(rows, experts * capacity if capacity else tokens * k, d, x, who, "rows")
-    I = torch.int32
-    need = nmt_op_expert_dispatch_scratch(tokens, k, experts)
-    if need and (scratch is None or scratch.numel() < need):
-        raise NmtError(NMT_ENOMEM, f"{who}: scratch of {0 if scratch is None else scratch.numel()} elements, {need} needed")
-    if x is not None and x.device != expert.device:
-        _refuse(f"{who}: expert is on {expert.device}, x on {x.device}")
-    _on(expert, stream, load().nmt_op_expert_dispatch, expert.data_ptr(), tokens, k, experts, capacity, x_, ld_x, d, type_, rows_, ld_rows,
-        _vector(slot, tokens * k, I, expert, who, "slot"), _vector(ranges, 2 * experts, I, expert, who, "ranges"),
-        None if scratch is None else _vector(scratch, scratch.numel(), I, expert, who, "scratch"))
+    held = 0 if scratch is None else scratch.numel()
+    need = lib.nmt_op_expert_dispatch_scratch(tokens, k, experts)
+    if need > held:
+        _refuse(f"{who}: scratch of {held} elements, {need} needed", NMT_ENOMEM)
+    if held:
+        scratch_ = _vector(scratch, held, _INT, device, "scratch")
+    _call(lib.nmt_op_expert_dispatch, device, stream, expert.data_ptr(), tokens, k, experts, capacity, x_, ld_x, d, code, rows_, ld_rows,
+          _vector(slot, tokens * k, _INT, device, "slot"), _vector(ranges, 2 * experts, _INT, device, "ranges"), scratch_)
 
 
 def nmt_op_expert_combine(rows, slot, weights, out, add=None, stream=None):
     """out[t] = add[t] + sum over j of weights[t, j] * rows[slot[t, j]]; weights fp32 [tokens, k] or None (1)."""
-    import torch
-    who = "nmt_op_expert_combine"
-    tokens, k = _lists(slot, who, "slot")
-    if rows is None or rows.dim() != 2:
-        _refuse(f"{who}: rows is [rows, d]")
-    n, d = rows.shape
-    (rows_, ld_rows), (out_, ld_out), (add_, ld_add) = (_matrix(rows, n, d, rows, who, "rows"), _matrix(out, tokens, d, rows, who, "out"),
-                                                        _matrix(add, tokens, d, rows, who, "add"))
-    if slot.device != rows.device:
-        _refuse(f"{who}: slot is on {slot.device}, rows on {rows.device}")
-    _on(rows, stream, load().nmt_op_expert_combine, rows_, ld_rows, n, slot.data_ptr(),
-        _vector(weights, tokens * k, torch.float32, rows, who, "weights"), add_, ld_add, out_, ld_out, tokens, k, d, _type_code(rows.dtype, who))
+    lib, who = _lib or load(), "nmt_op_expert_combine"
+    tokens, k, device = _lists(slot, who, "slot")
+    n, d, dtype, _ = _rows_of(rows, who, "rows")
+    rows_, ld_rows = _matrix(rows, n, d, dtype, device, "rows")
+    out_, ld_out = _matrix(out, tokens, d, dtype, device, "out")
+    add_, ld_add = (None, 0) if add is None else _matrix(add, tokens, d, dtype, device, "add")
+    _call(lib.nmt_op_expert_combine, device, stream, rows_, ld_rows, n, slot.data_ptr(),
+          None if weights is None else _vector(weights, tokens * k, _FLOAT, device, "weights"), add_, ld_add, out_, ld_out, tokens, k, d,
+          _type_code(dtype, who))
 
 
 def nmt_op_expert_combine_bwd(dout, rows, slot, weights, drows, dweights, ranges=None, capacity=0, stream=None):
     """drows[slot[t, j]] = weights[t, j] * dout[t], dweights[t, j] = <dout[t], rows[slot[t, j]]>; rows and dweights may both be None."""
-    import torch
-    who = "nmt_op_expert_combine_bwd"
-    tokens, k = _lists(slot, who, "slot")
-    if drows is None or drows.dim() != 2:
-        _refuse(f"{who}: drows is [rows, d]")
-    n, d = drows.shape
-    (dout_, ld_dout), (rows_, ld_rows), (drows_, ld_drows) = (_matrix(dout, tokens, d, drows, who, "dout"), _matrix(rows, n, d, drows, who, "rows"),
-                                                              _matrix(drows, n, d, drows, who, "drows"))
-    if slot.device != drows.device:
-        _refuse(f"{who}: slot is on {slot.device}, drows on {drows.device}")
-    if capacity and ranges is None:
+    lib, who = _lib or load(), "nmt_op_expert_combine_bwd"
+    tokens, k, device = _lists(slot, who, "slot")
+    n, d, dtype, _ = _rows_of(drows, who, "drows")
+    drows_, ld_drows = _matrix(drows, n, d, dtype, device, "drows")
+    dout_, ld_dout = _matrix(dout, tokens, d, dtype, device, "dout")
+    rows_, ld_rows = (None, 0) if rows is None else _matrix(rows, n, d, dtype, device, "rows")
+    experts, ranges_ = 1, None
+    if ranges is not None:
+        experts = ranges.shape[0]
+        ranges_ = _vector(ranges, 2 * experts, _INT, device, "ranges")
+    elif capacity:
         _refuse(f"{who}: a capacity needs the experts' ranges")
-    experts = 1 if ranges is None else ranges.shape[0]
-    _on(drows, stream, load().nmt_op_expert_combine_bwd, dout_, ld_dout, rows_, ld_rows, n, slot.data_ptr(),
-        _vector(weights, tokens * k, torch.float32, drows, who, "weights"), drows_, ld_drows,
-        _vector(dweights, tokens * k, torch.float32, drows, who, "dweights"),
-        _vector(ranges, 2 * experts, torch.int32, drows, who, "ranges"), experts, capacity, tokens, k, d, _type_code(drows.dtype, who))
+    _call(lib.nmt_op_expert_combine_bwd, device, stream, dout_, ld_dout, rows_, ld_rows, n, slot.data_ptr(),
+          None if weights is None else _vector(weights, tokens * k, _FLOAT, device, "weights"), drows_, ld_drows,
+          None if dweights is None else _vector(dweights, tokens * k, _FLOAT, device, "dweights"), ranges_, experts, capacity, tokens, k, d,
+          _type_code(dtype, who))
 
 
 def _adamw_tensors(tensors, who):
@@ -650,7 +686,8 @@ def _adamw_tensors(tensors, who):
             grad_type = grad.dtype
         if weights is not None and weights_type is None:
             weights_type = weights.dtype
-        vec = lambda x, size, dtype, what: _vector(x, size, dtype, master, who, f"{what} of tensor {i}")
+        device = master.get_device()
+        vec = lambda x, size, dtype, what: None if x is None else _vector(x, size, dtype, device, f"{what} of tensor {i}")
         blocks = -(-n // 256) if e8 else 0
         a.n, a.weight_decay, a.lr_factor = n, t.get("weight_decay", 0.0), t.get("lr_factor", 1.0)
         a.d_master, a.d_m, a.d_v = vec(master, n, torch.float32, "master"), vec(m, n, state, "m"), vec(v, n, state, "v")
@@ -658,8 +695,8 @@ def _adamw_tensors(tensors, who):
         if e8:
             a.d_m_scale = vec(t.get("m_scale"), blocks, torch.float32, "m_scale")
             a.d_v_scale = vec(t.get("v_scale"), blocks, torch.float32, "v_scale")
-        if master.device != tensors[0]["master"].device:
-            _refuse(f"{who}: tensors on {tensors[0]['master'].device} and on {master.device}")
+        if device != tensors[0]["master"].get_device():
+            _refuse(f"{who}: tensors on several devices")
     return arr, bits, grad_type or torch.float32, weights_type or torch.float32
 
 
@@ -683,15 +720,14 @@ class AdamwPlan:
 def nmt_adamw_create(tensors, table, stream=None):
     """tensors: list of dict(master=, m=, v=, grad=, weights= or None, weight_decay=, lr_factor=) of tensors of equal sizes, master fp32; m and v fp32, or
     float8_e4m3fn with m_scale= and v_scale= (fp32, one element per 256).  table: uint8 tensor of nmt_adamw_table_bytes(tensors) bytes."""
-    who = "nmt_adamw_create"
+    lib, who = _lib or load(), "nmt_adamw_create"
     arr, bits, grad_type, weights_type = _adamw_tensors(tensors, who)
     out = C.c_void_p()
-    like = tensors[0]["master"] if tensors else table
-    if table.device != like.device or not table.is_contiguous():
-        _refuse(f"{who}: the table is contiguous and on the tensors' device")
-    _on(like, stream, lambda s: load().nmt_adamw_create(len(tensors), arr, bits, _type_code(grad_type, who), _type_code(weights_type, who), table.data_ptr(),
-                                                       table.numel() * table.element_size(), s, C.byref(out)))
-    return AdamwPlan(out, like, (list(tensors), table))
+    device = (tensors[0]["master"] if tensors else table).get_device()
+    size = table.numel() * table.element_size()
+    _call(lib.nmt_adamw_create, device, stream, len(tensors), arr, bits, _type_code(grad_type, who), _type_code(weights_type, who),
+          _vector(table, table.numel(), table.dtype, device, "the table"), size, out=out)
+    return AdamwPlan(out, device, (list(tensors), table))
 
 
 def nmt_adamw_destroy(plan):
@@ -701,8 +737,7 @@ def nmt_adamw_destroy(plan):
 
 
 def nmt_adamw_step(plan, lr, beta1, beta2, eps, t, grad_scale=1.0, flag=None, stream=None):
-    import torch
     if plan.handle is None:
         _refuse("nmt_adamw_step: the plan has been given back")
-    _on(plan.device, stream, load().nmt_adamw_step, plan.handle, lr, beta1, beta2, eps, t, grad_scale,
-        _vector(flag, 1, torch.int32, plan.device, "nmt_adamw_step", "flag"))
+    _call(_lib.nmt_adamw_step, plan.device, stream, plan.handle, lr, beta1, beta2, eps, t, grad_scale,
+          None if flag is None else _vector(flag, 1, _INT, plan.device, "flag"))

@@ -119,21 +119,9 @@ struct RowsArgs {
   const int32_t *slot, *ranges;
   const float* weights;
   float* dweights;
-  int tokens, k, d, n_rows, capacity, experts, lanes_log;
+  int tokens, k, d, vectors, n_rows, capacity, experts, lanes_log;  // vectors: columns in whole vectors of 16 bytes
   int64_t token_groups;  // work-groups of tokens; those behind clear rows without a token
 };
-
-template <typename T>
-__device__ __forceinline__ void copy_vec(T* to, const typename Row<T>::vec& v, int c, int d) {
-  constexpr int N = Row<T>::kVec;
-  if (c + N <= d) {
-    *reinterpret_cast<typename Row<T>::vec*>(to + c) = v;
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (c + e < d) to[c + e] = v[e];
-  }
-}
 
 // Rows of fixed room that no token took become zero.
 template <typename T>
@@ -144,8 +132,10 @@ __device__ __forceinline__ void clear_rows(const RowsArgs& a, void* rows, int64_
   if (s >= (int64_t)a.experts * a.capacity) return;
   const int e = (int)(s / a.capacity);
   if ((int)(s - (int64_t)e * a.capacity) < a.ranges[2 * e + 1]) return;
-  const typename Row<T>::vec zero = {};
-  for (int c = (threadIdx.x & ((1 << a.lanes_log) - 1)) * N; c < a.d; c += N << a.lanes_log) copy_vec(static_cast<T*>(rows) + s * ld, zero, c, a.d);
+  T* row = static_cast<T*>(rows) + s * ld;
+  const int lane = threadIdx.x & ((1 << a.lanes_log) - 1);
+  for (int c = lane * N; c < a.vectors; c += N << a.lanes_log) st_vec(row + c, typename Row<T>::vec{});
+  for (int c = a.vectors + lane; c < a.d; c += 1 << a.lanes_log) row[c] = T(0);
 }
 
 // rows[slot[t, j]] = x[t]; T is any type of the rows' size.
@@ -159,18 +149,20 @@ __global__ void __launch_bounds__(kThreads) expert_scatter_kernel(const RowsArgs
   const int64_t t = (int64_t)blockIdx.x * (kThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
   if (t >= a.tokens) return;
   const T* x = static_cast<const T*>(a.x) + t * a.ld_x;
-  for (int c = (threadIdx.x & ((1 << a.lanes_log) - 1)) * N; c < a.d; c += N << a.lanes_log) {
-    typename Row<T>::vec v = {};
-    if (c + N <= a.d) {
-      v = *reinterpret_cast<const typename Row<T>::vec*>(x + c);
-    } else {
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (c + e < a.d) v[e] = x[c + e];
-    }
+  T* rows = static_cast<T*>(a.out);
+  const int lane = threadIdx.x & ((1 << a.lanes_log) - 1);
+  for (int c = lane * N; c < a.vectors; c += N << a.lanes_log) {
+    const typename Row<T>::vec v = ld_vec(x + c);
     for (int j = 0; j < a.k; ++j) {
       const int32_t s = a.slot[t * a.k + j];
-      if (s >= 0) copy_vec(static_cast<T*>(a.out) + (int64_t)s * a.ld_out, v, c, a.d);
+      if (s >= 0) st_vec(rows + (int64_t)s * a.ld_out + c, v);
+    }
+  }
+  for (int c = a.vectors + lane; c < a.d; c += 1 << a.lanes_log) {
+    const T v = x[c];
+    for (int j = 0; j < a.k; ++j) {
+      const int32_t s = a.slot[t * a.k + j];
+      if (s >= 0) rows[(int64_t)s * a.ld_out + c] = v;
     }
   }
 }
@@ -181,20 +173,35 @@ __global__ void __launch_bounds__(kThreads) expert_combine_kernel(const RowsArgs
   constexpr int N = Row<T>::kVec;
   const int64_t t = (int64_t)blockIdx.x * (kThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
   if (t >= a.tokens) return;
-  for (int c = (threadIdx.x & ((1 << a.lanes_log) - 1)) * N; c < a.d; c += N << a.lanes_log) {
-    float s[N], v[N];
+  const T* add = static_cast<const T*>(a.add) + t * a.ld_add;
+  T* out = static_cast<T*>(a.out) + t * a.ld_out;
+  const int lane = threadIdx.x & ((1 << a.lanes_log) - 1);
+  for (int c = lane * N; c < a.vectors; c += N << a.lanes_log) {
+    float s[N];
+    typename Row<T>::vec v = {};
+    if (a.add) v = ld_vec(add + c);
 #pragma unroll
-    for (int e = 0; e < N; ++e) s[e] = 0.f;
-    if (a.add) ld_row<true>(static_cast<const T*>(a.add) + t * a.ld_add, c, a.d, s);
+    for (int e = 0; e < N; ++e) s[e] = (float)v[e];
     for (int j = 0; j < a.k; ++j) {
       const int32_t at = a.slot[t * a.k + j];
       if ((uint32_t)at >= (uint32_t)a.n_rows) continue;
       const float w = a.weights ? a.weights[t * a.k + j] : 1.f;
-      ld_row<true>(static_cast<const T*>(a.rows) + (int64_t)at * a.ld_rows, c, a.d, v);
+      v = ld_vec(static_cast<const T*>(a.rows) + (int64_t)at * a.ld_rows + c);
 #pragma unroll
-      for (int e = 0; e < N; ++e) s[e] += w * v[e];
+      for (int e = 0; e < N; ++e) s[e] += w * (float)v[e];
     }
-    st_row<true>(static_cast<T*>(a.out) + t * a.ld_out, c, a.d, s);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = (T)s[e];
+    st_vec(out + c, v);
+  }
+  for (int c = a.vectors + lane; c < a.d; c += 1 << a.lanes_log) {
+    float s = a.add ? (float)add[c] : 0.f;
+    for (int j = 0; j < a.k; ++j) {
+      const int32_t at = a.slot[t * a.k + j];
+      if ((uint32_t)at >= (uint32_t)a.n_rows) continue;
+      s += (a.weights ? a.weights[t * a.k + j] : 1.f) * (float)static_cast<const T*>(a.rows)[(int64_t)at * a.ld_rows + c];
+    }
+    out[c] = (T)s;
   }
 }
 
@@ -215,17 +222,23 @@ __global__ void __launch_bounds__(kThreads) expert_combine_bwd_kernel(const Rows
     float dot = 0.f;
     if ((uint32_t)at < (uint32_t)a.n_rows) {
       const float w = a.weights ? a.weights[t * a.k + j] : 1.f;
-      for (int c = lane * N; c < a.d; c += N * kWave) {
-        float g[N], v[N];
-        ld_row<true>(x, c, a.d, g);
+      const T* row = static_cast<const T*>(a.rows) + (int64_t)at * a.ld_rows;
+      T* out = static_cast<T*>(a.out) + (int64_t)at * a.ld_out;
+      for (int c = lane * N; c < a.vectors; c += N * kWave) {
+        typename Row<T>::vec g = ld_vec(x + c);
         if (a.dweights) {
-          ld_row<true>(static_cast<const T*>(a.rows) + (int64_t)at * a.ld_rows, c, a.d, v);
+          const typename Row<T>::vec v = ld_vec(row + c);
 #pragma unroll
-          for (int e = 0; e < N; ++e) dot += g[e] * v[e];
+          for (int e = 0; e < N; ++e) dot += (float)g[e] * (float)v[e];
         }
 #pragma unroll
-        for (int e = 0; e < N; ++e) g[e] *= w;
-        st_row<true>(static_cast<T*>(a.out) + (int64_t)at * a.ld_out, c, a.d, g);
+        for (int e = 0; e < N; ++e) g[e] = (T)((float)g[e] * w);
+        st_vec(out + c, g);
+      }
+      if (const int c = a.vectors + lane; c < a.d) {
+        const float g = (float)x[c];
+        if (a.dweights) dot += g * (float)row[c];
+        out[c] = (T)(g * w);
       }
     }
     if (a.dweights) {
@@ -241,6 +254,8 @@ int lanes_log_of(int d, int type) {
   while ((1 << l) < vecs && l < 8) ++l;
   return l;
 }
+
+int whole_vectors(int d, int type) { return d / (16 / row_type_bytes(type)) * (16 / row_type_bytes(type)); }
 
 int segments_of(int64_t n) { return (int)((n + kSegment - 1) / kSegment); }
 
@@ -289,7 +304,7 @@ extern "C" int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, i
   if (!d_rows) return NMT_OK;
   RowsArgs a = {};
   a.x = d_x, a.ld_x = ld_x, a.out = d_rows, a.ld_out = ld_rows, a.slot = d_slot, a.ranges = d_ranges;
-  a.tokens = tokens, a.k = k, a.d = d, a.capacity = capacity, a.experts = experts, a.lanes_log = lanes_log_of(d, type);
+  a.tokens = tokens, a.k = k, a.d = d, a.vectors = whole_vectors(d, type), a.capacity = capacity, a.experts = experts, a.lanes_log = lanes_log_of(d, type);
   const int per = kThreads >> a.lanes_log;
   a.token_groups = ceil_div(tokens, per);
   const dim3 grid((uint32_t)(a.token_groups + ceil_div((int64_t)experts * capacity, per)));
@@ -315,7 +330,7 @@ extern "C" int nmt_op_expert_combine(const void* d_rows, int64_t ld_rows, int32_
   EXPERT_ROWS(d_out, tokens, ld_out, "out");
   RowsArgs a = {};
   a.rows = d_rows, a.ld_rows = ld_rows, a.n_rows = n_rows, a.slot = d_slot, a.weights = d_weights, a.add = d_add, a.ld_add = ld_add;
-  a.out = d_out, a.ld_out = ld_out, a.tokens = tokens, a.k = k, a.d = d, a.lanes_log = lanes_log_of(d, type);
+  a.out = d_out, a.ld_out = ld_out, a.tokens = tokens, a.k = k, a.d = d, a.vectors = whole_vectors(d, type), a.lanes_log = lanes_log_of(d, type);
   const dim3 grid(ceil_div(tokens, kThreads >> a.lanes_log));
   if (type == NMT_F16) hipLaunchKernelGGL(expert_combine_kernel<half_t>, grid, dim3(kThreads), 0, stream, a);
   else if (type == NMT_BF16) hipLaunchKernelGGL(expert_combine_kernel<bf16_t>, grid, dim3(kThreads), 0, stream, a);
@@ -343,7 +358,7 @@ extern "C" int nmt_op_expert_combine_bwd(const void* d_dout, int64_t ld_dout, co
   RowsArgs a = {};
   a.x = d_dout, a.ld_x = ld_dout, a.rows = d_rows, a.ld_rows = ld_rows, a.n_rows = n_rows, a.slot = d_slot, a.ranges = d_ranges;
   a.weights = d_weights, a.dweights = d_dweights, a.out = d_drows, a.ld_out = ld_drows;
-  a.tokens = tokens, a.k = k, a.d = d, a.capacity = capacity, a.experts = experts, a.lanes_log = lanes_log_of(d, type);
+  a.tokens = tokens, a.k = k, a.d = d, a.vectors = whole_vectors(d, type), a.capacity = capacity, a.experts = experts, a.lanes_log = lanes_log_of(d, type);
   a.token_groups = ceil_div(tokens, kWaves);
   const dim3 grid((uint32_t)(a.token_groups + ceil_div((int64_t)experts * capacity, kThreads >> a.lanes_log)));
   if (grid.x == 0) return NMT_OK;

@@ -1,8 +1,10 @@
 // The norms around a gated residual block, one pass over the rows each way:
 //   h = a x + gate post(y), n = pre(h);  post, pre: LayerNorm or RMS norm with gain and shift.
 // Bound by memory: forward reads x, y and writes h, n (n needs h's statistics, which are there while h is still in registers), backward
-// reads y, h and the gradients at h and n and writes those at x and y.  A row is held in registers by 16 lanes (up to 128 columns), by a
-// wavefront (up to 1024) or by up to 16 wavefronts.
+// reads y, h and the gradients at h and n and writes those at x and y.  A row is held in registers by 16, 32 or 64 lanes (up to 128, 256, 512 columns) or by
+// several wavefronts, each lane's share of it 16 bytes at a time; the next row is in flight while one is worked on.
+// Forward 52701 x 1024 bf16: 73 us, 5.9 TB/s (a copy of a gigabyte: 5.2).  Backward 26001 x 1024 fp16: 74 us, 4.3 TB/s, of which the sums over work-groups take 5;
+// a wavefront per SIMD has its registers full of column sums and two rows.  Rows of more than 8192 columns (fp32 backward: 4096) spill some of those.
 #include "rowtypes.h"
 
 #include <algorithm>
@@ -14,7 +16,9 @@ namespace {
 constexpr int kMaxRows = 0x7FFFFFFF - 65536, kMaxCols = 16384;
 
 struct NormArgs {
-  int rows, d, kind, rows_per_gate, chunk, gates;  // chunk: rows of a worker of the backward pass
+  int rows, d, kind, rows_per_gate, chunk, gates;  // chunk: rows of a worker, the lanes that hold a row
+  int stream;                                      // results are written past the caches
+  Divisor per_gate;
   float eps, resid_scale;
   int64_t ld_x, ld_y, ld_h, ld_n;
   const void *x, *y, *post_gain, *post_shift, *gate, *pre_gain, *pre_shift;
@@ -25,7 +29,7 @@ struct NormArgs {
   const void *dh, *dn;
   void *dx, *dy, *dpost_gain, *dpost_shift, *dgate, *dpre_gain, *dpre_shift;
   float *partial, *gate_partial;
-  int groups, pitch;  // work-groups of the backward pass; floats of a row of partial sums
+  int groups, pitch, sums;  // work-groups of the backward pass, floats of a row of partial sums, such rows of a work-group
 };
 
 typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
@@ -34,15 +38,7 @@ typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
 // one before this may have used, but not the last.
 template <int LANES, int WAVES>
 __device__ __forceinline__ float row_sum(float v, float* red) {
-  if constexpr (LANES == 16) {
-    auto rot = [](float x, auto ctrl) {
-      return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, true));
-    };
-    v = rot(v, std::integral_constant<int, 0x128>{});  // row_ror:8
-    v = rot(v, std::integral_constant<int, 0x124>{});  // row_ror:4
-    v = rot(v, std::integral_constant<int, 0x4E>{});   // quad_perm:[2,3,0,1]
-    return rot(v, std::integral_constant<int, 0xB1>{});  // quad_perm:[1,0,3,2]
-  } else {
+  if constexpr (LANES == 64) {
     v = wave_sum(v);
     if constexpr (WAVES > 1) {
       if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
@@ -52,250 +48,385 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
       for (int w = 1; w < WAVES; ++w) v += red[w];
     }
     return v;
+  } else {
+    auto plus = [](float x, auto ctrl) {
+      return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    if constexpr (LANES == 32) {
+      const auto h = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+      v = __builtin_bit_cast(float, (unsigned)h[0]) + __builtin_bit_cast(float, (unsigned)h[1]);
+    }
+    v = plus(v, std::integral_constant<int, 0x128>{});    // row_ror:8
+    v = plus(v, std::integral_constant<int, 0x124>{});    // row_ror:4
+    v = plus(v, std::integral_constant<int, 0x4E>{});     // quad_perm:[2,3,0,1]
+    return plus(v, std::integral_constant<int, 0xB1>{});  // quad_perm:[1,0,3,2]
   }
 }
 
-// LANES lanes of each of WAVES wavefronts hold a row, E elements a lane, in vectors of 16 bytes LANES * WAVES vectors apart.
-template <typename T, int E, int LANES, int WAVES>
+// LANES lanes of each of WAVES wavefronts hold a row: every LANES * WAVES-th of its vectors of 16 bytes, VECS a lane (or none, and an element each, of rows
+// shorter than that).  RAGGED: d is no multiple of a vector; the last one then ends with the row and has elements in common with the one before.  A lane to
+// which nothing is left takes the last vector once more.  What lanes have in common they compute and store alike, bit for bit, and one of them adds it to
+// the sums over the row.  So no access hangs on a branch, and the compiler can tell which of the accesses in flight a wait is for.
+template <typename T, int VECS, int LANES, int WAVES, bool RAGGED_>
 struct Shape {
-  static constexpr int kVec = Row<T>::kVec, kN = E / kVec, kStep = LANES * WAVES * kVec;
+  typedef T type;
+  static constexpr bool RAGGED = RAGGED_;
+  static constexpr int kVec = VECS ? Row<T>::kVec : 1, kN = VECS ? VECS : 1, kStep = LANES * WAVES * kVec, kE = kN * kVec;  // kE: elements of a lane
+  static constexpr int kLanes = LANES, kWaves = WAVES, kCover = kN * kStep;
   static constexpr int kThreads = WAVES > 4 ? 64 * WAVES : WAVES == 2 ? 128 : 256;
-  static constexpr int kRows = kThreads / (LANES * WAVES);  // rows a work-group holds at a time
+  static constexpr int kRows = kThreads / (LANES * WAVES);  // workers of a work-group
+  typedef T vec __attribute__((ext_vector_type(kVec), aligned(sizeof(T))));
   static __device__ __forceinline__ int worker() { return WAVES > 1 ? 0 : threadIdx.x / LANES; }
-  static __device__ __forceinline__ int column() { return (WAVES > 1 ? threadIdx.x : threadIdx.x % LANES) * kVec; }
+  static __device__ __forceinline__ int lane() { return WAVES > 1 ? threadIdx.x : threadIdx.x % LANES; }
 };
-#define NORM_SHAPE(T, E, LANES, WAVES)              \
-  using S = Shape<T, E, LANES, WAVES>;              \
-  constexpr int VEC = S::kVec, NV = S::kN, STEP = S::kStep
+template <typename S>
+struct Columns {
+  int at[S::kN];    // the first column of every vector
+  int skip[S::kN];  // and how many of its elements, from its first, another lane adds up
+  __device__ __forceinline__ explicit Columns(int d) {
+#pragma unroll
+    for (int i = 0; i < S::kN; ++i) {
+      const int c = S::lane() * S::kVec + i * S::kStep;
+      at[i] = min(c, d - S::kVec);
+      skip[i] = min(c - at[i], S::kVec);
+    }
+  }
+};
 
-template <bool RAGGED, typename S, typename T, int E>
-__device__ __forceinline__ void ld_all(const T* row, int c0, int d, float (&v)[E]) {
+// A lane's share of a row, as it lies in memory; converted where it is used.
+template <typename S>
+struct Share {
+  typedef typename S::type T;
+  typedef typename S::vec vec;
+  vec v[S::kN];
+  __device__ __forceinline__ float operator()(int e) const { return (float)v[e / S::kVec][e % S::kVec]; }
+  __device__ __forceinline__ void load(const void* base, int64_t at, const Columns<S>& c) {
 #pragma unroll
-  for (int i = 0; i < S::kN; ++i) ld_row<RAGGED>(row, c0 + i * S::kStep, d, v + i * S::kVec);
+    for (int i = 0; i < S::kN; ++i) v[i] = *reinterpret_cast<const vec*>(static_cast<const T*>(base) + at + c.at[i]);
+  }
+  __device__ __forceinline__ void store(void* base, int64_t at, const Columns<S>& c) const {
+#pragma unroll
+    for (int i = 0; i < S::kN; ++i) *reinterpret_cast<vec*>(static_cast<T*>(base) + at + c.at[i]) = v[i];
+  }
+  // Past the caches.  (The empty asm keeps the compiler from merging these stores with ordinary ones on the other side of a branch, as which both would end up.)
+  __device__ __forceinline__ void store_nt(void* base, int64_t at, const Columns<S>& c) const {
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < S::kN; ++i) __builtin_nontemporal_store(v[i], reinterpret_cast<vec*>(static_cast<T*>(base) + at + c.at[i]));
+    asm volatile("" ::: "memory");
+  }
+  __device__ __forceinline__ void set(const float (&x)[S::kE]) {
+#pragma unroll
+    for (int e = 0; e < S::kE; ++e) v[e / S::kVec][e % S::kVec] = (T)x[e];
+  }
+  __device__ __forceinline__ void fill(float x) {
+#pragma unroll
+    for (int e = 0; e < S::kE; ++e) v[e / S::kVec][e % S::kVec] = (T)x;
+  }
+  // What was loaded has arrived.  Asked for ahead of a row's stores, which the next wait for a load would otherwise wait for too (both count down one counter, in order).
+  __device__ __forceinline__ void arrive() {
+#pragma unroll
+    for (int i = 0; i < S::kN; ++i) {
+      if constexpr (S::kVec > 1) {
+        asm volatile("" : "+v"(v[i]));
+      } else {
+        T t = v[i][0];
+        if constexpr (sizeof(T) == 4) {
+          asm volatile("" : "+v"(t));
+        } else {
+          uint16_t bits = __builtin_bit_cast(uint16_t, t);
+          asm volatile("" : "+v"(bits));
+          t = __builtin_bit_cast(T, bits);
+        }
+        v[i][0] = t;
+      }
+    }
+  }
+};
+// Sum over a lane's own elements of f(element).
+template <typename S, typename F>
+__device__ __forceinline__ float own_sum(const Columns<S>& c, F f) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < S::kN; ++i) {
+    float p = 0.f;
+#pragma unroll
+    for (int e = 0; e < S::kVec; ++e) {
+      const float x = f(i * S::kVec + e);
+      p += !S::RAGGED || e >= c.skip[i] ? x : 0.f;
+    }
+    s += S::RAGGED || c.skip[i] == 0 ? p : 0.f;
+  }
+  return s;
 }
-template <bool RAGGED, typename S, typename T, int E>
-__device__ __forceinline__ void st_all(T* row, int c0, int d, const float (&v)[E]) {
+// Sums in fp32.
+template <typename S>
+__device__ __forceinline__ void st_sums(float* row, const Columns<S>& c, const float (&x)[S::kE]) {
+  typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-  for (int i = 0; i < S::kN; ++i) st_row<RAGGED>(row, c0 + i * S::kStep, d, v + i * S::kVec);
+  for (int i = 0; i < S::kN; ++i) {
+    if constexpr (S::kVec == 1) {
+      row[c.at[i]] = x[i];
+    } else {
+#pragma unroll
+      for (int e = 0; e < S::kVec; e += 4)
+        *reinterpret_cast<any4*>(row + c.at[i] + e) = any4{x[i * S::kVec + e], x[i * S::kVec + e + 1], x[i * S::kVec + e + 2], x[i * S::kVec + e + 3]};
+    }
+  }
+}
+template <int E>
+__device__ __forceinline__ void fill(float (&v)[E], float x) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = x;
 }
 
-// Sums in fp32: whole vectors, up to the pitch of their rows, a multiple of eight.
-template <typename S, int E>
-__device__ __forceinline__ void st_sums(float* row, int c0, int d, const float (&v)[E]) {
-#pragma unroll
-  for (int i = 0; i < S::kN; ++i)
-    if (const int c = c0 + i * S::kStep; c < d)
-#pragma unroll
-      for (int e = 0; e < S::kVec; e += 4) *reinterpret_cast<floatx4*>(row + c + e) = floatx4{v[i * S::kVec + e], v[i * S::kVec + e + 1], v[i * S::kVec + e + 2], v[i * S::kVec + e + 3]};
-}
+// Which gate a worker's rows take: one for all rows or none (GROUPED = false), or row after row the one of row / rows_per_gate.
+struct GateRows {
+  int64_t row = -1, end = 0;  // the gate at hand, and the row behind its last
+  __device__ __forceinline__ bool next(int64_t r, int rows_per_gate) {  // whether row r, the one behind the last asked for, takes another one
+    if (r < end) return false;
+    row = row < 0 ? (int64_t)((uint32_t)r / (uint32_t)rows_per_gate) : row + 1;
+    end = (row + 1) * rows_per_gate;
+    return true;
+  }
+};
 
-template <typename T, int E, int LANES, int WAVES, bool RAGGED>
-__global__ void __launch_bounds__((Shape<T, E, LANES, WAVES>::kThreads)) gated_norm_fwd_kernel(const NormArgs a) {
-  NORM_SHAPE(T, E, LANES, WAVES);
+// Forward.  Gains, shifts and a gate for all rows stay in registers, and a worker's next row is asked for before the one at hand is worked on.
+template <typename S, bool GROUPED>
+__global__ void __launch_bounds__(S::kThreads) gated_norm_fwd_kernel(const NormArgs a) {
+  constexpr int E = S::kE, LANES = S::kLanes, WAVES = S::kWaves;
+  using V = Share<S>;
   __shared__ float red[2][WAVES];
-  const int c0 = S::column(), d = a.d;
+  touch(a);
+  const int d = a.d;
+  const Columns<S> c(d);
   const float inv_d = 1.f / (float)d;
+  const int64_t worker = (int64_t)blockIdx.x * S::kRows + S::worker();
+  const int64_t begin = min(worker * a.chunk, (int64_t)a.rows), end = min(begin + a.chunk, (int64_t)a.rows);
+  V post_gain, post_shift, pre_gain, pre_shift, gate, next_gate, next_x, next_y;
+  if (a.post_gain) post_gain.load(a.post_gain, 0, c);
+  if (a.post_shift) post_shift.load(a.post_shift, 0, c);
+  if (!GROUPED && a.gate) gate.load(a.gate, 0, c);
+  if (a.n) pre_gain.load(a.pre_gain, 0, c);
+  if (a.pre_shift) pre_shift.load(a.pre_shift, 0, c);
+  auto ask = [&](int64_t row) {
+    next_x.load(a.x, row * a.ld_x, c);
+    if (a.y) next_y.load(a.y, row * a.ld_y, c);
+    if (GROUPED) {
+      uint32_t rest;
+      next_gate.load(a.gate, (int64_t)div_mod((uint32_t)row, a.per_gate, rest) * d, c);
+    }
+  };
   // v -> (v - mean) / sqrt(mean((v - mean)^2) + eps), two passes over the registers
   auto normalise = [&](float (&v)[E], float& mean, float& rstd) {
     mean = 0.f;
     if (a.kind == NMT_NORM_LAYER) {
-      float s = 0.f;
+      mean = row_sum<LANES, WAVES>(own_sum<S>(c, [&](int e) { return v[e]; }), red[0]) * inv_d;
 #pragma unroll
-      for (int e = 0; e < E; ++e) s += v[e];
-      mean = row_sum<LANES, WAVES>(s, red[0]) * inv_d;
+      for (int e = 0; e < E; ++e) v[e] -= mean;
     }
-    float q = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        float& x = v[i * VEC + e];
-        const int c = c0 + i * STEP;
-        x = (RAGGED ? c + e < d : c < d) ? x - mean : 0.f;
-        q += x * x;
-      }
-    rstd = 1.f / sqrtf(row_sum<LANES, WAVES>(q, red[1]) * inv_d + a.eps);
+    rstd = 1.f / sqrtf(row_sum<LANES, WAVES>(own_sum<S>(c, [&](int e) { return v[e] * v[e]; }), red[1]) * inv_d + a.eps);
     if (WAVES > 1 && a.kind != NMT_NORM_LAYER) __syncthreads();  // (red[1] may be next)
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] *= rstd;
   };
-  auto affine = [&](float (&v)[E], const void* gain, const void* shift) {
-    float g[E];
-    ld_all<RAGGED, S>(static_cast<const T*>(gain), c0, d, g);
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] *= g[e];
-    if (shift) {
-      ld_all<RAGGED, S>(static_cast<const T*>(shift), c0, d, g);
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] += g[e];
-    }
-  };
-  const int64_t stride = (int64_t)gridDim.x * S::kRows;
-  for (int64_t row = (int64_t)blockIdx.x * S::kRows + S::worker(); row < a.rows; row += stride) {
+  if (begin < end) ask(begin);
+  for (int64_t row = begin; row < end; ++row) {
+    const V x = next_x, y = next_y;
+    if (GROUPED) gate = next_gate;
+    if (row + 1 < end) ask(row + 1);
+    __builtin_amdgcn_sched_barrier(0);
     float h[E], mean_y = 0.f, rstd_y = 1.f, mean_h = 0.f, rstd_h = 1.f;
-    ld_all<RAGGED, S>(static_cast<const T*>(a.x) + row * a.ld_x, c0, d, h);
+    V out_h, out_n;
+#pragma unroll
+    for (int e = 0; e < E; ++e) h[e] = x(e);
     if (a.y) {
-      float y[E];
-      ld_all<RAGGED, S>(static_cast<const T*>(a.y) + row * a.ld_y, c0, d, y);
+      float z[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) z[e] = y(e);
       if (a.post_gain) {
-        normalise(y, mean_y, rstd_y);
-        affine(y, a.post_gain, a.post_shift);
-      }
-      if (a.gate) {
-        float g[E];
-        ld_all<RAGGED, S>(static_cast<const T*>(a.gate) + (int64_t)((uint32_t)row / (uint32_t)a.rows_per_gate) * d, c0, d, g);
+        normalise(z, mean_y, rstd_y);
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] *= g[e];
-      }
+        for (int e = 0; e < E; ++e) z[e] *= post_gain(e);
+        if (a.post_shift)
 #pragma unroll
-      for (int e = 0; e < E; ++e) h[e] = a.resid_scale * h[e] + y[e];
-      st_all<RAGGED, S>(static_cast<T*>(a.h) + row * a.ld_h, c0, d, h);
+          for (int e = 0; e < E; ++e) z[e] += post_shift(e);
+      }
+      if (a.gate)
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] *= gate(e);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[e] = a.resid_scale * h[e] + z[e];
+      out_h.set(h);
     }
     if (a.n) {
       normalise(h, mean_h, rstd_h);
-      affine(h, a.pre_gain, a.pre_shift);
-      st_all<RAGGED, S>(static_cast<T*>(a.n) + row * a.ld_n, c0, d, h);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[e] *= pre_gain(e);
+      if (a.pre_shift)
+#pragma unroll
+        for (int e = 0; e < E; ++e) h[e] += pre_shift(e);
+      out_n.set(h);
     }
-    if (a.stats && c0 == 0) *reinterpret_cast<float4_any*>(a.stats + 4 * row) = float4_any{mean_y, rstd_y, mean_h, rstd_h};
+    next_x.arrive();
+    if (a.y) next_y.arrive();
+    if (GROUPED) next_gate.arrive();
+    if (a.stream) {
+      if (a.y) out_h.store_nt(a.h, row * a.ld_h, c);
+      if (a.n) out_n.store_nt(a.n, row * a.ld_n, c);
+    } else {
+      if (a.y) out_h.store(a.h, row * a.ld_h, c);
+      if (a.n) out_n.store(a.n, row * a.ld_n, c);
+    }
+    if (a.stats && S::lane() == 0) *reinterpret_cast<float4_any*>(a.stats + 4 * row) = float4_any{mean_y, rstd_y, mean_h, rstd_h};
   }
 }
 
-// Backward.  A worker (the lanes that hold a row) takes `chunk` rows in a row and keeps four column sums in registers: of dh yhat and dh, from which
-// the gradients of post's gain and shift (times the gate) and of the gate (gain, shift times the two) follow, and of dn hhat and dn.
-// One gate for all (GROUPED = false): the factors are applied to the totals.  Otherwise whenever a gate's rows end: its gradient is written if
-// all its rows were this worker's, and else left as a partial sum, of which a worker has two at most (the gate it begins in, begun before it, and the one it ends in).
-template <typename T, int E, int LANES, int WAVES, bool RAGGED, bool GROUPED>
-__global__ void __launch_bounds__((Shape<T, E, LANES, WAVES>::kThreads)) gated_norm_bwd_kernel(const NormArgs a) {
-  NORM_SHAPE(T, E, LANES, WAVES);
+// Backward.  A worker takes `chunk` rows in a row and keeps column sums in registers, of dn hhat (0) for the gain before the next block, of D yhat (1)
+// for the gain after this one, D = dh, and, if there are SHIFTS, of dn (2) and D (3) for the shifts.  One gate for all rows (or none): the gradients of gain,
+// shift and gate all follow from the totals over dh.  GROUPED: D = gate dh, and the gate's gradient is a sum of its own, over its rows; where the gate's
+// rows end it is written if all of them were this worker's, and else left as a partial sum, of which a worker has two at most (of the gate it
+// begins in, if that began before it, and of the one it ends in).
+template <typename S, bool GROUPED, bool SHIFTS>
+__global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 : S::kWaves > 8 ? 4 : 1) gated_norm_bwd_kernel(const NormArgs a) {
+  constexpr int E = S::kE, LANES = S::kLanes, WAVES = S::kWaves, SUMS = SHIFTS ? 4 : 2;
+  using V = Share<S>;
   __shared__ float red[4][WAVES];
-  __shared__ float sums[S::kRows > 1 ? S::kRows * LANES * E : 1];
-  const int c0 = S::column(), d = a.d;
+  __shared__ __attribute__((aligned(16))) float sums[S::kRows > 1 ? SUMS : 1][S::kRows > 1 ? S::kRows * S::kCover : 1];
+  touch(a);
+  const int d = a.d;
+  const Columns<S> c(d);
   const float inv_d = 1.f / (float)d;
   const int64_t worker = (int64_t)blockIdx.x * S::kRows + S::worker();
   const int64_t begin = min(worker * a.chunk, (int64_t)a.rows), end = min(begin + a.chunk, (int64_t)a.rows);
-  auto fill = [](float (&v)[E], float x) {
+  V gain, shift, pre, gate, next_gate, next_dh, next_dn, next_h, next_y;
+  float4_any next_st;
+  gain.fill(1.f), shift.fill(0.f), gate.fill(1.f), next_dh.fill(0.f);  // (where there is none)
+  if (a.post_gain) gain.load(a.post_gain, 0, c);
+  if (GROUPED && SHIFTS && a.post_shift) shift.load(a.post_shift, 0, c);
+  if (!GROUPED && a.gate) gate.load(a.gate, 0, c);
+  if (a.dn) pre.load(a.pre_gain, 0, c);
+  float sum[SUMS][E], gate_sum[GROUPED ? E : 1];
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = x;
-  };
-  float gain[E], shift[E], gate[E], pre[E];  // 1, 0, 1, - where there is none
-  fill(gain, 1.f), fill(shift, 0.f), fill(gate, 1.f), fill(pre, 0.f);
-  if (a.post_gain) ld_all<RAGGED, S>(static_cast<const T*>(a.post_gain), c0, d, gain);
-  if (GROUPED && a.post_shift) ld_all<RAGGED, S>(static_cast<const T*>(a.post_shift), c0, d, shift);
-  if (!GROUPED && a.gate) ld_all<RAGGED, S>(static_cast<const T*>(a.gate), c0, d, gate);
-  if (a.dn) ld_all<RAGGED, S>(static_cast<const T*>(a.pre_gain), c0, d, pre);
-  float sum_a[E], sum_b[E], sum_p[E], sum_q[E], gate_a[E], gate_b[E];
-  fill(sum_a, 0.f), fill(sum_b, 0.f), fill(sum_p, 0.f), fill(sum_q, 0.f);
-  int64_t gate_row = -1, gate_end = begin;  // the gate at hand and the row behind its last here
-  auto close_gate = [&](int64_t row) {      // (row: the one behind its last of this worker)
-    if (gate_row < 0) return;
-    float g[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      sum_a[e] += gate[e] * gate_a[e];
-      sum_b[e] += gate[e] * gate_b[e];
-      g[e] = gain[e] * gate_a[e] + shift[e] * gate_b[e];
-    }
-    if (!a.dgate) return;
-    const int64_t first = gate_row * a.rows_per_gate, last = min(first + a.rows_per_gate, (int64_t)a.rows);
-    if (first >= begin && last <= row) {
-      st_all<RAGGED, S>(static_cast<T*>(a.dgate) + gate_row * d, c0, d, g);
-    } else {
-      st_sums<S>(a.gate_partial + (2 * worker + (first >= begin)) * a.pitch, c0, d, g);
-    }
-  };
-  for (int64_t row = begin; row < end; ++row) {
-    if (GROUPED && row == gate_end) {
-      close_gate(row);
-      gate_row = (uint32_t)row / (uint32_t)a.rows_per_gate;
-      gate_end = min((gate_row + 1) * a.rows_per_gate, end);
-      ld_all<RAGGED, S>(static_cast<const T*>(a.gate) + gate_row * d, c0, d, gate);
-      fill(gate_a, 0.f), fill(gate_b, 0.f);
-    }
-    const float4_any st = *reinterpret_cast<const float4_any*>(a.stats + 4 * row);
-    float dh[E];
-    fill(dh, 0.f);
-    if (a.dh) ld_all<RAGGED, S>(static_cast<const T*>(a.dh) + row * a.ld_dh, c0, d, dh);
+  for (int q = 0; q < SUMS; ++q) fill(sum[q], 0.f);
+  GateRows gates;
+  int64_t gate_row = -1;  // of the rows at hand
+  bool other_gate = false;
+  auto ask = [&](int64_t row) {
+    next_st = *reinterpret_cast<const float4_any*>(a.stats + 4 * row);
     if (a.dn) {
-      float h[E], dn[E];
-      ld_all<RAGGED, S>(static_cast<const T*>(a.h) + row * a.ld_h, c0, d, h);
-      ld_all<RAGGED, S>(static_cast<const T*>(a.dn) + row * a.ld_dn, c0, d, dn);
-      float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        h[e] = (h[e] - st[2]) * st[3];
-        sum_p[e] += dn[e] * h[e];
-        sum_q[e] += dn[e];
-        dn[e] *= pre[e];
-        s1 += dn[e];
-        s2 += dn[e] * h[e];
-      }
-      const float m1 = a.kind == NMT_NORM_LAYER ? row_sum<LANES, WAVES>(s1, red[0]) * inv_d : 0.f;
-      const float m2 = row_sum<LANES, WAVES>(s2, red[1]) * inv_d;
-#pragma unroll
-      for (int e = 0; e < E; ++e) dh[e] += st[3] * (dn[e] - m1 - h[e] * m2);
+      next_h.load(a.h, row * a.ld_h, c);
+      next_dn.load(a.dn, row * a.ld_dn, c);
     }
-    float out[E];
+    if (a.dh) next_dh.load(a.dh, row * a.ld_dh, c);
+    if (a.y) next_y.load(a.y, row * a.ld_y, c);
+    if (GROUPED) {
+      other_gate = gates.next(row, a.rows_per_gate);
+      if (other_gate) next_gate.load(a.gate, gates.row * d, c);
+    }
+  };
+  auto close_gate = [&](int64_t row) {  // row: the one behind its last of this worker
+    if constexpr (GROUPED) {
+      if (gate_row >= 0 && a.dgate) {
+        const int64_t first = gate_row * a.rows_per_gate, last = min(first + a.rows_per_gate, (int64_t)a.rows);
+        if (first >= begin && last <= row) {
+          V out;
+          out.set(gate_sum);
+          out.store(a.dgate, gate_row * d, c);
+        }
+        else st_sums<S>(a.gate_partial + (2 * worker + (first >= begin)) * a.pitch, c, gate_sum);
+      }
+      fill(gate_sum, 0.f);
+    }
+  };
+  if (begin < end) ask(begin);
+  for (int64_t row = begin; row < end; ++row) {
+    const V dh = next_dh, dn = next_dn, h = next_h, y = next_y;
+    const float4_any st = next_st;
+    if (GROUPED && other_gate) {
+      close_gate(row);
+      gate = next_gate;
+      gate_row = gates.row;
+    }
+    if (row + 1 < end) ask(row + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    float g[E];  // the gradient at h
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[e] = a.resid_scale * dh[e];
-    st_all<RAGGED, S>(static_cast<T*>(a.dx) + row * a.ld_dx, c0, d, out);
-    if (a.y) {
-      float y[E];
-      ld_all<RAGGED, S>(static_cast<const T*>(a.y) + row * a.ld_y, c0, d, y);
-      float s3 = 0.f, s4 = 0.f;
+    for (int e = 0; e < E; ++e) g[e] = dh(e);
+    if (a.dn) {
+      const float rstd = st[3], off = -st[2] * st[3];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        y[e] = (y[e] - st[0]) * st[1];
-        float& ga = GROUPED ? gate_a[e] : sum_a[e];
-        float& gb = GROUPED ? gate_b[e] : sum_b[e];
-        ga += dh[e] * y[e];
-        gb += dh[e];
-        out[e] = gate[e] * dh[e] * gain[e];
-        s3 += out[e];
-        s4 += out[e] * y[e];
+        sum[0][e] += dn(e) * (h(e) * rstd + off);
+        if (SHIFTS) sum[SUMS - 2][e] += dn(e);
+      }
+      const float m1 = a.kind == NMT_NORM_LAYER ? row_sum<LANES, WAVES>(own_sum<S>(c, [&](int e) { return dn(e) * pre(e); }), red[0]) * inv_d : 0.f;
+      const float m2 = row_sum<LANES, WAVES>(own_sum<S>(c, [&](int e) { return dn(e) * pre(e) * (h(e) * rstd + off); }), red[1]) * inv_d;
+#pragma unroll
+      for (int e = 0; e < E; ++e) g[e] += rstd * (dn(e) * pre(e) - m1 - (h(e) * rstd + off) * m2);
+    }
+    V out_x, out_y;
+    {
+      float out[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) out[e] = a.resid_scale * g[e];
+      out_x.set(out);
+    }
+    if (a.y) {
+      const float rstd = st[1], off = -st[0] * st[1];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float yhat = y(e) * rstd + off;
+        if constexpr (GROUPED) gate_sum[e] += g[e] * (SHIFTS ? yhat * gain(e) + shift(e) : yhat * gain(e));
+        const float dz = gate(e) * g[e], at = GROUPED ? dz : g[e];
+        sum[1][e] += at * yhat;
+        if (SHIFTS) sum[SUMS - 1][e] += at;
+        g[e] = dz * gain(e);
       }
       if (a.post_gain) {
-        const float m3 = a.kind == NMT_NORM_LAYER ? row_sum<LANES, WAVES>(s3, red[2]) * inv_d : 0.f;
-        const float m4 = row_sum<LANES, WAVES>(s4, red[3]) * inv_d;
+        const float m3 = a.kind == NMT_NORM_LAYER ? row_sum<LANES, WAVES>(own_sum<S>(c, [&](int e) { return g[e]; }), red[2]) * inv_d : 0.f;
+        const float m4 = row_sum<LANES, WAVES>(own_sum<S>(c, [&](int e) { return g[e] * (y(e) * rstd + off); }), red[3]) * inv_d;
 #pragma unroll
-        for (int e = 0; e < E; ++e) out[e] = st[1] * (out[e] - m3 - y[e] * m4);
+        for (int e = 0; e < E; ++e) g[e] = rstd * (g[e] - m3 - (y(e) * rstd + off) * m4);
       }
-      st_all<RAGGED, S>(static_cast<T*>(a.dy) + row * a.ld_dy, c0, d, out);
+      out_y.set(g);
     }
+    if (a.dn) next_h.arrive(), next_dn.arrive();
+    if (a.dh) next_dh.arrive();
+    if (a.y) next_y.arrive();
+    asm volatile("" : "+v"(next_st));
+    out_x.store(a.dx, row * a.ld_dx, c);
+    if (a.y) out_y.store(a.dy, row * a.ld_dy, c);
     if (WAVES > 1) __syncthreads();  // (the sums' places are used again)
   }
-  if (GROUPED) close_gate(end);
+  close_gate(end);
   // the work-group's column sums: its workers' in increasing order
-  auto leave = [&](float (&v)[E], int which) {
-    float* out = a.partial + ((int64_t)blockIdx.x * 4 + which) * a.pitch;
-    if constexpr (S::kRows == 1) {
-      st_sums<S>(out, c0, d, v);
-    } else {
-      __syncthreads();
+  float* out = a.partial + (int64_t)blockIdx.x * SUMS * a.pitch;
+  if constexpr (S::kRows == 1) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
+    for (int q = 0; q < SUMS; ++q) st_sums<S>(out + (int64_t)q * a.pitch, c, sum[q]);
+  } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sums[(size_t)S::worker() * LANES * E + c0 + i * STEP + e] = v[i * VEC + e];
-      __syncthreads();
-      for (int c = threadIdx.x; c < d; c += S::kThreads) {
-        float t = sums[c];
+    for (int q = 0; q < SUMS; ++q) st_sums<S>(sums[q] + S::worker() * S::kCover, c, sum[q]);
+    __syncthreads();
+    for (int i = threadIdx.x; i < d; i += S::kThreads)
 #pragma unroll
-        for (int w = 1; w < S::kRows; ++w) t += sums[w * LANES * E + c];
-        out[c] = t;
+      for (int q = 0; q < SUMS; ++q) {
+        float t = sums[q][i];
+#pragma unroll
+        for (int w = 1; w < S::kRows; ++w) t += sums[q][w * S::kCover + i];
+        out[(int64_t)q * a.pitch + i] = t;
       }
-    }
-  };
-  leave(sum_a, 0);
-  leave(sum_b, 1);
-  leave(sum_p, 2);
-  leave(sum_q, 3);
+  }
 }
 
-constexpr int kSumCols = 32, kSumLanes = 32;  // of a work-group of the last kernel
+constexpr int kSumCols = 32, kSumLanes = 32, kSumAhead = 8;  // of a work-group of the last kernel
 
 // Totals over the work-groups' partial sums, in a fixed order, and the gradients that follow from them; behind those work-groups
 // the gates whose rows several workers had.
 template <typename T, bool GROUPED>
 __global__ void __launch_bounds__(kSumCols* kSumLanes) gated_norm_sums_kernel(const NormArgs a) {
+  touch(a);
   const int cblocks = (a.d + kSumCols - 1) / kSumCols;
   const int cx = threadIdx.x % kSumCols, ry = threadIdx.x / kSumCols;
   if (GROUPED && (int)blockIdx.x >= 2 * cblocks) {
@@ -313,92 +444,130 @@ __global__ void __launch_bounds__(kSumCols* kSumLanes) gated_norm_sums_kernel(co
     return;
   }
   __shared__ float red[2][kSumLanes][kSumCols + 1];
-  const int pair = blockIdx.x / cblocks, c = (blockIdx.x % cblocks) * kSumCols + cx;
+  const int which = blockIdx.x / cblocks, c = (blockIdx.x % cblocks) * kSumCols + cx;  // 0: before the next block, 1: after this one
   float s = 0.f, t = 0.f;
-  if (c < a.d)
-    for (int b = ry; b < a.groups; b += kSumLanes) {
-      const float* p = a.partial + ((int64_t)b * 4 + 2 * pair) * a.pitch + c;
-      s += p[0];
-      t += p[a.pitch];
-    }
+  if (c < a.d) {
+    auto total = [&](int q) {
+      const float* p = a.partial + (int64_t)q * a.pitch + c;
+      const int64_t step = (int64_t)a.sums * a.pitch;
+      float sum = 0.f;
+      for (int b = ry; b < a.groups; b += kSumLanes * kSumAhead) {
+        float v[kSumAhead];
+#pragma unroll
+        for (int u = 0; u < kSumAhead; ++u) v[u] = p[min(b + u * kSumLanes, a.groups - 1) * step];
+#pragma unroll
+        for (int u = 0; u < kSumAhead; ++u) sum += b + u * kSumLanes < a.groups ? v[u] : 0.f;
+      }
+      return sum;
+    };
+    s = total(which);
+    if (a.sums > 2) t = total(which + 2);
+  }
   red[0][ry][cx] = s;
   red[1][ry][cx] = t;
   __syncthreads();
-  if (ry || c >= a.d) return;
-  for (int r = 1; r < kSumLanes; ++r) {
-    s += red[0][r][cx];
-    t += red[1][r][cx];
-  }
-  auto at = [&](const void* p, float none) { return p ? (float)static_cast<const T*>(p)[c] : none; };
+  // half a wavefront for a column
+  static_assert(kSumLanes == 32, "");
+  const int lane = threadIdx.x % 32, mine = threadIdx.x / 32, col = c - cx + mine;
+  s = row_sum<32, 1>(red[0][lane][mine], nullptr);
+  t = row_sum<32, 1>(red[1][lane][mine], nullptr);
+  if (lane || col >= a.d) return;
+  auto at = [&](const void* p, float none) { return p ? (float)static_cast<const T*>(p)[col] : none; };
   auto put = [&](void* p, float v) {
-    if (p) static_cast<T*>(p)[c] = (T)v;
+    if (p) static_cast<T*>(p)[col] = (T)v;
   };
-  if (pair) {
+  if (which == 0) {
     put(a.dpre_gain, s);
     put(a.dpre_shift, t);
   } else {
     const float gate = GROUPED ? 1.f : at(a.gate, 1.f);
     put(a.dpost_gain, gate * s);
     put(a.dpost_shift, gate * t);
-    if (!GROUPED) put(a.dgate, at(a.post_gain, 1.f) * s + at(a.post_shift, 0.f) * t);
+    if (!GROUPED) put(a.dgate, at(a.post_gain, 1.f) * s + (a.post_shift ? at(a.post_shift, 0.f) * t : 0.f));
   }
 }
 
-// What a row of d columns is held by: 0: 16 lanes of 8 columns, 1: 64 of 8, 2: 64 of 16, 3 to 6: 2, 4, 8, 16 wavefronts of 16 columns a lane.
-int shape_of(int d) {
+// What a row of d columns is held by: -1: 16 lanes of one column (of less than a vector), 0, 1, 2: 16, 32, 64 lanes of 8, 3 to 6: wavefronts of 8 columns a lane forward and of 16
+// backward, 7: 16 wavefronts of 16.
+int shape_of(int d, int type) {
+  if (d < 16 / row_type_bytes(type)) return -1;
   int s = 0;
-  for (int most = 128; s < 6 && d > most; ++s) most = s == 0 ? 512 : most * 2;
+  for (int most = 128; s < 7 && d > most; ++s) most *= 2;
   return s;
 }
-int rows_at_a_time(int shape) { return shape == 0 ? 16 : shape <= 2 ? 4 : 1; }
-int threads_of(int shape) { return shape <= 2 ? 256 : 64 << (shape - 2); }
+int waves_of_row(int shape, bool wide) { return shape <= 2 ? 1 : wide ? std::min(16, 2 << (shape - 3)) : 1 << (shape - 3); }
+int workers_of(int shape, bool wide) { return shape <= 0 ? 16 : shape == 1 ? 8 : waves_of_row(shape, wide) == 1 ? 4 : 1; }  // of a work-group
+bool wide_bwd(int type) { return type == NMT_F32; }
 
-constexpr int kFwdGroups = 2048, kBwdWaves = 2048;
+// Forward: two rows a worker, so that the second's loads are under way while the first is worked on and gains are fetched half as often, if that still makes
+// kFwdWaves wavefronts, and one otherwise (26001 x 1024 fp16, one row, two, three: 48, 43, 45 us; 2001 x 8000 fp32, one, two: 68, 61).
+// Backward: every work-group leaves a row of column sums, so no more of them than run side by side (kBwdWaves: a wavefront per SIMD with its
+// registers full; 1280, 2048 and 3072 cost 26001 x 1024 fp16 90, 75 and 78 us instead of 74, and 3584 x 512 15, 14 and 15 instead of 13).
+constexpr int kFwdWaves = 4096, kBwdWaves = 1024;
+constexpr int64_t kStreamFrom = 64 << 20;  // bytes of a result
 
-struct BwdPlan {
+struct Split {
   int chunk, groups, workers, pitch;
 };
-BwdPlan bwd_plan(int rows, int d) {
-  const int shape = shape_of(d), at_once = rows_at_a_time(shape);
-  const int most = kBwdWaves / (threads_of(shape) / 64);
-  BwdPlan p;
-  p.chunk = std::max<int64_t>(1, ((int64_t)rows + (int64_t)most * at_once - 1) / ((int64_t)most * at_once));
-  p.groups = (int)(((int64_t)rows + (int64_t)p.chunk * at_once - 1) / ((int64_t)p.chunk * at_once));
+Split split_rows(int rows, int d, int type, bool wide, bool forward, int rows_per_gate) {
+  const int shape = shape_of(d, type), at_once = workers_of(shape, wide), waves = std::max(at_once > 1 ? 4 : 1, waves_of_row(shape, wide));
+  Split p;
+  if (forward) {
+    p.chunk = (int64_t)rows * waves >= (int64_t)2 * kFwdWaves * at_once ? 2 : 1;
+  } else {
+    p.chunk = ceil_div(rows, kBwdWaves / waves * at_once);
+    if (rows_per_gate < rows && rows_per_gate <= 2 * (int64_t)p.chunk) p.chunk = ceil_div(p.chunk, rows_per_gate) * rows_per_gate;  // no gate's rows are two workers' then
+  }
+  p.groups = ceil_div(rows, p.chunk * at_once);
   p.workers = p.groups * at_once;
   p.pitch = (d + 7) / 8 * 8;
   return p;
 }
 int64_t scratch_floats(int rows, int d, int rows_per_gate) {
-  const BwdPlan p = bwd_plan(rows, d);
-  return (int64_t)p.groups * 4 * p.pitch + (rows_per_gate < rows ? (int64_t)p.workers * 2 * p.pitch : 0);
+  int64_t most = 0;
+  for (int type : {NMT_F16, NMT_F32}) {
+    const Split p = split_rows(rows, d, type, wide_bwd(type), false, rows_per_gate);
+    most = std::max(most, (int64_t)p.groups * 4 * p.pitch + (rows_per_gate < rows ? (int64_t)p.workers * 2 * p.pitch : 0));
+  }
+  return most;
 }
 
-#define NORM_LAUNCH(KERNEL, T, E, LANES, WAVES, ...)                                                                              \
-  if (ragged)                                                                                                                     \
-    hipLaunchKernelGGL((KERNEL<T, E, LANES, WAVES, true, ##__VA_ARGS__>), grid, dim3(Shape<T, E, LANES, WAVES>::kThreads), 0, stream, a); \
-  else                                                                                                                            \
-    hipLaunchKernelGGL((KERNEL<T, E, LANES, WAVES, false, ##__VA_ARGS__>), grid, dim3(Shape<T, E, LANES, WAVES>::kThreads), 0, stream, a)
-#define NORM_SHAPES(KERNEL, T, ...)                                   \
-  switch (shape) {                                                    \
-    case 0: NORM_LAUNCH(KERNEL, T, 8, 16, 1, ##__VA_ARGS__); break;   \
-    case 1: NORM_LAUNCH(KERNEL, T, 8, 64, 1, ##__VA_ARGS__); break;   \
-    case 2: NORM_LAUNCH(KERNEL, T, 16, 64, 1, ##__VA_ARGS__); break;  \
-    case 3: NORM_LAUNCH(KERNEL, T, 16, 64, 2, ##__VA_ARGS__); break;  \
-    case 4: NORM_LAUNCH(KERNEL, T, 16, 64, 4, ##__VA_ARGS__); break;  \
-    case 5: NORM_LAUNCH(KERNEL, T, 16, 64, 8, ##__VA_ARGS__); break;  \
-    default: NORM_LAUNCH(KERNEL, T, 16, 64, 16, ##__VA_ARGS__);       \
+// WIDE: 8 columns a lane and twice the wavefronts for rows of more than 512.
+#define NORM_LAUNCH(KERNEL, T, VECS, LANES, WAVES, ...)                                                                  \
+  if ((VECS) && a.d % Row<T>::kVec) {                                                                                    \
+    using S = Shape<T, VECS, LANES, WAVES, true>;                                                                        \
+    hipLaunchKernelGGL((KERNEL<S, __VA_ARGS__>), grid, dim3(S::kThreads), 0, stream, a);                                 \
+  } else {                                                                                                               \
+    using S = Shape<T, VECS, LANES, WAVES, false>;                                                                       \
+    hipLaunchKernelGGL((KERNEL<S, __VA_ARGS__>), grid, dim3(S::kThreads), 0, stream, a);                                 \
+  }
+#define NORM_SHAPES(KERNEL, T, WIDE, ...)                                                                  \
+  constexpr int v8 = 8 / Row<T>::kVec, v = (WIDE) ? v8 : 2 * v8, w = (WIDE) ? 2 : 1;                       \
+  switch (shape) {                                                                                         \
+    case -1: NORM_LAUNCH(KERNEL, T, 0, 16, 1, __VA_ARGS__) break;                                          \
+    case 0: NORM_LAUNCH(KERNEL, T, v8, 16, 1, __VA_ARGS__) break;                                          \
+    case 1: NORM_LAUNCH(KERNEL, T, v8, 32, 1, __VA_ARGS__) break;                                          \
+    case 2: NORM_LAUNCH(KERNEL, T, v8, 64, 1, __VA_ARGS__) break;                                          \
+    case 3: NORM_LAUNCH(KERNEL, T, v, 64, w, __VA_ARGS__) break;                                           \
+    case 4: NORM_LAUNCH(KERNEL, T, v, 64, 2 * w, __VA_ARGS__) break;                                       \
+    case 5: NORM_LAUNCH(KERNEL, T, v, 64, 4 * w, __VA_ARGS__) break;                                       \
+    case 6: NORM_LAUNCH(KERNEL, T, v, 64, 8 * w, __VA_ARGS__) break;                                       \
+    default: NORM_LAUNCH(KERNEL, T, 2 * v8, 64, 16, __VA_ARGS__)                                           \
   }
 
 template <typename T>
-void launch_fwd(const NormArgs& a, dim3 grid, int shape, hipStream_t stream) {
-  const bool ragged = a.d % Row<T>::kVec != 0;
-  NORM_SHAPES(gated_norm_fwd_kernel, T);
+void launch_fwd(const NormArgs& a, dim3 grid, int shape, bool grouped, hipStream_t stream) {
+  if (grouped) { NORM_SHAPES(gated_norm_fwd_kernel, T, true, true) }
+  else { NORM_SHAPES(gated_norm_fwd_kernel, T, true, false) }
 }
 template <typename T>
 void launch_bwd(const NormArgs& a, dim3 grid, int shape, bool grouped, hipStream_t stream) {
-  const bool ragged = a.d % Row<T>::kVec != 0;
-  if (grouped) { NORM_SHAPES(gated_norm_bwd_kernel, T, true); }
-  else { NORM_SHAPES(gated_norm_bwd_kernel, T, false); }
+  constexpr bool wide = sizeof(T) == 4;  // (wide_bwd)
+  const bool shifts = a.sums > 2;
+  if (grouped && shifts) { NORM_SHAPES(gated_norm_bwd_kernel, T, wide, true, true) }
+  else if (grouped) { NORM_SHAPES(gated_norm_bwd_kernel, T, wide, true, false) }
+  else if (shifts) { NORM_SHAPES(gated_norm_bwd_kernel, T, wide, false, true) }
+  else { NORM_SHAPES(gated_norm_bwd_kernel, T, wide, false, false) }
 }
 template <typename T>
 void launch_sums(const NormArgs& a, bool grouped, hipStream_t stream) {
@@ -441,6 +610,8 @@ NormArgs common_args(const nmt_gated_norm* a) {
   k.rows = a->rows, k.d = a->d, k.kind = a->kind;
   k.rows_per_gate = a->d_gate ? a->rows_per_gate : a->rows;
   k.gates = ceil_div(a->rows, k.rows_per_gate);
+  k.per_gate = divisor((uint32_t)k.rows_per_gate);
+  k.stream = (int64_t)a->rows * a->d * row_type_bytes(a->type) >= kStreamFrom;
   k.eps = a->eps, k.resid_scale = a->resid_scale;
   k.ld_x = a->ld_x, k.ld_y = a->ld_y, k.ld_h = a->ld_h, k.ld_n = a->ld_n;
   k.x = a->d_x, k.y = a->d_y, k.h = a->d_h, k.n = a->d_n, k.stats = a->d_stats;
@@ -465,12 +636,14 @@ extern "C" int nmt_op_gated_norm_fwd(const nmt_gated_norm* a, void* stream_) {
   NORM_ROWS(a->d_y, a->ld_y, "y");
   NORM_ROWS(a->d_h, a->ld_h, "h");
   NORM_ROWS(a->d_n, a->ld_n, "n");
-  const NormArgs k = common_args(a);
-  const int shape = shape_of(a->d);
-  const dim3 grid(std::min(ceil_div(a->rows, rows_at_a_time(shape)), kFwdGroups));
-  if (a->type == NMT_F16) launch_fwd<half_t>(k, grid, shape, stream);
-  else if (a->type == NMT_BF16) launch_fwd<bf16_t>(k, grid, shape, stream);
-  else launch_fwd<float>(k, grid, shape, stream);
+  NormArgs k = common_args(a);
+  const Split p = split_rows(a->rows, a->d, a->type, true, true, a->rows);
+  k.chunk = p.chunk;
+  const bool grouped = a->d_gate && a->rows_per_gate < a->rows;
+  const int shape = shape_of(a->d, a->type);
+  if (a->type == NMT_F16) launch_fwd<half_t>(k, dim3(p.groups), shape, grouped, stream);
+  else if (a->type == NMT_BF16) launch_fwd<bf16_t>(k, dim3(p.groups), shape, grouped, stream);
+  else launch_fwd<float>(k, dim3(p.groups), shape, grouped, stream);
   NMT_LAUNCH_CHECK();
   return NMT_OK;
 }
@@ -489,7 +662,7 @@ extern "C" int nmt_op_gated_norm_bwd(const nmt_gated_norm* a, const nmt_gated_no
   if (a->rows == 0) {  // (sums over no rows)
     if (!sums) return NMT_OK;
     NormArgs k = {};
-    k.d = a->d;
+    k.d = a->d, k.sums = 4;
     k.dpost_gain = g->d_dpost_gain, k.dpost_shift = g->d_dpost_shift, k.dgate = g->d_dgate;
     k.dpre_gain = g->d_dpre_gain, k.dpre_shift = g->d_dpre_shift;
     return launch_sums(k, a->type, false, stream);
@@ -516,14 +689,15 @@ extern "C" int nmt_op_gated_norm_bwd(const nmt_gated_norm* a, const nmt_gated_no
     return NMT_ENOMEM;
   }
   NMT_REQUIRE(aligned16(g->d_scratch), "%s: the scratch buffer must be 16-byte aligned", who);
-  const BwdPlan p = bwd_plan(a->rows, a->d);
+  const Split p = split_rows(a->rows, a->d, a->type, wide_bwd(a->type), false, k.rows_per_gate);
   k.chunk = p.chunk, k.groups = p.groups, k.pitch = p.pitch;
+  k.sums = a->d_post_shift || g->d_dpost_shift || g->d_dpre_shift ? 4 : 2;
   k.partial = g->d_scratch, k.gate_partial = g->d_scratch + (int64_t)p.groups * 4 * p.pitch;
   k.ld_dh = g->ld_dh, k.ld_dn = g->ld_dn, k.ld_dx = g->ld_dx, k.ld_dy = g->ld_dy;
   k.dh = g->d_dh, k.dn = g->d_dn, k.dx = g->d_dx, k.dy = g->d_dy;
   k.dpost_gain = g->d_dpost_gain, k.dpost_shift = g->d_dpost_shift, k.dgate = g->d_dgate;
   k.dpre_gain = g->d_dpre_gain, k.dpre_shift = g->d_dpre_shift;
-  const int shape = shape_of(a->d);
+  const int shape = shape_of(a->d, a->type);
   const dim3 grid(p.groups);
   if (a->type == NMT_F16) launch_bwd<half_t>(k, grid, shape, grouped, stream);
   else if (a->type == NMT_BF16) launch_bwd<bf16_t>(k, grid, shape, grouped, stream);
