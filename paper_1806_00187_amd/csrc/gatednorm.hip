@@ -38,29 +38,15 @@ typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
 // one before this may have used, but not the last.
 template <int LANES, int WAVES>
 __device__ __forceinline__ float row_sum(float v, float* red) {
-  if constexpr (LANES == 64) {
-    v = wave_sum(v);
-    if constexpr (WAVES > 1) {
-      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-      __syncthreads();
-      v = red[0];
+  v = lanes_sum<LANES>(v);
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = red[0];
 #pragma unroll
-      for (int w = 1; w < WAVES; ++w) v += red[w];
-    }
-    return v;
-  } else {
-    auto plus = [](float x, auto ctrl) {
-      return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, true));
-    };
-    if constexpr (LANES == 32) {
-      const auto h = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
-      v = __builtin_bit_cast(float, (unsigned)h[0]) + __builtin_bit_cast(float, (unsigned)h[1]);
-    }
-    v = plus(v, std::integral_constant<int, 0x128>{});    // row_ror:8
-    v = plus(v, std::integral_constant<int, 0x124>{});    // row_ror:4
-    v = plus(v, std::integral_constant<int, 0x4E>{});     // quad_perm:[2,3,0,1]
-    return plus(v, std::integral_constant<int, 0xB1>{});  // quad_perm:[1,0,3,2]
+    for (int w = 1; w < WAVES; ++w) v += red[w];
   }
+  return v;
 }
 
 // LANES lanes of each of WAVES wavefronts hold a row: every LANES * WAVES-th of its vectors of 16 bytes, VECS a lane (or none, and an element each, of rows
@@ -469,8 +455,8 @@ __global__ void __launch_bounds__(kSumCols* kSumLanes) gated_norm_sums_kernel(co
   // half a wavefront for a column
   static_assert(kSumLanes == 32, "");
   const int lane = threadIdx.x % 32, mine = threadIdx.x / 32, col = c - cx + mine;
-  s = row_sum<32, 1>(red[0][lane][mine], nullptr);
-  t = row_sum<32, 1>(red[1][lane][mine], nullptr);
+  s = lanes_sum<32>(red[0][lane][mine]);
+  t = lanes_sum<32>(red[1][lane][mine]);
   if (lane || col >= a.d) return;
   auto at = [&](const void* p, float none) { return p ? (float)static_cast<const T*>(p)[col] : none; };
   auto put = [&](void* p, float v) {
