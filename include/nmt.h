@@ -374,7 +374,7 @@ int nmt_op_dropout_mask(uint8_t* d_keep, int32_t rows, int32_t n_cols, const nmt
  * Operators for models beyond the step above: deeper ones (norms around a gated residual block), sparse ones (tokens
  * sorted by expert and back) and larger ones (AdamW over many tensors, its states in 8 bits if wanted).
  * Rows are fp16, bf16 or fp32; sums, statistics and norms are fp32.  Rows may lie any distance >= d apart (ld, in
- * elements), and d and every address may be any that the type itself allows.  Nothing is atomic: the same inputs give the same bits.
+ * elements), and d and every address may be any that the type itself allows.  The same inputs give the same bits.
  * No rows and no tokens are a call like any other: sums over none are zero, ranges are empty.
  * ------------------------------------------------------------------------------------------ */
 #define NMT_F16 0
@@ -410,7 +410,7 @@ int nmt_op_gated_norm_fwd(const nmt_gated_norm* a /*host*/, void* stream);
  * d_dn: gradient at n (NULL: none); one of the two is there, and d_pre_gain with d_dn.  Written: d_dx (resid_scale times the gradient at h) and, with d_y, d_dy, of the
  * rows' type, and the gradients of gains, shifts and gate (sums over the rows in fp32, rounded once to the rows' type; each may be NULL).  d_dx may be d_dh and
  * d_dy may be d_dn with the same distance between rows.
- * d_scratch: 16-byte aligned, of nmt_op_gated_norm_bwd_scratch(rows, d, rows_per_gate) floats. */
+ * d_scratch: 16-byte aligned, of nmt_op_gated_norm_bwd_scratch(rows, d, rows_per_gate) floats, which serve fewer rows too. */
 typedef struct nmt_gated_norm_grad {
   int64_t ld_dh, ld_dn, ld_dx, ld_dy;
   const void *d_dh, *d_dn;
@@ -429,12 +429,12 @@ int nmt_op_gated_norm_bwd(const nmt_gated_norm* a /*host*/, const nmt_gated_norm
  *   capacity  > 0: expert e has the rows [e * capacity, (e + 1) * capacity) of d_rows, so that products of a size the host knows can be
  *                  enqueued; choices beyond them are dropped, and rows without a token are set to zero.
  * d_slot [tokens, k]: the row of every choice, -1 if it was dropped.  d_ranges [experts, 2]: first row and number of rows of every expert.
- * d_x NULL: the lists alone (d_rows is then NULL too).  d_scratch: nmt_op_expert_dispatch_scratch int32 elements.
- * k <= 64, experts <= 1024, tokens * k and experts * capacity <= 2^30. */
+ * d_x NULL: the lists alone (d_rows is then NULL too).  d_scratch: scratch_ints >= nmt_op_expert_dispatch_scratch int32 elements.
+ * k <= 64, experts <= 1024, tokens * k and experts * capacity <= 2^29, d <= 2^20. */
 int64_t nmt_op_expert_dispatch_scratch(int32_t tokens, int32_t k, int32_t experts);
 int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, int32_t k, int32_t experts, int32_t capacity, const void* d_x,
                            int64_t ld_x, int32_t d, int32_t type, void* d_rows, int64_t ld_rows, int32_t* d_slot, int32_t* d_ranges,
-                           int32_t* d_scratch, void* stream);
+                           int32_t* d_scratch, int64_t scratch_ints, void* stream);
 
 /* And back: out[t] = add[t] + sum over j of weights[t, j] * rows[slot[t, j]], in fp32 in the order of j, rounded once.  A choice whose slot lies
  * outside [0, n_rows) adds nothing, whatever its weight.  d_weights fp32 [tokens, k], NULL: 1 (with the slots of nmt_op_expert_dispatch this is its
@@ -445,7 +445,8 @@ int nmt_op_expert_combine(const void* d_rows, int64_t ld_rows, int32_t n_rows, c
 /* Gradients of the above: d_drows[slot[t, j]] = weights[t, j] * dout[t] and d_dweights[t, j] = the inner product of dout[t] and rows[slot[t, j]]
  * (0 for a dropped choice).  capacity and d_ranges as in nmt_op_expert_dispatch: rows without a token become zero where capacity > 0 and stay
  * as they were otherwise (d_ranges may then be NULL).  d_weights NULL: 1.  d_rows and d_dweights may both be NULL.  d_drows may be d_rows with
- * the same distance between rows; n_rows rows each.  The gradient of `add` is dout. */
+ * the same distance between rows; n_rows rows each.  No two choices
+ * share a slot (those of nmt_op_expert_dispatch do not).  The gradient of `add` is dout. */
 int nmt_op_expert_combine_bwd(const void* d_dout, int64_t ld_dout, const void* d_rows, int64_t ld_rows, int32_t n_rows,
                               const int32_t* d_slot, const float* d_weights, void* d_drows, int64_t ld_drows, float* d_dweights,
                               const int32_t* d_ranges, int32_t experts, int32_t capacity, int32_t tokens, int32_t k, int32_t d,

@@ -113,7 +113,7 @@ _SIGNATURES = {
     "nmt_op_gated_norm_bwd_scratch": (_I64, [_I32, _I32, _I32]),
     "nmt_op_gated_norm_bwd": (C.c_int, [C.POINTER(nmt_gated_norm), C.POINTER(nmt_gated_norm_grad), _P]),
     "nmt_op_expert_dispatch_scratch": (_I64, [_I32, _I32, _I32]),
-    "nmt_op_expert_dispatch": (C.c_int, [_P, _I32, _I32, _I32, _I32, _P, _I64, _I32, _I32, _P, _I64, _P, _P, _P, _P]),
+    "nmt_op_expert_dispatch": (C.c_int, [_P, _I32, _I32, _I32, _I32, _P, _I64, _I32, _I32, _P, _I64, _P, _P, _P, _I64, _P]),
     "nmt_op_expert_combine": (C.c_int, [_P, _I64, _I32, _P, _P, _P, _I64, _P, _I64, _I32, _I32, _I32, _I32, _P]),
     "nmt_op_expert_combine_bwd": (C.c_int, [_P, _I64, _P, _I64, _I32, _P, _P, _P, _I64, _P, _P, _I32, _I32, _I32, _I32, _I32, _I32, _P]),
     "nmt_adamw_table_bytes": (_I64, [_I32, C.POINTER(nmt_adamw_tensor)]),
@@ -434,12 +434,15 @@ NMT_F16, NMT_BF16, NMT_F32 = 0, 1, 2
 NMT_NORM_LAYER, NMT_NORM_RMS = 0, 1
 _KINDS = {"layer": NMT_NORM_LAYER, "rms": NMT_NORM_RMS}
 _TYPES = {}          # torch dtypes -> type codes; filled with _FLOAT and _INT when torch is there (load())
-_FLOAT = _INT = None
+_FLOAT = _INT = _torch = _raw_stream = None
 
 
 def _torch_types():
-    global _FLOAT, _INT
+    global _FLOAT, _INT, _torch, _raw_stream
     import torch
+    _torch = torch
+    # (what torch.cuda.current_stream looks up, without the Stream object around it: 0.1 us instead of 1)
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
     _TYPES.update({torch.float16: NMT_F16, torch.bfloat16: NMT_BF16, torch.float32: NMT_F32})
     _FLOAT, _INT = torch.float32, torch.int32
 
@@ -484,16 +487,15 @@ def _vector(t, n, dtype, device, what):
 
 def _call(fn, device, stream, *args, out=None):
     """fn(*args, stream[, address of out]) with `device` as the current one; its current stream if none is given."""
-    import torch
     if device < 0:
         _refuse(f"{fn.__name__}: the tensors are not on a GPU")
     if stream is None:
-        stream = torch.cuda.current_stream(device).cuda_stream
+        stream = _raw_stream(device)
     last = (stream,) if out is None else (stream, C.byref(out))
-    if device == torch.cuda.current_device():
+    if device == _torch.cuda.current_device():
         rc = fn(*args, *last)
     else:
-        with torch.cuda.device(device):
+        with _torch.cuda.device(device):
             rc = fn(*args, *last)
     if rc != NMT_OK:
         _check(rc)
@@ -625,13 +627,10 @@ def nmt_op_expert_dispatch(expert, experts, capacity, x, rows, slot, ranges, scr
     elif x is not rows:
         _refuse(f"{who}: tokens and the experts' rows belong together")
     held = 0 if scratch is None else scratch.numel()
-    need = lib.nmt_op_expert_dispatch_scratch(tokens, k, experts)
-    if need > held:
-        _refuse(f"{who}: scratch of {held} elements, {need} needed", NMT_ENOMEM)
     if held:
         scratch_ = _vector(scratch, held, _INT, device, "scratch")
     _call(lib.nmt_op_expert_dispatch, device, stream, expert.data_ptr(), tokens, k, experts, capacity, x_, ld_x, d, code, rows_, ld_rows,
-          _vector(slot, tokens * k, _INT, device, "slot"), _vector(ranges, 2 * experts, _INT, device, "ranges"), scratch_)
+          _vector(slot, tokens * k, _INT, device, "slot"), _vector(ranges, 2 * experts, _INT, device, "ranges"), scratch_, held)
 
 
 def nmt_op_expert_combine(rows, slot, weights, out, add=None, stream=None):

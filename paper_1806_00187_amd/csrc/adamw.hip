@@ -232,7 +232,7 @@ int count_pieces(const char* who, int32_t n, const nmt_adamw_tensor* tensors, in
     NMT_REQUIRE(tensors[i].n >= 0 && tensors[i].n <= (1ll << 40), "%s: tensor %d has %lld elements", who, i, (long long)tensors[i].n);
     *pieces += pieces_of(tensors[i].n);
   }
-  NMT_REQUIRE(*pieces <= 0x7FFFFFFF, "%s: more than 2^31 pieces", who);
+  NMT_REQUIRE(*pieces < (1 << 24), "%s: more than 2^24 pieces of %d elements", who, kPiece);  // (a grid has less than 2^32 threads)
   return NMT_OK;
 }
 bool type_ok(int t) { return t == NMT_F16 || t == NMT_BF16 || t == NMT_F32; }

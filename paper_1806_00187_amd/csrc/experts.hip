@@ -17,7 +17,7 @@ constexpr int kWhole = 16384;       // up to so many choices every work-group of
 constexpr int kWholeThreads = 1024;
 constexpr int64_t kStreamFrom = 96 << 20;  // bytes of the experts' rows (large_rows)
 constexpr int kMaxExperts = 1024, kMaxChoices = 64;
-constexpr int64_t kMaxItems = 1 << 30;
+constexpr int64_t kMaxItems = 1 << 29;
 
 typedef int32_t int4_any __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -223,6 +223,9 @@ __global__ void __launch_bounds__(THREADS) expert_dispatch_kernel(const SortArgs
   }
 }
 
+// Work-groups in two dimensions: one has less than 2^32 threads.
+__device__ __forceinline__ int64_t group_of() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // Rows of fixed room that no token took become zero.
 template <typename T>
 __device__ __forceinline__ void clear_rows(const RowsArgs& a, void* rows, int64_t ld, int64_t group) {
@@ -240,11 +243,11 @@ template <typename T, bool STREAM>
 __global__ void __launch_bounds__(kThreads) expert_scatter_kernel(const RowsArgs a) {
   constexpr int N = Row<T>::kVec;
   touch(a);
-  if (blockIdx.x >= a.token_groups) {
-    clear_rows<T>(a, a.out, a.ld_out, blockIdx.x - a.token_groups);
+  if (group_of() >= a.token_groups) {
+    clear_rows<T>(a, a.out, a.ld_out, group_of() - a.token_groups);
     return;
   }
-  const int64_t t = (int64_t)blockIdx.x * (kThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
+  const int64_t t = group_of() * (kThreads >> a.lanes_log) + (threadIdx.x >> a.lanes_log);
   if (t >= a.tokens) return;
   const T* x = static_cast<const T*>(a.x) + t * a.ld_x;
   T* rows = static_cast<T*>(a.out);
@@ -292,7 +295,7 @@ struct Choices {
 template <int LANES>
 __device__ __forceinline__ int64_t token_of() {
   const uint32_t mine = threadIdx.x / LANES;
-  return (int64_t)blockIdx.x * (kThreads / LANES) + (LANES == 64 ? __builtin_amdgcn_readfirstlane(mine) : mine);
+  return group_of() * (kThreads / LANES) + (LANES == 64 ? __builtin_amdgcn_readfirstlane(mine) : mine);
 }
 
 // out[t] = add[t] + sum over j of weights[t, j] rows[slot[t, j]], in the order of j.  LANES lanes per token; AHEAD rows, two vectors a lane of each, are asked for together.
@@ -359,8 +362,8 @@ template <typename T, int LANES, int AHEAD, bool STREAM>
 __global__ void __launch_bounds__(kThreads) expert_combine_bwd_kernel(const RowsArgs a) {
   constexpr int N = Row<T>::kVec;
   touch(a);
-  if (blockIdx.x >= a.token_groups) {
-    clear_rows<T>(a, a.out, a.ld_out, blockIdx.x - a.token_groups);
+  if (group_of() >= a.token_groups) {
+    clear_rows<T>(a, a.out, a.ld_out, group_of() - a.token_groups);
     return;
   }
   const int lane = threadIdx.x % LANES;
@@ -429,6 +432,13 @@ bool large_rows(int64_t rows, int d, size_t size) { return rows * d * (int64_t)s
 
 int segments_of(int64_t n) { return (int)((n + kSegment - 1) / kSegment); }
 
+dim3 grid_of(int64_t groups) {
+  const int64_t x = std::min<int64_t>(groups, 1 << 20);
+  return dim3((uint32_t)x, x ? (uint32_t)((groups + x - 1) / x) : 1);
+}
+
+int64_t scratch_of(int tokens, int k, int experts) { return tokens ? (int64_t)(segments_of((int64_t)tokens * k) + 1) * experts : 0; }
+
 int check_lists(const char* who, int tokens, int k, int experts, int capacity) {
   NMT_REQUIRE(tokens >= 0 && k >= 1 && k <= kMaxChoices && (int64_t)tokens * k <= kMaxItems, "%s: %d tokens of %d choices", who, tokens, k);
   NMT_REQUIRE(experts >= 1 && experts <= kMaxExperts, "%s: %d experts outside [1, %d]", who, experts, kMaxExperts);
@@ -446,12 +456,12 @@ int check_rows(const char* who, int d, int type) {
 
 extern "C" int64_t nmt_op_expert_dispatch_scratch(int32_t tokens, int32_t k, int32_t experts) {
   if (check_lists("nmt_op_expert_dispatch_scratch", tokens, k, experts, 0) != NMT_OK) return NMT_EINVAL;
-  return tokens ? (int64_t)(segments_of((int64_t)tokens * k) + 1) * experts : 0;
+  return scratch_of(tokens, k, experts);
 }
 
 extern "C" int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, int32_t k, int32_t experts, int32_t capacity, const void* d_x,
                                       int64_t ld_x, int32_t d, int32_t type, void* d_rows, int64_t ld_rows, int32_t* d_slot,
-                                      int32_t* d_ranges, int32_t* d_scratch, void* stream_) {
+                                      int32_t* d_ranges, int32_t* d_scratch, int64_t scratch_ints, void* stream_) {
   const char* who = "nmt_op_expert_dispatch";
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   if (const int rc = check_lists(who, tokens, k, experts, capacity); rc != NMT_OK) return rc;
@@ -462,7 +472,11 @@ extern "C" int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, i
     EXPERT_ROWS(d_x, tokens, ld_x, "x");
     EXPERT_ROWS(d_rows, capacity ? (int64_t)experts * capacity : n, ld_rows, "the experts");
   }
-  NMT_REQUIRE(d_ranges && (tokens == 0 || (d_expert && d_slot && d_scratch)), "%s: null pointer", who);
+  NMT_REQUIRE(d_ranges && (tokens == 0 || (d_expert && d_slot)), "%s: null pointer", who);
+  if (const int64_t need = scratch_of(tokens, k, experts); need > (d_scratch ? scratch_ints : 0)) {
+    nmt_set_error("%s: scratch of %lld elements, %lld needed", who, (long long)(d_scratch ? scratch_ints : 0), (long long)need);
+    return NMT_ENOMEM;
+  }
   SortArgs s = {};
   s.expert = d_expert, s.n = (int)n, s.experts = experts, s.capacity = capacity, s.segments = segments_of(n);
   s.hist = d_scratch, s.totals = d_scratch + (int64_t)s.segments * experts, s.slot = d_slot, s.ranges = d_ranges;
@@ -495,7 +509,7 @@ extern "C" int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, i
   if (!d_rows) return NMT_OK;
   const int per = kThreads >> a.lanes_log;
   a.token_groups = ceil_div(tokens, per);
-  const dim3 rows_grid((uint32_t)(a.token_groups + ceil_div((int64_t)experts * capacity, per)));
+  const dim3 rows_grid = grid_of(a.token_groups + ceil_div((int64_t)experts * capacity, per));
   const bool large = large_rows(n, d, row_type_bytes(type));
   if (type == NMT_F32) hipLaunchKernelGGL((large ? expert_scatter_kernel<uint32_t, true> : expert_scatter_kernel<uint32_t, false>), rows_grid, dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL((large ? expert_scatter_kernel<uint16_t, true> : expert_scatter_kernel<uint16_t, false>), rows_grid, dim3(kThreads), 0, stream, a);
@@ -505,7 +519,7 @@ extern "C" int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, i
 
 template <typename T, int LANES, bool STREAM>
 static void launch_combine(const RowsArgs& a, hipStream_t stream) {
-  const dim3 grid(ceil_div(a.tokens, kThreads / LANES));
+  const dim3 grid = grid_of(ceil_div(a.tokens, kThreads / LANES));
   if (a.k == 1) hipLaunchKernelGGL((expert_combine_kernel<T, LANES, 1, STREAM>), grid, dim3(kThreads), 0, stream, a);
   else if (a.k == 2) hipLaunchKernelGGL((expert_combine_kernel<T, LANES, 2, STREAM>), grid, dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL((expert_combine_kernel<T, LANES, 4, STREAM>), grid, dim3(kThreads), 0, stream, a);
@@ -520,7 +534,7 @@ static void launch_combine(const RowsArgs& a, hipStream_t stream) {
 template <typename T, int LANES, bool STREAM>
 static void launch_combine_bwd(RowsArgs a, hipStream_t stream) {
   a.token_groups = ceil_div(a.tokens, kThreads / LANES);
-  const dim3 grid((uint32_t)(a.token_groups + ceil_div((int64_t)a.experts * a.capacity, kThreads >> a.lanes_log)));
+  const dim3 grid = grid_of(a.token_groups + ceil_div((int64_t)a.experts * a.capacity, kThreads >> a.lanes_log));
   if (grid.x == 0) return;
   if (a.k == 1) hipLaunchKernelGGL((expert_combine_bwd_kernel<T, LANES, 1, STREAM>), grid, dim3(kThreads), 0, stream, a);
   else if (a.k == 2) hipLaunchKernelGGL((expert_combine_bwd_kernel<T, LANES, 2, STREAM>), grid, dim3(kThreads), 0, stream, a);

@@ -254,6 +254,10 @@ __global__ void __launch_bounds__(S::kThreads) gated_norm_fwd_kernel(const NormA
         for (int e = 0; e < E; ++e) h[e] += pre_shift(e);
       out_n.set(h);
     }
+    if (WAVES > 1 && !a.post_gain && !a.n) {  // (h may lie where x does, and lanes of two wavefronts may have loaded the same of it: no sum over the row has held the first up)
+      out_h.arrive();
+      __syncthreads();
+    }
     next_x.arrive();
     if (a.y) next_y.arrive();
     if (GROUPED) next_gate.arrive();
@@ -381,9 +385,13 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
     if (a.dh) next_dh.arrive();
     if (a.y) next_y.arrive();
     asm volatile("" : "+v"(next_st));
+    if (WAVES > 1) {  // the sums' places are used again; and dx may lie where dh does, dy where dn, of which lanes of two wavefronts may have loaded the same
+      out_x.arrive();
+      if (a.y) out_y.arrive();
+      __syncthreads();
+    }
     out_x.store(a.dx, row * a.ld_dx, c);
     if (a.y) out_y.store(a.dy, row * a.ld_dy, c);
-    if (WAVES > 1) __syncthreads();  // (the sums' places are used again)
   }
   close_gate(end);
   // the work-group's column sums: its workers' in increasing order
@@ -499,7 +507,7 @@ Split split_rows(int rows, int d, int type, bool wide, bool forward, int rows_pe
   const int shape = shape_of(d, type), at_once = workers_of(shape, wide), waves = std::max(at_once > 1 ? 4 : 1, waves_of_row(shape, wide));
   Split p;
   if (forward) {
-    p.chunk = (int64_t)rows * waves >= (int64_t)2 * kFwdWaves * at_once ? 2 : 1;
+    p.chunk = (int64_t)rows * waves >= (int64_t)2 * kFwdWaves * at_once ? std::max(2, ceil_div(rows, (int64_t)at_once << 22)) : 1;  // (a grid has less than 2^32 threads)
   } else {
     p.chunk = ceil_div(rows, kBwdWaves / waves * at_once);
     if (rows_per_gate < rows && rows_per_gate <= 2 * (int64_t)p.chunk) p.chunk = ceil_div(p.chunk, rows_per_gate) * rows_per_gate;  // no gate's rows are two workers' then
@@ -509,11 +517,13 @@ Split split_rows(int rows, int d, int type, bool wide, bool forward, int rows_pe
   p.pitch = (d + 7) / 8 * 8;
   return p;
 }
+// Of a pass of up to `rows` rows, of any type.
 int64_t scratch_floats(int rows, int d, int rows_per_gate) {
   int64_t most = 0;
   for (int type : {NMT_F16, NMT_F32}) {
-    const Split p = split_rows(rows, d, type, wide_bwd(type), false, rows_per_gate);
-    most = std::max(most, (int64_t)p.groups * 4 * p.pitch + (rows_per_gate < rows ? (int64_t)p.workers * 2 * p.pitch : 0));
+    const int shape = shape_of(d, type), at_once = workers_of(shape, wide_bwd(type)), waves = std::max(at_once > 1 ? 4 : 1, waves_of_row(shape, wide_bwd(type)));
+    const int64_t groups = std::min(ceil_div(rows, at_once), kBwdWaves / waves), pitch = (d + 7) / 8 * 8;
+    most = std::max(most, groups * 4 * pitch + (rows_per_gate < rows ? groups * at_once * 2 * pitch : 0));
   }
   return most;
 }

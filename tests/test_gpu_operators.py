@@ -144,6 +144,13 @@ def test_gated_norm_forward_of_rows_anywhere(d, ld, shift, dtype):
     check_forward(23, d, dtype, "rms", 4, 1.0, "ypgns", 1, ld, shift, in_place=True)
 
 
+@pytest.mark.parametrize("d", [530, 700, 1030, 1600, 2500, 5000, 9000])
+@pytest.mark.parametrize("parts", ["y", "yg", "yp", "yn"])
+def test_gated_norm_forward_in_place_of_its_inputs(d, parts):
+    """Rows held by several wavefronts, some of whose lanes take the same columns."""
+    check_forward(300, d, F16, "rms", 9, 0.9, parts, d, in_place=True)
+
+
 def check_backward(rows, d, dtype, kind, per, resid, parts, seed, ld=None, shift=0, in_place=False):
     s = norm_inputs(rows, d, dtype, kind, per, seed, "s" in parts)
     post, gate, pre = s["post"] if "p" in parts else None, s["gate"] if "g" in parts else None, s["pre"] if "n" in parts else None
@@ -233,6 +240,21 @@ def test_gated_norm_backward_of_any_rows_and_gates(rows, per):
 def test_gated_norm_backward_of_rows_anywhere(d, ld, shift, dtype):
     check_backward(23, d, dtype, "layer", None, 1.0, "yhpgns", 1, ld, shift)
     check_backward(23, d, dtype, "rms", 4, 1.0, "yhpgns", 1, ld, shift, in_place=True)
+
+
+@pytest.mark.parametrize("d", [530, 700, 1030, 1600, 2500, 5000, 9000])
+@pytest.mark.parametrize("parts", ["yh", "yhg", "yhp", "yhn", "hn"])
+def test_gated_norm_backward_in_place_of_its_inputs(d, parts):
+    check_backward(300, d, F16, "rms", 9, 0.9, parts, d, in_place=True)
+    check_backward(300, d, F32, "layer", 9, 0.9, parts, d, in_place=True)
+
+
+def test_gated_norm_scratch_serves_fewer_rows():
+    for d in (64, 512, 777, 1024, 2048, 8192):
+        for per in (None, 7):
+            sizes = [A.nmt_op_gated_norm_bwd_scratch(n, d, per) for n in (1, 10, 63, 500, 1023, 1024, 1025, 4096, 4097, 50000, 10 ** 6)]
+            assert sizes == sorted(sizes)
+    check_backward(1023, 64, F16, "rms", 7, 1.0, "yhpgns", 1)
 
 
 @pytest.mark.parametrize("kind", ["layer", "rms"])
@@ -763,3 +785,134 @@ def test_calls_on_two_streams_at_once():
         b.run(stream=t.cuda_stream)
     torch.cuda.synchronize()
     assert same(want[0], a.outputs()) and same(want[1], b.outputs())
+
+
+# ---- together ----------------------------------------------------------------------------------------
+def test_a_sparse_gated_block_trains():
+    """Norm, experts, their products, weighted sum, norm with gate and residual, the next norm; the way back; AdamW over everything.  Against autograd in 64 bits: some ten
+    tensors lie in fp16 between a loss and a gradient, each off by at most 2^-11 of its values: 10 * 2^-11 of a gradient's norm, and as much again for the products' fp32."""
+    T, d, F, E, k, cap = 240, 64, 128, 4, 2, 200
+    g = gen(77)
+    r = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    x, ch, cn = r(T, d).half(), r(T, d).half(), r(T, d).half()
+    # (biases of +-6 over products of size 1: no ReLU hangs on a rounding)
+    side = torch.where(torch.arange(F, device=DEV) % 2 == 0, 6.0, -6.0)
+    P = {f"w1.{e}": r(F, d) / d ** .5 for e in range(E)} | {f"b1.{e}": side + .1 * r(F) for e in range(E)} | {f"w2.{e}": r(d, F) / F ** .5 for e in range(E)} \
+        | {"first_g": 1 + .1 * r(d), "first_s": .1 * r(d), "post_g": 1 + .1 * r(d), "post_s": .1 * r(d), "gate": .5 + .1 * r(1, d), "pre_g": 1 + .1 * r(d), "pre_s": .1 * r(d)}
+    P = {n: v.half() for n, v in P.items()}
+    ids, w = choices(T, k, E, 5, dropped=0.1, skew=0.3), torch.rand(T, k, generator=g, device=DEV)
+    new = lambda *s, t=F16: torch.empty(*s, dtype=t, device=DEV)
+    I32 = torch.int32
+    # forwards
+    n0, st0 = new(T, d), new(T, 4, t=F32)
+    A.nmt_op_gated_norm_fwd(x, None, None, n0, st0, pre=(P["first_g"], P["first_s"]))
+    rows, slot, ranges, scratch = new(E * cap, d), new(T, k, t=I32), new(E, 2, t=I32), new(A.nmt_op_expert_dispatch_scratch(T, k, E), t=I32)
+    A.nmt_op_expert_dispatch(ids, E, cap, n0, rows, slot, ranges, scratch)
+    assert int(ranges[:, 1].max()) < cap and int((slot < 0).sum()) > 0          # room is left, and some choices are dropped
+    hid, made = new(E * cap, F), new(E * cap, d)
+    of = lambda t, e: t[e * cap:(e + 1) * cap]
+    for e in range(E):
+        A.nmt_op_gemm(of(rows, e), 0, d, P[f"w1.{e}"], 0, d, of(hid, e), F, cap, F, d, bias=P[f"b1.{e}"], relu=True)
+        A.nmt_op_gemm(of(hid, e), 0, F, P[f"w2.{e}"], 0, F, of(made, e), d, cap, d, F)
+    out, h, n1, st1 = new(T, d), new(T, d), new(T, d), new(T, 4, t=F32)
+    A.nmt_op_expert_combine(made, slot, w, out)
+    parts = dict(post=(P["post_g"], P["post_s"]), gate=P["gate"], pre=(P["pre_g"], P["pre_s"]), resid_scale=0.9)
+    A.nmt_op_gated_norm_fwd(x, out, h, n1, st1, **parts)
+    # back
+    G = {n: torch.empty_like(v) for n, v in P.items()}
+    dx, dout, partial = new(T, d), new(T, d), new(A.nmt_op_gated_norm_bwd_scratch(T, d), t=F32)
+    A.nmt_op_gated_norm_bwd(ch, cn, out, h, st1, dx, dout, partial, dpost=(G["post_g"], G["post_s"]), dgate=G["gate"], dpre=(G["pre_g"], G["pre_s"]), **parts)
+    dmade, dw = new(E * cap, d), new(T, k, t=F32)
+    A.nmt_op_expert_combine_bwd(dout, made, slot, w, dmade, dw, ranges, cap)
+    dhid, drows = new(E * cap, F), new(E * cap, d)
+    for e in range(E):
+        A.nmt_op_gemm(of(dmade, e), 0, d, P[f"w2.{e}"], 1, F, of(dhid, e), F, cap, F, d, relu_src=of(hid, e))
+        A.nmt_op_gemm(of(dhid, e), 0, F, P[f"w1.{e}"], 1, d, of(drows, e), d, cap, d, F)
+        A.nmt_op_wgrad_group([(of(dhid, e), F, of(rows, e), d, G[f"w1.{e}"], d, G[f"b1.{e}"], F, d, cap), (of(dmade, e), d, of(hid, e), F, G[f"w2.{e}"], F, None, d, F, cap)])
+    dn0 = new(T, d)
+    A.nmt_op_expert_combine(drows, slot, None, dn0)
+    A.nmt_op_gated_norm_bwd(dx, dn0, None, x, st0, dx, None, partial, pre=(P["first_g"], P["first_s"]), dpre=(G["first_g"], G["first_s"]))
+    torch.cuda.synchronize()
+    # the same in 64 bits
+    leaf = {n: v.to(D).requires_grad_() for n, v in P.items()}
+    X, W = x.to(D).requires_grad_(), w.to(D).requires_grad_()
+    N0 = R.gated_norm(X, pre=(leaf["first_g"], leaf["first_s"]))[1]
+    Y = torch.zeros(T, d, dtype=D, device=DEV)
+    for j in range(k):
+        for e in range(E):
+            t = ((ids[:, j] == e) & (slot[:, j] >= 0)).nonzero().reshape(-1)
+            Y = Y.index_add(0, t, W[t, j, None] * (torch.relu(N0[t] @ leaf[f"w1.{e}"].t() + leaf[f"b1.{e}"]) @ leaf[f"w2.{e}"].t()))
+    H, N1 = R.gated_norm(X, Y, (leaf["post_g"], leaf["post_s"]), leaf["gate"], (leaf["pre_g"], leaf["pre_s"]), resid_scale=0.9)
+    ((H * ch.to(D)).sum() + (N1 * cn.to(D)).sum()).backward()
+    bound = 20 * 2.0 ** -11
+    near = lambda got, want, what: None if float((got.to(D) - want.detach()).norm()) <= bound * float(want.detach().norm()) else pytest.fail(
+        f"{what}: {float((got.to(D) - want).norm() / want.norm()):.5f}")
+    near(h, H, "h"), near(n1, N1, "n"), near(dx, X.grad, "x"), near(dw, W.grad, "weights")
+    for n in P:
+        near(G[n], leaf[n].grad, n)
+    # and the step, from these gradients
+    for bits in (32, 8):
+        tensors = []
+        for n, v in P.items():
+            size = v.numel()
+            t = dict(master=v.float().reshape(-1), grad=G[n].reshape(-1), weights=v.clone().reshape(-1), weight_decay=0.01 if v.dim() == 2 and v.shape[0] > 1 else 0.0, lr_factor=1.0)
+            for s in ("m", "v"):
+                t[s] = torch.zeros(size, device=DEV) if bits == 32 else torch.zeros(size, dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)
+                if bits == 8:
+                    t[s + "_scale"] = torch.zeros(-(-size // 256), device=DEV)
+            tensors.append(t)
+        plan = A.nmt_adamw_create(tensors, torch.empty(A.nmt_adamw_table_bytes(tensors), dtype=torch.uint8, device=DEV))
+        for t in (1, 2):
+            check_step(tensors, bits, t, plan)
+        A.nmt_adamw_destroy(plan)
+
+
+# ---- sessions ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("weight_decay,state_bits", [(0.01, 32), (0.0, 8), (0.05, 8)])
+def test_sessions_update_with_adamw(weight_decay, state_bits):
+    """Weights after three updates of two sub-batches each, from the accumulated gradients the session itself holds; an update that overflows changes nothing."""
+    import nmt_inputs as I
+    from paper_1806_00187_amd.session import Session
+    model = I.MODELS["tiny"]
+    sess = Session(model, I.init_weights(seed=0, **model), max_sentences=8, weight_decay=weight_decay, state_bits=state_bits)
+    batches = [sess.to_device(I.tiny_batch(seed=s)) for s in (1001, 1002)]
+    of = lambda flat, off, n: flat[off:off + n]
+
+    def pieces():
+        out, at = [], 0
+        for name, (off, rows, cols) in sess.layout.items():
+            n = rows * cols
+            t = dict(master=of(sess.master, off, n), m=of(sess.m, off, n), v=of(sess.v, off, n), grad=of(sess.acc, off, n), weights=of(sess.w16, off, n),
+                     weight_decay=weight_decay if rows > 1 else 0.0, lr_factor=1.0)
+            if state_bits == 8:
+                blocks = -(-n // 256)
+                t.update(m_scale=of(sess.m_scale, at, blocks), v_scale=of(sess.v_scale, at, blocks))
+                at += blocks
+            out.append(t)
+        return out
+    for t in (1, 2, 3):
+        before = [dict(master=x["master"].to(D), state=states(x, state_bits)) for x in pieces()]
+        _, ntok, flag = sess.update(batches, 128.0, 1e-3, t)
+        assert flag == 0
+        for x, b in zip(pieces(), before):
+            m, v = b["state"]
+            w, _, _ = R.adamw(b["master"], m, v, x["grad"].to(D) / (128.0 * ntok), 1e-3, 0.9, 0.98, 1e-8, t, x["weight_decay"])
+            step = (w - b["master"]).abs()
+            # (as in check_step, 24 U32 of the step's terms, and of the factor 1 / (128 tokens) in fp32 one more; |m| / root v is at most 1 / sqrt(1 - beta2) beyond the step)
+            within(x["master"], w, 2 * U32 * w.abs() + 64 * U32 * 1e-3 * (8 + step / 1e-3), "master")
+            assert torch.equal(x["weights"], x["master"].half())
+    keep = [t.view(torch.uint8).clone() for t in (sess.master, sess.m, sess.v, sess.w16)]
+    _, _, flag = sess.update(batches, 128.0 * 2 ** 20, 1e-3, 4)
+    assert flag == 1 and all(torch.equal(a, t.view(torch.uint8)) for a, t in zip(keep, (sess.master, sess.m, sess.v, sess.w16)))
+    sess.close()
+
+
+def test_sessions_without_decay_in_32_bits_keep_adam():
+    import nmt_inputs as I
+    from paper_1806_00187_amd.session import Session
+    model = I.MODELS["tiny"]
+    sess = Session(model, I.init_weights(seed=0, **model), max_sentences=8)
+    assert sess.plan is None and sess.m.dtype == torch.float32
+    sess.close()
+    with pytest.raises(ValueError):
+        Session(model, I.init_weights(seed=0, **model), state_bits=16)

@@ -69,15 +69,22 @@ def test_null_structs_are_refused():
     refused(lib.nmt_adamw_create(0, None, 32, 0, 0, None, 0, None, None))
 
 
-DISPATCH = dict(expert=P, tokens=4, k=2, experts=8, capacity=0, x=P, ld_x=16, d=16, type=0, rows=P, ld_rows=16, slot=P, ranges=P, scratch=P)
+DISPATCH = dict(expert=P, tokens=4, k=2, experts=8, capacity=0, x=P, ld_x=16, d=16, type=0, rows=P, ld_rows=16, slot=P, ranges=P, scratch=P, scratch_ints=1 << 20)
 
 
 @pytest.mark.parametrize("bad", [dict(tokens=-1), dict(k=0), dict(k=65), dict(experts=0), dict(experts=1025), dict(capacity=-1), dict(capacity=2 ** 28),
                                  dict(tokens=2 ** 30), dict(d=0), dict(type=3), dict(ld_x=15), dict(ld_rows=15), dict(x=None), dict(rows=None),
-                                 dict(expert=None), dict(slot=None), dict(ranges=None), dict(scratch=None)])
+                                 dict(expert=None), dict(slot=None), dict(ranges=None)])
 def test_dispatch_refuses(bad):
     a = dict(DISPATCH, **bad)
     refused(A.load().nmt_op_expert_dispatch(*a.values(), None), says="nmt_op_expert_dispatch")
+
+
+def test_dispatch_wants_the_scratch_it_asks_for():
+    need = A.nmt_op_expert_dispatch_scratch(4, 2, 8)
+    for bad in (dict(scratch=None), dict(scratch_ints=need - 1)):
+        a = dict(DISPATCH, **bad)
+        refused(A.load().nmt_op_expert_dispatch(*a.values(), None), A.NMT_ENOMEM, str(need))
 
 
 COMBINE = dict(rows=P, ld_rows=16, n_rows=8, slot=P, weights=P, add=P, ld_add=16, out=P, ld_out=16, tokens=4, k=2, d=16, type=0)
@@ -172,7 +179,7 @@ def test_gated_norm_binding_refuses(change):
 @pytest.mark.parametrize("change,code", [(dict(expert=torch.zeros(4, 2, dtype=torch.int64)), -1), (dict(expert=torch.zeros(8, dtype=torch.int32)), -1),
                                          (dict(rows=rows(7, 16)), -1), (dict(capacity=2), -1), (dict(x=rows(5, 16)), -1), (dict(x=None), -1),
                                          (dict(slot=torch.zeros(4, 1, dtype=torch.int32)), -1), (dict(ranges=torch.zeros(8, dtype=torch.int32)), -1),
-                                         (dict(scratch=torch.zeros(0, dtype=torch.int32)), -3), (dict(experts=2000), -1), ({}, -1)])
+                                         (dict(scratch=torch.zeros(8)), -1), (dict(experts=2000), -1), ({}, -1)])
 def test_dispatch_binding_refuses(change, code):
     i = lambda *s: torch.zeros(*s, dtype=torch.int32)
     a = dict(expert=i(4, 2), experts=8, capacity=0, x=rows(4, 16), rows=rows(8, 16), slot=i(4, 2), ranges=i(8, 2), scratch=i(4096))
