@@ -24,9 +24,11 @@ class Session:
     (choose_streams; auto_streams=False keeps the streams as created)."""
 
     def __init__(self, model, weights, max_sentences=1024, max_len=256, act_dropout=0.0, label_smoothing=0.1, ln_eps=1e-5,
-                 seed=0, pad_id=1, device="cuda:0", optimizer=True, n_pipes=1, auto_streams=True):
+                 seed=0, pad_id=1, device="cuda:0", optimizer=True, n_pipes=1, auto_streams=True, weight_decay=0.0, state_bits=32):
         """model: dict(enc_layers, dec_layers, d_model, n_heads, d_ff, vocab, dropout);
-        weights: dict name -> float16 numpy array (initial fp16 weights = initial master values)."""
+        weights: dict name -> float16 numpy array (initial fp16 weights = initial master values).
+        weight_decay > 0 or state_bits = 8: the updates are AdamW's (nmt_adamw_step) instead of Adam's, with weight decay on matrices and none
+        on biases and LayerNorm vectors; 8 bits: the moments take one byte each (float8_e4m3fn m and v, with scales m_scale and v_scale per 256 elements)."""
         self.device = torch.device(device)
         self.model = dict(model)
         self.n_pipes = n_pipes
@@ -52,14 +54,18 @@ class Session:
         if optimizer:
             self.master = self.w16.float()
             self.acc = torch.zeros(self.P, dtype=torch.float32, device=self.device)
-            self.m = torch.zeros_like(self.acc)
-            self.v = torch.zeros_like(self.acc)
+            if state_bits not in (8, 32):
+                raise ValueError(f"state_bits = {state_bits}: 8 or 32")
+            state = torch.float8_e4m3fn if state_bits == 8 else torch.float32
+            self.m, self.v = (torch.zeros(self.P, dtype=torch.uint8 if state_bits == 8 else state, device=self.device).view(state) for _ in range(2))
         else:
             self.master = self.acc = self.m = self.v = None
+        self.plan = self._adamw_plan(weight_decay, state_bits) if optimizer and (weight_decay or state_bits == 8) else None
         self.workspaces = [None] * n_pipes
         self.loss_sums = [torch.zeros(1, dtype=torch.float32, device=self.device) for _ in range(n_pipes)]
         self.ntoks = [torch.zeros(1, dtype=torch.int32, device=self.device) for _ in range(n_pipes)]
         self.loss_sum, self.ntok = self.loss_sums[0], self.ntoks[0]
+        self._inv_scale = 1.0
         # what an update reports, side by side so that the host fetches it with one copy
         self._report = torch.zeros(3, dtype=torch.int32, device=self.device)
         self.flag, self.ntok_tot = self._report[0:1], self._report[1:2]
@@ -70,8 +76,25 @@ class Session:
         for p in range(n_pipes):
             self._bind(p)
 
+    def _adamw_plan(self, weight_decay, state_bits):
+        """The tensors of the layout as nmt_adamw_create takes them: views of the flat buffers."""
+        blocks = {name: -(-rows * cols // 256) for name, (_, rows, cols) in self.layout.items()}
+        if state_bits == 8:
+            self.m_scale, self.v_scale = (torch.zeros(sum(blocks.values()), dtype=torch.float32, device=self.device) for _ in range(2))
+        tensors, at = [], 0
+        for name, (off, rows, cols) in self.layout.items():
+            part = slice(off, off + rows * cols)
+            t = dict(master=self.master[part], m=self.m[part], v=self.v[part], grad=self.acc[part], weights=self.w16[part],
+                     weight_decay=weight_decay if rows > 1 else 0.0)
+            if state_bits == 8:
+                t.update(m_scale=self.m_scale[at:at + blocks[name]], v_scale=self.v_scale[at:at + blocks[name]])
+                at += blocks[name]
+            tensors.append(t)
+        return nmt.nmt_adamw_create(tensors, torch.empty(nmt.nmt_adamw_table_bytes(tensors), dtype=torch.uint8, device=self.device))
+
     def _bind(self, pipe=0):
-        nmt.nmt_bind(self.ctxs[pipe], self.w16, self.g16s[pipe], self.master, self.acc, self.m, self.v, self.workspaces[pipe])
+        m, v = (self.m, self.v) if self.plan is None else (None, None)
+        nmt.nmt_bind(self.ctxs[pipe], self.w16, self.g16s[pipe], self.master, self.acc, m, v, self.workspaces[pipe])
 
     @property
     def workspace(self):
@@ -83,6 +106,8 @@ class Session:
             for c in self.ctxs:
                 nmt.nmt_destroy(c)
             self.ctxs, self.ctx = [], None
+            if self.plan is not None:
+                nmt.nmt_adamw_destroy(self.plan)
 
     def reserve(self, B, S=None, T=None):
         """Workspace for one (B, S, T) batch, or for a group given as a list of (B, S, T, micro)."""
@@ -182,12 +207,22 @@ class Session:
 
     def check_overflow(self, inv_scale):
         nmt.nmt_check_overflow(self.ctx, inv_scale, self.flag)
+        self._inv_scale = inv_scale
 
     def adam_step(self, lr, t, betas=(0.9, 0.98), eps=1e-8):
-        nmt.nmt_adam_step(self.ctx, lr, betas[0], betas[1], eps, t, self.flag)
+        """The update with the gradient acc * inv_scale of the last check_overflow, unless that raised the flag."""
+        if self.plan is not None:
+            nmt.nmt_adamw_step(self.plan, lr, betas[0], betas[1], eps, t, grad_scale=self._inv_scale, flag=self.flag)
+        else:
+            nmt.nmt_adam_step(self.ctx, lr, betas[0], betas[1], eps, t, self.flag)
 
     def finish_update(self, first, inv_scale, lr, t, betas=(0.9, 0.98), eps=1e-8):
         """accumulate(first), check_overflow and adam_step in one call"""
+        if self.plan is not None:
+            self.accumulate(first)
+            self.check_overflow(inv_scale)
+            self.adam_step(lr, t, betas, eps)
+            return
         nmt.nmt_finish_update(self.ctx, first, inv_scale, lr, betas[0], betas[1], eps, t, self.flag)
 
     # ---- one weight update from k micro-batches ----
