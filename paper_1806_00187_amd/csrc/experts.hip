@@ -14,6 +14,7 @@ constexpr int kThreads = 256;
 constexpr int kSegment = 1024;      // choices that share a row of counts
 constexpr int kChunk = kWave;       // choices of a work-group of the dispatch
 constexpr int kWhole = 16384;       // up to so many choices every work-group of the dispatch counts all of them itself
+constexpr int kSummed = 4096;       // up to so many counts of segments every work-group adds up itself (32768 choices to 64 experts and back 33.6 -> 31.4 us, 105402: 124 -> 127)
 constexpr int kWholeThreads = 1024;
 constexpr int64_t kStreamFrom = 96 << 20;  // bytes of the experts' rows (large_rows)
 constexpr int kMaxExperts = 1024, kMaxChoices = 64;
@@ -24,6 +25,7 @@ typedef int32_t int4_any __attribute__((ext_vector_type(4), aligned(4)));
 struct SortArgs {
   const int32_t* expert;
   int n, experts, capacity, segments, bits;
+  Divisor by_experts;
   int32_t *hist, *totals, *slot, *ranges;
 };
 
@@ -99,20 +101,25 @@ struct RowsArgs {
   const int32_t *slot, *ranges;
   const float* weights;
   float* dweights;
-  int tokens, k, d, vectors, n_rows, capacity, experts, lanes_log;  // vectors: columns in whole vectors of 16 bytes; 2^lanes_log lanes take a row
+  int tokens, k, d, n_rows, capacity, experts, lanes_log;  // 2^lanes_log lanes take a row
+  // A row's columns [0, vectors) go in vectors of 16 bytes, the last of which ends with them: where `vectors` is no multiple of a vector it has elements in common with the one
+  // before, which come out the same.  The columns from `vectors` on go one by one: of rows shorter than a vector, and of sums formed in place, where nothing may be read twice.
+  int vectors;
   int64_t token_groups;                                             // work-groups of tokens; those behind clear rows without a token
   Divisor by_k, by_capacity;
 };
 
 template <typename T>
 __device__ __forceinline__ void clear_row(T* row, int lane, int lanes, const RowsArgs& a) {
-  for (int c = lane * Row<T>::kVec; c < a.vectors; c += Row<T>::kVec * lanes) st_vec(row + c, typename Row<T>::vec{});
+  for (int c = lane * Row<T>::kVec; c < a.vectors; c += Row<T>::kVec * lanes) st_vec(row + min(c, a.vectors - Row<T>::kVec), typename Row<T>::vec{});
   for (int c = a.vectors + lane; c < a.d; c += lanes) row[c] = T(0);
 }
 
-// The slots of a chunk of choices and, T being any type of the rows' size and not void, the rows that go there.  WHOLE: the choices before
-// the chunk and all others are counted here; otherwise the counts of the segments before the chunk's, and the totals, are there.
-template <typename T, bool WHOLE, int THREADS>
+// Where the counts before a chunk and the totals come from: WHOLE: every choice is counted here; SUMMED: counts of segments, added up here; SCANNED: by the scan.
+enum Counts { WHOLE, SUMMED, SCANNED };
+
+// The slots of a chunk of choices and, T being any type of the rows' size and not void, the rows that go there.
+template <typename T, Counts COUNTS, int THREADS>
 __global__ void __launch_bounds__(THREADS) expert_dispatch_kernel(const SortArgs s, const RowsArgs a) {
   touch(s);
   touch(a);
@@ -123,15 +130,38 @@ __global__ void __launch_bounds__(THREADS) expert_dispatch_kernel(const SortArgs
   const int begin = (int)min((int64_t)blockIdx.x * kChunk, (int64_t)s.n), end = min(begin + kChunk, s.n);
   const int segment = begin / kSegment;
   for (int e = threadIdx.x; e < s.experts; e += THREADS) {
-    before[e] = WHOLE ? 0 : s.hist[(int64_t)segment * s.experts + e];
-    total[e] = WHOLE ? 0 : s.totals[e];
+    before[e] = COUNTS == SCANNED ? s.hist[(int64_t)segment * s.experts + e] : 0;
+    total[e] = COUNTS == SCANNED ? s.totals[e] : 0;
   }
   const int mine = begin + lane < end ? s.expert[begin + lane] : -1;  // (wavefront 0's to place)
   __syncthreads();
-  if (WHOLE) each_choice(s, 0, s.n, [&](int i, int e) { atomicAdd(i < begin ? &before[e] : &total[e], 1); });
-  else each_choice(s, segment * kSegment, begin, [&](int, int e) { atomicAdd(&before[e], 1); });
+  if (COUNTS == WHOLE) {
+    each_choice(s, 0, s.n, [&](int i, int e) { atomicAdd(i < begin ? &before[e] : &total[e], 1); });
+  } else {
+    if (COUNTS == SUMMED) {
+      const int entries = s.segments * s.experts, mine_from = segment * s.experts;
+      constexpr int AHEAD = 8;
+      for (int i = threadIdx.x; i < entries; i += AHEAD * THREADS) {
+        int32_t v[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) v[u] = s.hist[min(i + u * THREADS, entries - 1)];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+          const int at = i + u * THREADS;
+          uint32_t e;
+          div_mod((uint32_t)at, s.by_experts, e);
+          if (at < entries && v[u]) atomicAdd(at < mine_from ? &before[e] : &total[e], v[u]);
+        }
+      }
+    }
+    __syncthreads();
+    if (COUNTS == SUMMED)
+      for (int e = threadIdx.x; e < s.experts; e += THREADS) total[e] += before[e];
+    __syncthreads();
+    each_choice(s, segment * kSegment, begin, [&](int, int e) { atomicAdd(&before[e], 1); });
+  }
   __syncthreads();
-  if (WHOLE) {
+  if (COUNTS == WHOLE) {
     for (int e = threadIdx.x; e < s.experts; e += THREADS) total[e] += before[e];
     __syncthreads();
   }
@@ -200,7 +230,8 @@ __global__ void __launch_bounds__(THREADS) expert_dispatch_kernel(const SortArgs
         from[u] = x + (int64_t)div_mod((uint32_t)(begin + min(i, end - begin - 1)), a.by_k, rest) * a.ld_x;
         to[u] = slot < 0 ? nullptr : rows + (int64_t)slot * a.ld_out;
       }
-      for (int c = part * N; c < a.vectors; c += N << a.lanes_log) {
+      for (int c0 = part * N; c0 < a.vectors; c0 += N << a.lanes_log) {
+        const int c = min(c0, a.vectors - N);
         typename Row<T>::vec v[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) v[u] = ld_vec(from[u] + c);
@@ -252,7 +283,8 @@ __global__ void __launch_bounds__(kThreads) expert_scatter_kernel(const RowsArgs
   const T* x = static_cast<const T*>(a.x) + t * a.ld_x;
   T* rows = static_cast<T*>(a.out);
   const int lane = threadIdx.x & ((1 << a.lanes_log) - 1);
-  for (int c = lane * N; c < a.vectors; c += N << a.lanes_log) {
+  for (int c0 = lane * N; c0 < a.vectors; c0 += N << a.lanes_log) {
+    const int c = min(c0, a.vectors - N);
     const typename Row<T>::vec v = ld_vec(x + c);
     for (int j = 0; j < a.k; ++j) {
       const int32_t s = a.slot[t * a.k + j];
@@ -312,7 +344,7 @@ __global__ void __launch_bounds__(kThreads) expert_combine_kernel(const RowsArgs
   Choices<AHEAD> at;
   at.load(a, t * a.k, 0);
   for (int c = lane * N; c < a.vectors; c += VECS * N * LANES) {
-    const int col[2] = {c, VECS > 1 && c + N * LANES < a.vectors ? c + N * LANES : c};  // (the same vector twice where there is no second)
+    const int col[2] = {min(c, a.vectors - N), min(c + N * LANES, a.vectors - N)};  // (the last vector twice where there is no second)
     float s[VECS][N];
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
@@ -379,7 +411,8 @@ __global__ void __launch_bounds__(kThreads) expert_combine_bwd_kernel(const Rows
     float dot[AHEAD];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) dot[u] = 0.f;
-    for (int c = lane * N; c < a.vectors; c += N * LANES) {
+    for (int c0 = lane * N; c0 < a.vectors; c0 += N * LANES) {
+      const int c = min(c0, a.vectors - N);
       const typename Row<T>::vec g = ld_vec(x + c);
       typename Row<T>::vec v[AHEAD] = {};
       if (read) {
@@ -391,7 +424,7 @@ __global__ void __launch_bounds__(kThreads) expert_combine_bwd_kernel(const Rows
         typename Row<T>::vec o;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          dot[u] += (float)g[e] * (float)v[u][e];
+          dot[u] += e >= c0 - c ? (float)g[e] * (float)v[u][e] : 0.f;
           o[e] = (T)((float)g[e] * at.w[u]);
         }
         if (at.there[u]) st_vec<STREAM>(out + at.row[u] * a.ld_out + c, o);
@@ -423,7 +456,7 @@ int lanes_log_of(int d, int type) {
   return l;
 }
 
-int whole_vectors(int d, int type) { return d / (16 / row_type_bytes(type)) * (16 / row_type_bytes(type)); }
+int vector_columns(int d, int type) { return d >= 16 / row_type_bytes(type) ? d : 0; }
 
 // Rows that the last-level cache would not hold until they are read again go past it: 105402 x 1024 bf16 (216 MB) to the experts and back 142 -> 123 us, the gradients of
 // 52012 x 1024 fp16 (107 MB) 80 -> 68.  With two products each way in between there is nothing in it (216 MB: 1105 and 1107 us, 131 MB: 661 and 669), and smaller rows lose
@@ -486,25 +519,27 @@ extern "C" int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, i
   a.tokens = tokens, a.k = k, a.capacity = capacity, a.experts = experts, a.by_k = divisor(k), a.by_capacity = divisor(std::max(capacity, 1));
   if (d_rows) {
     a.x = d_x, a.ld_x = ld_x, a.out = d_rows, a.ld_out = ld_rows;
-    a.d = d, a.vectors = whole_vectors(d, type), a.lanes_log = lanes_log_of(d, type);
+    a.d = d, a.vectors = vector_columns(d, type), a.lanes_log = lanes_log_of(d, type);
   }
-  const bool whole = n <= kWhole;
+  s.by_experts = divisor(experts);
+  const bool whole = n <= kWhole, scan = (int64_t)s.segments * experts > kSummed;
   if (!whole) {
     hipLaunchKernelGGL(expert_count_kernel, dim3(s.segments), dim3(kThreads), sizeof(int32_t) * experts, stream, s);
     NMT_LAUNCH_CHECK();
-    hipLaunchKernelGGL(expert_scan_kernel, dim3(ceil_div(experts, kWave)), dim3(kScanWaves * kWave), 0, stream, s);
+    if (scan) hipLaunchKernelGGL(expert_scan_kernel, dim3(ceil_div(experts, kWave)), dim3(kScanWaves * kWave), 0, stream, s);
     NMT_LAUNCH_CHECK();
   }
   const dim3 grid(std::max(1, ceil_div(n, kChunk)));
   const size_t lds = sizeof(int32_t) * experts * 3;
   if (whole) {
-    if (!d_rows) hipLaunchKernelGGL((expert_dispatch_kernel<void, true, kWholeThreads>), grid, dim3(kWholeThreads), lds, stream, s, a);
-    else if (type == NMT_F32) hipLaunchKernelGGL((expert_dispatch_kernel<uint32_t, true, kWholeThreads>), grid, dim3(kWholeThreads), lds, stream, s, a);
-    else hipLaunchKernelGGL((expert_dispatch_kernel<uint16_t, true, kWholeThreads>), grid, dim3(kWholeThreads), lds, stream, s, a);
+    if (!d_rows) hipLaunchKernelGGL((expert_dispatch_kernel<void, WHOLE, kWholeThreads>), grid, dim3(kWholeThreads), lds, stream, s, a);
+    else if (type == NMT_F32) hipLaunchKernelGGL((expert_dispatch_kernel<uint32_t, WHOLE, kWholeThreads>), grid, dim3(kWholeThreads), lds, stream, s, a);
+    else hipLaunchKernelGGL((expert_dispatch_kernel<uint16_t, WHOLE, kWholeThreads>), grid, dim3(kWholeThreads), lds, stream, s, a);
     NMT_LAUNCH_CHECK();
     return NMT_OK;
   }
-  hipLaunchKernelGGL((expert_dispatch_kernel<void, false, kThreads>), grid, dim3(kThreads), lds, stream, s, a);
+  if (scan) hipLaunchKernelGGL((expert_dispatch_kernel<void, SCANNED, kThreads>), grid, dim3(kThreads), lds, stream, s, a);
+  else hipLaunchKernelGGL((expert_dispatch_kernel<void, SUMMED, kThreads>), grid, dim3(kThreads), lds, stream, s, a);
   NMT_LAUNCH_CHECK();
   if (!d_rows) return NMT_OK;
   const int per = kThreads >> a.lanes_log;
@@ -563,7 +598,9 @@ extern "C" int nmt_op_expert_combine(const void* d_rows, int64_t ld_rows, int32_
   EXPERT_ROWS(d_out, tokens, ld_out, "out");
   RowsArgs a = {};
   a.rows = d_rows, a.ld_rows = ld_rows, a.n_rows = n_rows, a.slot = d_slot, a.weights = d_weights, a.add = d_add, a.ld_add = ld_add;
-  a.out = d_out, a.ld_out = ld_out, a.tokens = tokens, a.k = k, a.d = d, a.vectors = whole_vectors(d, type), a.lanes_log = lanes_log_of(d, type);
+  a.out = d_out, a.ld_out = ld_out, a.tokens = tokens, a.k = k, a.d = d, a.lanes_log = lanes_log_of(d, type);
+  const int vec = 16 / row_type_bytes(type);
+  a.vectors = d_add && d_add == d_out ? d / vec * vec : vector_columns(d, type);
   if (type == NMT_F16) launch_combine<half_t>(a, stream);
   else if (type == NMT_BF16) launch_combine<bf16_t>(a, stream);
   else launch_combine<float>(a, stream);
@@ -590,7 +627,7 @@ extern "C" int nmt_op_expert_combine_bwd(const void* d_dout, int64_t ld_dout, co
   RowsArgs a = {};
   a.x = d_dout, a.ld_x = ld_dout, a.rows = d_rows, a.ld_rows = ld_rows, a.n_rows = n_rows, a.slot = d_slot, a.ranges = d_ranges;
   a.weights = d_weights, a.dweights = d_dweights, a.out = d_drows, a.ld_out = ld_drows;
-  a.tokens = tokens, a.k = k, a.d = d, a.vectors = whole_vectors(d, type), a.capacity = capacity, a.experts = experts, a.lanes_log = lanes_log_of(d, type);
+  a.tokens = tokens, a.k = k, a.d = d, a.vectors = vector_columns(d, type), a.capacity = capacity, a.experts = experts, a.lanes_log = lanes_log_of(d, type);
   a.by_capacity = divisor(std::max(capacity, 1));
   if (type == NMT_F16) launch_combine_bwd<half_t>(a, stream);
   else if (type == NMT_BF16) launch_combine_bwd<bf16_t>(a, stream);

@@ -1,7 +1,7 @@
 // The norms around a gated residual block, one pass over the rows each way:
 //   h = a x + gate post(y), n = pre(h);  post, pre: LayerNorm or RMS norm with gain and shift.
 // Bound by memory: forward reads x, y and writes h, n (n needs h's statistics, which are there while h is still in registers), backward
-// reads y, h and the gradients at h and n and writes those at x and y.  A row is held in registers by 16, 32 or 64 lanes (up to 128, 256, 512 columns) or by
+// reads y, h and the gradients at h and n and writes those at x and y.  A row is held in registers by 8 to 64 lanes (up to 64, 128, 256, 512 columns) or by
 // several wavefronts, each lane's share of it 16 bytes at a time; the next row is in flight while one is worked on.
 // Forward 52701 x 1024 bf16: 73 us, 5.9 TB/s (a copy of a gigabyte: 5.2).  Backward 26001 x 1024 fp16: 74 us, 4.3 TB/s, of which the sums over work-groups take 5;
 // a wavefront per SIMD has its registers full of column sums and two rows.  Rows of more than 8192 columns (fp32 backward: 4096) spill some of those.
@@ -481,16 +481,16 @@ __global__ void __launch_bounds__(kSumCols* kSumLanes) gated_norm_sums_kernel(co
   }
 }
 
-// What a row of d columns is held by: -1: 16 lanes of one column (of less than a vector), 0, 1, 2: 16, 32, 64 lanes of 8, 3 to 6: wavefronts of 8 columns a lane forward and of 16
-// backward, 7: 16 wavefronts of 16.
+// What a row of d columns is held by: -1: 16 lanes of one column (of less than a vector), 0 to 3: 8, 16, 32, 64 lanes of 8, 4 to 7: wavefronts of 8 columns a lane forward and of 16
+// backward, 8: 16 wavefronts of 16.
 int shape_of(int d, int type) {
   if (d < 16 / row_type_bytes(type)) return -1;
   int s = 0;
-  for (int most = 128; s < 7 && d > most; ++s) most *= 2;
+  for (int most = 64; s < 8 && d > most; ++s) most *= 2;
   return s;
 }
-int waves_of_row(int shape, bool wide) { return shape <= 2 ? 1 : wide ? std::min(16, 2 << (shape - 3)) : 1 << (shape - 3); }
-int workers_of(int shape, bool wide) { return shape <= 0 ? 16 : shape == 1 ? 8 : waves_of_row(shape, wide) == 1 ? 4 : 1; }  // of a work-group
+int waves_of_row(int shape, bool wide) { return shape <= 3 ? 1 : wide ? std::min(16, 2 << (shape - 4)) : 1 << (shape - 4); }
+int workers_of(int shape, bool wide) { return shape < 0 ? 16 : shape <= 3 ? 32 >> shape : waves_of_row(shape, wide) == 1 ? 4 : 1; }  // of a work-group
 bool wide_bwd(int type) { return type == NMT_F32; }
 
 // Forward: two rows a worker, so that the second's loads are under way while the first is worked on and gains are fetched half as often, if that still makes
@@ -541,13 +541,14 @@ int64_t scratch_floats(int rows, int d, int rows_per_gate) {
   constexpr int v8 = 8 / Row<T>::kVec, v = (WIDE) ? v8 : 2 * v8, w = (WIDE) ? 2 : 1;                       \
   switch (shape) {                                                                                         \
     case -1: NORM_LAUNCH(KERNEL, T, 0, 16, 1, __VA_ARGS__) break;                                          \
-    case 0: NORM_LAUNCH(KERNEL, T, v8, 16, 1, __VA_ARGS__) break;                                          \
-    case 1: NORM_LAUNCH(KERNEL, T, v8, 32, 1, __VA_ARGS__) break;                                          \
-    case 2: NORM_LAUNCH(KERNEL, T, v8, 64, 1, __VA_ARGS__) break;                                          \
-    case 3: NORM_LAUNCH(KERNEL, T, v, 64, w, __VA_ARGS__) break;                                           \
-    case 4: NORM_LAUNCH(KERNEL, T, v, 64, 2 * w, __VA_ARGS__) break;                                       \
-    case 5: NORM_LAUNCH(KERNEL, T, v, 64, 4 * w, __VA_ARGS__) break;                                       \
-    case 6: NORM_LAUNCH(KERNEL, T, v, 64, 8 * w, __VA_ARGS__) break;                                       \
+    case 0: NORM_LAUNCH(KERNEL, T, v8, 8, 1, __VA_ARGS__) break;                                           \
+    case 1: NORM_LAUNCH(KERNEL, T, v8, 16, 1, __VA_ARGS__) break;                                          \
+    case 2: NORM_LAUNCH(KERNEL, T, v8, 32, 1, __VA_ARGS__) break;                                          \
+    case 3: NORM_LAUNCH(KERNEL, T, v8, 64, 1, __VA_ARGS__) break;                                          \
+    case 4: NORM_LAUNCH(KERNEL, T, v, 64, w, __VA_ARGS__) break;                                           \
+    case 5: NORM_LAUNCH(KERNEL, T, v, 64, 2 * w, __VA_ARGS__) break;                                       \
+    case 6: NORM_LAUNCH(KERNEL, T, v, 64, 4 * w, __VA_ARGS__) break;                                       \
+    case 7: NORM_LAUNCH(KERNEL, T, v, 64, 8 * w, __VA_ARGS__) break;                                       \
     default: NORM_LAUNCH(KERNEL, T, 2 * v8, 64, 16, __VA_ARGS__)                                           \
   }
 

@@ -27,7 +27,7 @@ __device__ __forceinline__ void st_vec(T* p, const typename Row<T>::vec& x) {
   else *v = x;
 }
 
-// Sum over a wavefront's groups of 16, 32 or 64 lanes; every lane gets its group's.
+// Sum over a wavefront's groups of 8, 16, 32 or 64 lanes; every lane gets its group's.
 template <int LANES>
 __device__ __forceinline__ float lanes_sum(float v) {
   if constexpr (LANES == 64) {
@@ -40,8 +40,12 @@ __device__ __forceinline__ float lanes_sum(float v) {
       const auto h = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
       v = __builtin_bit_cast(float, (unsigned)h[0]) + __builtin_bit_cast(float, (unsigned)h[1]);
     }
-    v = plus(v, std::integral_constant<int, 0x128>{});    // row_ror:8
-    v = plus(v, std::integral_constant<int, 0x124>{});    // row_ror:4
+    if constexpr (LANES == 8) {
+      v = plus(v, std::integral_constant<int, 0x141>{});  // row_half_mirror
+    } else {
+      v = plus(v, std::integral_constant<int, 0x128>{});  // row_ror:8
+      v = plus(v, std::integral_constant<int, 0x124>{});  // row_ror:4
+    }
     v = plus(v, std::integral_constant<int, 0x4E>{});     // quad_perm:[2,3,0,1]
     return plus(v, std::integral_constant<int, 0xB1>{});  // quad_perm:[1,0,3,2]
   }
