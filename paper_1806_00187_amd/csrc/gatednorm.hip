@@ -4,7 +4,8 @@
 // reads y, h and the gradients at h and n and writes those at x and y.  A row is held in registers by 8 to 64 lanes (up to 64, 128, 256, 512 columns) or by
 // several wavefronts, each lane's share of it 16 bytes at a time; the next row is in flight while one is worked on.
 // Forward 52701 x 1024 bf16: 73 us, 5.9 TB/s (a copy of a gigabyte: 5.2).  Backward 26001 x 1024 fp16: 74 us, 4.3 TB/s, of which the sums over work-groups take 5;
-// a wavefront per SIMD has its registers full of column sums and two rows.  Rows of more than 8192 columns (fp32 backward: 4096) spill some of those.
+// a wavefront per SIMD has its registers full of column sums and two rows.  Backward, fp32 rows of 4097 to 8192 columns do without the second row (3001 x 5000: 120 us for 360 MB), and
+// rows of more than 8192 spill (2001 x 9000 bf16: 316 us for 216 MB).
 #include "rowtypes.h"
 
 #include <algorithm>
@@ -190,11 +191,15 @@ __global__ void __launch_bounds__(S::kThreads) gated_norm_fwd_kernel(const NormA
   const int64_t worker = (int64_t)blockIdx.x * S::kRows + S::worker();
   const int64_t begin = min(worker * a.chunk, (int64_t)a.rows), end = min(begin + a.chunk, (int64_t)a.rows);
   V post_gain, post_shift, pre_gain, pre_shift, gate, next_gate, next_x, next_y;
-  if (a.post_gain) post_gain.load(a.post_gain, 0, c);
-  if (a.post_shift) post_shift.load(a.post_shift, 0, c);
-  if (!GROUPED && a.gate) gate.load(a.gate, 0, c);
-  if (a.n) pre_gain.load(a.pre_gain, 0, c);
-  if (a.pre_shift) pre_shift.load(a.pre_shift, 0, c);
+  auto vectors = [&] {
+    if (a.post_gain) post_gain.load(a.post_gain, 0, c);
+    if (a.post_shift) post_shift.load(a.post_shift, 0, c);
+    if (!GROUPED && a.gate) gate.load(a.gate, 0, c);
+    if (a.n) pre_gain.load(a.pre_gain, 0, c);
+    if (a.pre_shift) pre_shift.load(a.pre_shift, 0, c);
+  };
+  constexpr bool AHEAD = WAVES <= 8 || E <= 8;  // (16 wavefronts of 16 columns a lane: 128 registers, which do not hold two rows and the gains)
+  if (AHEAD) vectors();
   auto ask = [&](int64_t row) {
     next_x.load(a.x, row * a.ld_x, c);
     if (a.y) next_y.load(a.y, row * a.ld_y, c);
@@ -216,12 +221,16 @@ __global__ void __launch_bounds__(S::kThreads) gated_norm_fwd_kernel(const NormA
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] *= rstd;
   };
-  if (begin < end) ask(begin);
+  if (AHEAD && begin < end) ask(begin);
   for (int64_t row = begin; row < end; ++row) {
+    if (!AHEAD) {
+      ask(row);
+      vectors();
+    }
     const V x = next_x, y = next_y;
     if (GROUPED) gate = next_gate;
-    if (row + 1 < end) ask(row + 1);
-    __builtin_amdgcn_sched_barrier(0);
+    if (AHEAD && row + 1 < end) ask(row + 1);
+    if (AHEAD) __builtin_amdgcn_sched_barrier(0);
     float h[E], mean_y = 0.f, rstd_y = 1.f, mean_h = 0.f, rstd_h = 1.f;
     V out_h, out_n;
 #pragma unroll
@@ -258,9 +267,11 @@ __global__ void __launch_bounds__(S::kThreads) gated_norm_fwd_kernel(const NormA
       out_h.arrive();
       __syncthreads();
     }
-    next_x.arrive();
-    if (a.y) next_y.arrive();
-    if (GROUPED) next_gate.arrive();
+    if (AHEAD) {
+      next_x.arrive();
+      if (a.y) next_y.arrive();
+      if (GROUPED) next_gate.arrive();
+    }
     if (a.stream) {
       if (a.y) out_h.store_nt(a.h, row * a.ld_h, c);
       if (a.n) out_n.store_nt(a.n, row * a.ld_n, c);
@@ -278,7 +289,7 @@ __global__ void __launch_bounds__(S::kThreads) gated_norm_fwd_kernel(const NormA
 // rows end it is written if all of them were this worker's, and else left as a partial sum, of which a worker has two at most (of the gate it
 // begins in, if that began before it, and of the one it ends in).
 template <typename S, bool GROUPED, bool SHIFTS>
-__global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 : S::kWaves > 8 ? 4 : 1) gated_norm_bwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 : 1) gated_norm_bwd_kernel(const NormArgs a) {
   constexpr int E = S::kE, LANES = S::kLanes, WAVES = S::kWaves, SUMS = SHIFTS ? 4 : 2;
   using V = Share<S>;
   __shared__ float red[4][WAVES];
@@ -292,10 +303,17 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
   V gain, shift, pre, gate, next_gate, next_dh, next_dn, next_h, next_y;
   float4_any next_st;
   gain.fill(1.f), shift.fill(0.f), gate.fill(1.f), next_dh.fill(0.f);  // (where there is none)
-  if (a.post_gain) gain.load(a.post_gain, 0, c);
-  if (GROUPED && SHIFTS && a.post_shift) shift.load(a.post_shift, 0, c);
-  if (!GROUPED && a.gate) gate.load(a.gate, 0, c);
-  if (a.dn) pre.load(a.pre_gain, 0, c);
+  auto vectors_after = [&] {
+    if (a.post_gain) gain.load(a.post_gain, 0, c);
+    if (GROUPED && SHIFTS && a.post_shift) shift.load(a.post_shift, 0, c);
+    if (!GROUPED && a.gate) gate.load(a.gate, 0, c);
+  };
+  auto vectors_before = [&] {
+    if (a.dn) pre.load(a.pre_gain, 0, c);
+  };
+  // Where the column sums and a row fill the registers by themselves gains are fetched where they are used, row after row.
+  constexpr bool AHEAD = E * sizeof(typename S::type) <= 32;
+  if (AHEAD) vectors_after(), vectors_before();
   float sum[SUMS][E], gate_sum[GROUPED ? E : 1];
 #pragma unroll
   for (int q = 0; q < SUMS; ++q) fill(sum[q], 0.f);
@@ -329,8 +347,12 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
       fill(gate_sum, 0.f);
     }
   };
-  if (begin < end) ask(begin);
+  if (AHEAD && begin < end) ask(begin);
   for (int64_t row = begin; row < end; ++row) {
+    if (!AHEAD) {
+      ask(row);
+      vectors_before();
+    }
     const V dh = next_dh, dn = next_dn, h = next_h, y = next_y;
     const float4_any st = next_st;
     if (GROUPED && other_gate) {
@@ -338,8 +360,8 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
       gate = next_gate;
       gate_row = gates.row;
     }
-    if (row + 1 < end) ask(row + 1);
-    __builtin_amdgcn_sched_barrier(0);
+    if (AHEAD && row + 1 < end) ask(row + 1);
+    if (AHEAD) __builtin_amdgcn_sched_barrier(0);
     float g[E];  // the gradient at h
 #pragma unroll
     for (int e = 0; e < E; ++e) g[e] = dh(e);
@@ -362,6 +384,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
       for (int e = 0; e < E; ++e) out[e] = a.resid_scale * g[e];
       out_x.set(out);
     }
+    if (!AHEAD) vectors_after();
     if (a.y) {
       const float rstd = st[1], off = -st[0] * st[1];
 #pragma unroll
@@ -381,10 +404,12 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
       }
       out_y.set(g);
     }
-    if (a.dn) next_h.arrive(), next_dn.arrive();
-    if (a.dh) next_dh.arrive();
-    if (a.y) next_y.arrive();
-    asm volatile("" : "+v"(next_st));
+    if (AHEAD) {
+      if (a.dn) next_h.arrive(), next_dn.arrive();
+      if (a.dh) next_dh.arrive();
+      if (a.y) next_y.arrive();
+      asm volatile("" : "+v"(next_st));
+    }
     if (WAVES > 1) {  // the sums' places are used again; and dx may lie where dh does, dy where dn, of which lanes of two wavefronts may have loaded the same
       out_x.arrive();
       if (a.y) out_y.arrive();
@@ -481,35 +506,37 @@ __global__ void __launch_bounds__(kSumCols* kSumLanes) gated_norm_sums_kernel(co
   }
 }
 
-// What a row of d columns is held by: -1: 16 lanes of one column (of less than a vector), 0 to 3: 8, 16, 32, 64 lanes of 8, 4 to 7: wavefronts of 8 columns a lane forward and of 16
-// backward, 8: 16 wavefronts of 16.
+// What a row of d columns is held by: -1: 16 lanes of one column (of less than a vector), 0 to 3: 8, 16, 32, 64 lanes of 8, 4 to 7: 2 to 16 wavefronts of 8 columns a lane, or, backward and
+// 16-bit, 1 to 8 of 16 (fp32: 8 of 16 instead of 16 of 8), 8: 16 of 16, backward 8 of 32.
+enum { kForward, kBackward, kBackwardWide };
 int shape_of(int d, int type) {
   if (d < 16 / row_type_bytes(type)) return -1;
   int s = 0;
   for (int most = 64; s < 8 && d > most; ++s) most *= 2;
   return s;
 }
-int waves_of_row(int shape, bool wide) { return shape <= 3 ? 1 : wide ? std::min(16, 2 << (shape - 4)) : 1 << (shape - 4); }
-int workers_of(int shape, bool wide) { return shape < 0 ? 16 : shape <= 3 ? 32 >> shape : waves_of_row(shape, wide) == 1 ? 4 : 1; }  // of a work-group
-bool wide_bwd(int type) { return type == NMT_F32; }
+int waves_of_row(int shape, int form) { return shape <= 3 ? 1 : form == kForward ? std::min(16, 2 << (shape - 4)) : std::min(8, (form == kBackward ? 1 : 2) << (shape - 4)); }
+int workers_of(int shape, int form) { return shape < 0 ? 16 : shape <= 3 ? 32 >> shape : waves_of_row(shape, form) == 1 ? 4 : 1; }  // of a work-group
+int backward_form(int type) { return type == NMT_F32 ? kBackwardWide : kBackward; }
 
 // Forward: two rows a worker, so that the second's loads are under way while the first is worked on and gains are fetched half as often, if that still makes
 // kFwdWaves wavefronts, and one otherwise (26001 x 1024 fp16, one row, two, three: 48, 43, 45 us; 2001 x 8000 fp32, one, two: 68, 61).
 // Backward: every work-group leaves a row of column sums, so no more of them than run side by side (kBwdWaves: a wavefront per SIMD with its
 // registers full; 1280, 2048 and 3072 cost 26001 x 1024 fp16 90, 75 and 78 us instead of 74, and 3584 x 512 15, 14 and 15 instead of 13).
 constexpr int kFwdWaves = 4096, kBwdWaves = 1024;
+int bwd_groups(int waves) { return std::max(kBwdWaves / waves, device_info().cus); }  // (of wavefronts for a row: one work-group to a compute unit)
 constexpr int64_t kStreamFrom = 64 << 20;  // bytes of a result
 
 struct Split {
   int chunk, groups, workers, pitch;
 };
-Split split_rows(int rows, int d, int type, bool wide, bool forward, int rows_per_gate) {
-  const int shape = shape_of(d, type), at_once = workers_of(shape, wide), waves = std::max(at_once > 1 ? 4 : 1, waves_of_row(shape, wide));
+Split split_rows(int rows, int d, int type, int form, int rows_per_gate) {
+  const int shape = shape_of(d, type), at_once = workers_of(shape, form), waves = std::max(at_once > 1 ? 4 : 1, waves_of_row(shape, form));
   Split p;
-  if (forward) {
+  if (form == kForward) {
     p.chunk = (int64_t)rows * waves >= (int64_t)2 * kFwdWaves * at_once ? std::max(2, ceil_div(rows, (int64_t)at_once << 22)) : 1;  // (a grid has less than 2^32 threads)
   } else {
-    p.chunk = ceil_div(rows, kBwdWaves / waves * at_once);
+    p.chunk = ceil_div(rows, bwd_groups(waves) * at_once);
     if (rows_per_gate < rows && rows_per_gate <= 2 * (int64_t)p.chunk) p.chunk = ceil_div(p.chunk, rows_per_gate) * rows_per_gate;  // no gate's rows are two workers' then
   }
   p.groups = ceil_div(rows, p.chunk * at_once);
@@ -521,14 +548,13 @@ Split split_rows(int rows, int d, int type, bool wide, bool forward, int rows_pe
 int64_t scratch_floats(int rows, int d, int rows_per_gate) {
   int64_t most = 0;
   for (int type : {NMT_F16, NMT_F32}) {
-    const int shape = shape_of(d, type), at_once = workers_of(shape, wide_bwd(type)), waves = std::max(at_once > 1 ? 4 : 1, waves_of_row(shape, wide_bwd(type)));
-    const int64_t groups = std::min(ceil_div(rows, at_once), kBwdWaves / waves), pitch = (d + 7) / 8 * 8;
+    const int shape = shape_of(d, type), form = backward_form(type), at_once = workers_of(shape, form), waves = std::max(at_once > 1 ? 4 : 1, waves_of_row(shape, form));
+    const int64_t groups = std::min(ceil_div(rows, at_once), bwd_groups(waves)), pitch = (d + 7) / 8 * 8;
     most = std::max(most, groups * 4 * pitch + (rows_per_gate < rows ? groups * at_once * 2 * pitch : 0));
   }
   return most;
 }
 
-// WIDE: 8 columns a lane and twice the wavefronts for rows of more than 512.
 #define NORM_LAUNCH(KERNEL, T, VECS, LANES, WAVES, ...)                                                                  \
   if ((VECS) && a.d % Row<T>::kVec) {                                                                                    \
     using S = Shape<T, VECS, LANES, WAVES, true>;                                                                        \
@@ -537,34 +563,36 @@ int64_t scratch_floats(int rows, int d, int rows_per_gate) {
     using S = Shape<T, VECS, LANES, WAVES, false>;                                                                       \
     hipLaunchKernelGGL((KERNEL<S, __VA_ARGS__>), grid, dim3(S::kThreads), 0, stream, a);                                 \
   }
-#define NORM_SHAPES(KERNEL, T, WIDE, ...)                                                                  \
-  constexpr int v8 = 8 / Row<T>::kVec, v = (WIDE) ? v8 : 2 * v8, w = (WIDE) ? 2 : 1;                       \
-  switch (shape) {                                                                                         \
-    case -1: NORM_LAUNCH(KERNEL, T, 0, 16, 1, __VA_ARGS__) break;                                          \
-    case 0: NORM_LAUNCH(KERNEL, T, v8, 8, 1, __VA_ARGS__) break;                                           \
-    case 1: NORM_LAUNCH(KERNEL, T, v8, 16, 1, __VA_ARGS__) break;                                          \
-    case 2: NORM_LAUNCH(KERNEL, T, v8, 32, 1, __VA_ARGS__) break;                                          \
-    case 3: NORM_LAUNCH(KERNEL, T, v8, 64, 1, __VA_ARGS__) break;                                          \
-    case 4: NORM_LAUNCH(KERNEL, T, v, 64, w, __VA_ARGS__) break;                                           \
-    case 5: NORM_LAUNCH(KERNEL, T, v, 64, 2 * w, __VA_ARGS__) break;                                       \
-    case 6: NORM_LAUNCH(KERNEL, T, v, 64, 4 * w, __VA_ARGS__) break;                                       \
-    case 7: NORM_LAUNCH(KERNEL, T, v, 64, 8 * w, __VA_ARGS__) break;                                       \
-    default: NORM_LAUNCH(KERNEL, T, 2 * v8, 64, 16, __VA_ARGS__)                                           \
+// FORM: see shape_of.
+#define NORM_SHAPES(KERNEL, T, FORM, ...)                                                                                \
+  constexpr int v8 = 8 / Row<T>::kVec, v = (FORM) == kBackward ? 2 * v8 : v8, w = (FORM) == kBackward ? 1 : 2;           \
+  constexpr bool f = (FORM) == kForward;                                                                                 \
+  switch (shape) {                                                                                                       \
+    case -1: NORM_LAUNCH(KERNEL, T, 0, 16, 1, __VA_ARGS__) break;                                                        \
+    case 0: NORM_LAUNCH(KERNEL, T, v8, 8, 1, __VA_ARGS__) break;                                                         \
+    case 1: NORM_LAUNCH(KERNEL, T, v8, 16, 1, __VA_ARGS__) break;                                                        \
+    case 2: NORM_LAUNCH(KERNEL, T, v8, 32, 1, __VA_ARGS__) break;                                                        \
+    case 3: NORM_LAUNCH(KERNEL, T, v8, 64, 1, __VA_ARGS__) break;                                                        \
+    case 4: NORM_LAUNCH(KERNEL, T, v, 64, w, __VA_ARGS__) break;                                                         \
+    case 5: NORM_LAUNCH(KERNEL, T, v, 64, 2 * w, __VA_ARGS__) break;                                                     \
+    case 6: NORM_LAUNCH(KERNEL, T, v, 64, 4 * w, __VA_ARGS__) break;                                                     \
+    case 7: NORM_LAUNCH(KERNEL, T, f ? v8 : 2 * v8, 64, f ? 16 : 8, __VA_ARGS__) break;                                  \
+    default: NORM_LAUNCH(KERNEL, T, f ? 2 * v8 : 4 * v8, 64, f ? 16 : 8, __VA_ARGS__)                                    \
   }
 
 template <typename T>
 void launch_fwd(const NormArgs& a, dim3 grid, int shape, bool grouped, hipStream_t stream) {
-  if (grouped) { NORM_SHAPES(gated_norm_fwd_kernel, T, true, true) }
-  else { NORM_SHAPES(gated_norm_fwd_kernel, T, true, false) }
+  if (grouped) { NORM_SHAPES(gated_norm_fwd_kernel, T, kForward, true) }
+  else { NORM_SHAPES(gated_norm_fwd_kernel, T, kForward, false) }
 }
 template <typename T>
 void launch_bwd(const NormArgs& a, dim3 grid, int shape, bool grouped, hipStream_t stream) {
-  constexpr bool wide = sizeof(T) == 4;  // (wide_bwd)
+  constexpr int form = sizeof(T) == 4 ? kBackwardWide : kBackward;  // (backward_form)
   const bool shifts = a.sums > 2;
-  if (grouped && shifts) { NORM_SHAPES(gated_norm_bwd_kernel, T, wide, true, true) }
-  else if (grouped) { NORM_SHAPES(gated_norm_bwd_kernel, T, wide, true, false) }
-  else if (shifts) { NORM_SHAPES(gated_norm_bwd_kernel, T, wide, false, true) }
-  else { NORM_SHAPES(gated_norm_bwd_kernel, T, wide, false, false) }
+  if (grouped && shifts) { NORM_SHAPES(gated_norm_bwd_kernel, T, form, true, true) }
+  else if (grouped) { NORM_SHAPES(gated_norm_bwd_kernel, T, form, true, false) }
+  else if (shifts) { NORM_SHAPES(gated_norm_bwd_kernel, T, form, false, true) }
+  else { NORM_SHAPES(gated_norm_bwd_kernel, T, form, false, false) }
 }
 template <typename T>
 void launch_sums(const NormArgs& a, bool grouped, hipStream_t stream) {
@@ -634,7 +662,7 @@ extern "C" int nmt_op_gated_norm_fwd(const nmt_gated_norm* a, void* stream_) {
   NORM_ROWS(a->d_h, a->ld_h, "h");
   NORM_ROWS(a->d_n, a->ld_n, "n");
   NormArgs k = common_args(a);
-  const Split p = split_rows(a->rows, a->d, a->type, true, true, a->rows);
+  const Split p = split_rows(a->rows, a->d, a->type, kForward, a->rows);
   k.chunk = p.chunk;
   const bool grouped = a->d_gate && a->rows_per_gate < a->rows;
   const int shape = shape_of(a->d, a->type);
@@ -686,7 +714,7 @@ extern "C" int nmt_op_gated_norm_bwd(const nmt_gated_norm* a, const nmt_gated_no
     return NMT_ENOMEM;
   }
   NMT_REQUIRE(aligned16(g->d_scratch), "%s: the scratch buffer must be 16-byte aligned", who);
-  const Split p = split_rows(a->rows, a->d, a->type, wide_bwd(a->type), false, k.rows_per_gate);
+  const Split p = split_rows(a->rows, a->d, a->type, backward_form(a->type), k.rows_per_gate);
   k.chunk = p.chunk, k.groups = p.groups, k.pitch = p.pitch;
   k.sums = a->d_post_shift || g->d_dpost_shift || g->d_dpre_shift ? 4 : 2;
   k.partial = g->d_scratch, k.gate_partial = g->d_scratch + (int64_t)p.groups * 4 * p.pitch;
