@@ -12,11 +12,16 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kSegment = 1024;      // choices that share a row of counts
-constexpr int kChunk = kWave;       // choices of a work-group of the dispatch
+constexpr int kChunk = kWave;       // choices of a work-group of the dispatch, or fewer (spread)
 constexpr int kWhole = 16384;       // up to so many choices every work-group of the dispatch counts all of them itself
 constexpr int kSummed = 4096;       // up to so many counts of segments every work-group adds up itself (32768 choices to 64 experts and back 33.6 -> 31.4 us, 105402: 124 -> 127)
 constexpr int kWholeThreads = 1024;
+constexpr int kGroups = 256;        // a compute unit each
+constexpr int64_t kCopied = 32 << 10;  // bytes that a work-group of kWholeThreads has in flight
 constexpr int64_t kStreamFrom = 96 << 20;  // bytes of the experts' rows (large_rows)
+// Fewer wavefronts than these leave compute units waiting: the columns of a token's row go to several.  16 tokens of 8 x 8192 bf16 to the experts and back 21.9 -> 9.8 us,
+// 8000 of 4 x 4096 123 -> 118; gradients 46 -> 11.8 and 178 -> 164.
+constexpr int kFewWaves = 8192;
 constexpr int kMaxExperts = 1024, kMaxChoices = 64;
 constexpr int64_t kMaxItems = 1 << 29;
 
@@ -24,7 +29,7 @@ typedef int32_t int4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 struct SortArgs {
   const int32_t* expert;
-  int n, experts, capacity, segments, bits;
+  int n, experts, capacity, segments, bits, chunk;
   Divisor by_experts;
   int32_t *hist, *totals, *slot, *ranges;
 };
@@ -101,7 +106,7 @@ struct RowsArgs {
   const int32_t *slot, *ranges;
   const float* weights;
   float* dweights;
-  int tokens, k, d, n_rows, capacity, experts, lanes_log;  // 2^lanes_log lanes take a row
+  int tokens, k, d, n_rows, capacity, experts, lanes_log, parts_log;  // 2^lanes_log lanes take a row; of a combine, 2^parts_log wavefronts
   // A row's columns [0, vectors) go in vectors of 16 bytes, the last of which ends with them: where `vectors` is no multiple of a vector it has elements in common with the one
   // before, which come out the same.  The columns from `vectors` on go one by one: of rows shorter than a vector, and of sums formed in place, where nothing may be read twice.
   int vectors;
@@ -127,7 +132,7 @@ __global__ void __launch_bounds__(THREADS) expert_dispatch_kernel(const SortArgs
   __shared__ int32_t slots[kChunk], waves[THREADS / kWave];
   int32_t *before = lds, *total = lds + s.experts, *first = total + s.experts;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int begin = (int)min((int64_t)blockIdx.x * kChunk, (int64_t)s.n), end = min(begin + kChunk, s.n);
+  const int begin = (int)min((int64_t)blockIdx.x * s.chunk, (int64_t)s.n), end = min(begin + s.chunk, s.n);  // (nothing behind the last chunk: only rows to clear)
   const int segment = begin / kSegment;
   for (int e = threadIdx.x; e < s.experts; e += THREADS) {
     before[e] = COUNTS == SCANNED ? s.hist[(int64_t)segment * s.experts + e] : 0;
@@ -323,11 +328,19 @@ struct Choices {
     }
   }
 };
+// A single element, rounded as those of a vector are: to fp32 and then to T.  (One instruction would do both and round once, so that results in place, where rows end in
+// single elements, would differ from others now and then.)
+template <typename T>
+__device__ __forceinline__ T rounded(float v) {
+  asm volatile("" : "+v"(v));
+  return (T)v;
+}
+
 // The token of LANES lanes; of a whole wavefront a number the scalar unit holds, and with it its slots and weights.
 template <int LANES>
 __device__ __forceinline__ int64_t token_of() {
   const uint32_t mine = threadIdx.x / LANES;
-  return group_of() * (kThreads / LANES) + (LANES == 64 ? __builtin_amdgcn_readfirstlane(mine) : mine);
+  return group_of() * (kThreads / LANES) + (LANES >= 64 ? __builtin_amdgcn_readfirstlane(mine) : mine);
 }
 
 // out[t] = add[t] + sum over j of weights[t, j] rows[slot[t, j]], in the order of j.  LANES lanes per token; AHEAD rows, two vectors a lane of each, are asked for together.
@@ -336,14 +349,16 @@ __global__ void __launch_bounds__(kThreads) expert_combine_kernel(const RowsArgs
   constexpr int N = Row<T>::kVec, VECS = LANES == 64 ? 2 : 1;
   touch(a);
   const int lane = threadIdx.x % LANES;
-  const int64_t t = token_of<LANES>();
+  const int64_t mine = token_of<LANES>(), t = LANES == 64 ? mine >> a.parts_log : mine;
+  const int part = LANES == 64 ? (int)mine & ((1 << a.parts_log) - 1) : 0;
+  const int step = (VECS * N * LANES) << (LANES == 64 ? a.parts_log : 0);
   if (t >= a.tokens) return;
   const T* add = static_cast<const T*>(a.add) + t * a.ld_add;
   const T* rows = static_cast<const T*>(a.rows);
   T* out = static_cast<T*>(a.out) + t * a.ld_out;
   Choices<AHEAD> at;
   at.load(a, t * a.k, 0);
-  for (int c = lane * N; c < a.vectors; c += VECS * N * LANES) {
+  for (int c = (part * VECS * LANES + lane) * N; c < a.vectors; c += step) {
     const int col[2] = {min(c, a.vectors - N), min(c + N * LANES, a.vectors - N)};  // (the last vector twice where there is no second)
     float s[VECS][N];
 #pragma unroll
@@ -375,7 +390,7 @@ __global__ void __launch_bounds__(kThreads) expert_combine_kernel(const RowsArgs
       st_vec<STREAM>(out + col[i], o);
     }
   }
-  if (const int c = a.vectors + lane; c < a.d) {
+  if (const int c = a.vectors + lane; c < a.d && part == 0) {
     float s = a.add ? (float)add[c] : 0.f;
     for (int j0 = 0; j0 < a.k && a.n_rows > 0; j0 += AHEAD) {
       if (a.k > AHEAD) at.load(a, t * a.k, j0);
@@ -385,7 +400,7 @@ __global__ void __launch_bounds__(kThreads) expert_combine_kernel(const RowsArgs
         s = at.there[u] ? s + at.w[u] * v : s;
       }
     }
-    out[c] = (T)s;
+    out[c] = rounded<T>(s);
   }
 }
 
@@ -393,6 +408,7 @@ __global__ void __launch_bounds__(kThreads) expert_combine_kernel(const RowsArgs
 template <typename T, int LANES, int AHEAD, bool STREAM>
 __global__ void __launch_bounds__(kThreads) expert_combine_bwd_kernel(const RowsArgs a) {
   constexpr int N = Row<T>::kVec;
+  __shared__ float part[LANES / kWave + 1][AHEAD];
   touch(a);
   if (group_of() >= a.token_groups) {
     clear_rows<T>(a, a.out, a.ld_out, group_of() - a.token_groups);
@@ -436,15 +452,28 @@ __global__ void __launch_bounds__(kThreads) expert_combine_bwd_kernel(const Rows
       for (int u = 0; u < AHEAD; ++u) {
         if (!at.there[u]) continue;
         if (read) dot[u] += g * (float)rows[at.row[u] * a.ld_rows + c];
-        out[at.row[u] * a.ld_out + c] = (T)(g * at.w[u]);
+        out[at.row[u] * a.ld_out + c] = rounded<T>(g * at.w[u]);
       }
     }
     if (a.dweights) {
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        const float s = lanes_sum<LANES>(dot[u]);
-        if (lane == 0 && j0 + u < a.k) a.dweights[t * a.k + j0 + u] = at.there[u] ? s : 0.f;
+        dot[u] = lanes_sum<LANES < kWave ? LANES : kWave>(dot[u]);
+        if (LANES > kWave && lane % kWave == 0) part[lane / kWave][u] = dot[u];
       }
+      if (LANES > kWave) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+          dot[u] = 0.f;
+#pragma unroll
+          for (int w = 0; w < LANES / kWave; ++w) dot[u] += part[w][u];
+        }
+        __syncthreads();
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (lane == 0 && j0 + u < a.k) a.dweights[t * a.k + j0 + u] = at.there[u] ? dot[u] : 0.f;
     }
   }
 }
@@ -468,6 +497,13 @@ int segments_of(int64_t n) { return (int)((n + kSegment - 1) / kSegment); }
 dim3 grid_of(int64_t groups) {
   const int64_t x = std::min<int64_t>(groups, 1 << 20);
   return dim3((uint32_t)x, x ? (uint32_t)((groups + x - 1) / x) : 1);
+}
+
+// A dispatch of one launch: chunks of fewer choices where these work-groups are few and have much to copy each (16 tokens of 8 x 8192 bf16 and back 37.8 -> 21.9 us), and
+// work-groups beyond the chunks' to clear rows (64 experts' 512 rows of 512 fp16 for 128 choices 213 -> 12 us).
+void spread(int64_t n, int64_t row_bytes, int64_t room, int* chunk, int* groups) {
+  while (*chunk > 1 && *groups < kGroups && *chunk * row_bytes > kCopied) *chunk /= 2, *groups = ceil_div(n, *chunk);
+  *groups = std::max<int64_t>(*groups, std::min<int64_t>(kGroups, room * row_bytes / kCopied));
 }
 
 int64_t scratch_of(int tokens, int k, int experts) { return tokens ? (int64_t)(segments_of((int64_t)tokens * k) + 1) * experts : 0; }
@@ -510,6 +546,7 @@ extern "C" int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, i
     nmt_set_error("%s: scratch of %lld elements, %lld needed", who, (long long)(d_scratch ? scratch_ints : 0), (long long)need);
     return NMT_ENOMEM;
   }
+  NMT_REQUIRE(tokens == 0 || d_expert != d_slot, "%s: slots in place of the choices, which every work-group reads", who);
   SortArgs s = {};
   s.expert = d_expert, s.n = (int)n, s.experts = experts, s.capacity = capacity, s.segments = segments_of(n);
   s.hist = d_scratch, s.totals = d_scratch + (int64_t)s.segments * experts, s.slot = d_slot, s.ranges = d_ranges;
@@ -529,7 +566,10 @@ extern "C" int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, i
     if (scan) hipLaunchKernelGGL(expert_scan_kernel, dim3(ceil_div(experts, kWave)), dim3(kScanWaves * kWave), 0, stream, s);
     NMT_LAUNCH_CHECK();
   }
-  const dim3 grid(std::max(1, ceil_div(n, kChunk)));
+  s.chunk = kChunk;
+  int groups = ceil_div(n, kChunk);
+  if (whole && d_rows) spread(n, (int64_t)d * row_type_bytes(type), (int64_t)experts * capacity, &s.chunk, &groups);
+  const dim3 grid(std::max(1, groups));
   const size_t lds = sizeof(int32_t) * experts * 3;
   if (whole) {
     if (!d_rows) hipLaunchKernelGGL((expert_dispatch_kernel<void, WHOLE, kWholeThreads>), grid, dim3(kWholeThreads), lds, stream, s, a);
@@ -554,13 +594,15 @@ extern "C" int nmt_op_expert_dispatch(const int32_t* d_expert, int32_t tokens, i
 
 template <typename T, int LANES, bool STREAM>
 static void launch_combine(const RowsArgs& a, hipStream_t stream) {
-  const dim3 grid = grid_of(ceil_div(a.tokens, kThreads / LANES));
+  const dim3 grid = grid_of(ceil_div((int64_t)a.tokens << a.parts_log, kThreads / LANES));
   if (a.k == 1) hipLaunchKernelGGL((expert_combine_kernel<T, LANES, 1, STREAM>), grid, dim3(kThreads), 0, stream, a);
   else if (a.k == 2) hipLaunchKernelGGL((expert_combine_kernel<T, LANES, 2, STREAM>), grid, dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL((expert_combine_kernel<T, LANES, 4, STREAM>), grid, dim3(kThreads), 0, stream, a);
 }
 template <typename T>
-static void launch_combine(const RowsArgs& a, hipStream_t stream) {
+static void launch_combine(RowsArgs a, hipStream_t stream) {
+  if (a.lanes_log > 5)
+    while (((int64_t)a.tokens << a.parts_log) < kFewWaves && (2 * 64 * Row<T>::kVec) << a.parts_log < a.d) ++a.parts_log;
   if (a.lanes_log <= 4) launch_combine<T, 16, false>(a, stream);
   else if (a.lanes_log == 5) launch_combine<T, 32, false>(a, stream);
   else if (large_rows((int64_t)a.tokens * a.k, a.d, sizeof(T))) launch_combine<T, 64, true>(a, stream);
@@ -576,10 +618,15 @@ static void launch_combine_bwd(RowsArgs a, hipStream_t stream) {
   else hipLaunchKernelGGL((expert_combine_bwd_kernel<T, LANES, 4, STREAM>), grid, dim3(kThreads), 0, stream, a);
 }
 template <typename T>
-static void launch_combine_bwd(const RowsArgs& a, hipStream_t stream) {
+static void launch_combine_bwd(RowsArgs a, hipStream_t stream) {
+  const bool large = large_rows((int64_t)a.tokens * a.k, a.d, sizeof(T));
+  if (a.lanes_log > 7 && a.tokens < kFewWaves) {
+    if (a.rows == a.out) a.vectors = a.d / Row<T>::kVec * Row<T>::kVec;  // (no wavefront reads what another has written)
+    return large ? launch_combine_bwd<T, 256, true>(a, stream) : launch_combine_bwd<T, 256, false>(a, stream);
+  }
   if (a.lanes_log <= 4) launch_combine_bwd<T, 16, false>(a, stream);
   else if (a.lanes_log == 5) launch_combine_bwd<T, 32, false>(a, stream);
-  else if (large_rows((int64_t)a.tokens * a.k, a.d, sizeof(T))) launch_combine_bwd<T, 64, true>(a, stream);
+  else if (large) launch_combine_bwd<T, 64, true>(a, stream);
   else launch_combine_bwd<T, 64, false>(a, stream);
 }
 

@@ -462,6 +462,45 @@ def test_tokens_go_to_their_experts_and_back(tokens, k, experts, capacity, d, dt
         assert torch.equal(made[flat[took].long()], drows[flat[took].long()])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,k,experts,capacity,d", [(1, 8, 64, 0, 8192), (1, 1, 2, 0, 2049), (3, 5, 8, 0, 4099), (17, 2, 8, 40, 2057), (2, 64, 9, 0, 4100), (40, 3, 5, 7, 20000),
+                                                         (2200, 1, 7, 0, 2100), (8191, 2, 4, 0, 1111), (8192, 2, 4, 0, 1111), (8192, 1, 4, 2100, 2051)])
+def test_few_tokens_of_wide_rows(tokens, k, experts, capacity, d, dtype):
+    """Several wavefronts take a token; in place too, where rows of no whole number of vectors end in single elements."""
+    test_tokens_go_to_their_experts_and_back(tokens, k, experts, capacity, d, dtype)
+    g = gen(d)
+    ids = choices(tokens, k, experts, d, 0.1)
+    n = experts * capacity if capacity else tokens * k
+    slot, ranges = dispatched(ids, experts, capacity)
+    made, um = guarded(n, d, dtype, torch.randn(n, d, generator=g, device=DEV), d + 1, 1)
+    dout, weights = torch.randn(tokens, d, generator=g, device=DEV).to(dtype), torch.rand(tokens, k, generator=g, device=DEV)
+    first, dweights = torch.full((n, d), GUARD, dtype=dtype, device=DEV), torch.full((tokens, k), GUARD, device=DEV)
+    flat = slot.reshape(-1)
+    took = (flat >= 0).nonzero().reshape(-1)
+    terms = dout.to(D)[took // k] * made.to(D)[flat[took].long()]
+    A.nmt_op_expert_combine_bwd(dout, None, slot, weights, first, None, ranges, capacity)
+    A.nmt_op_expert_combine_bwd(dout, made, slot, weights, made, dweights, ranges, capacity)
+    assert torch.equal(made[flat[took].long()], first[flat[took].long()])
+    dw, size = torch.zeros(tokens * k, dtype=D, device=DEV), torch.zeros(tokens * k, dtype=D, device=DEV)
+    dw[took], size[took] = terms.sum(1), terms.abs().sum(1)
+    within(dweights.reshape(-1), dw, (-(-d // 64) + 64) * U32 * size, "dweights in place")     # (additions in a lane, then across lanes)
+    assert um()
+
+
+@pytest.mark.parametrize("tokens,k,experts,capacity,d", [(8, 2, 64, 512, 1024), (0, 1, 3, 5000, 777), (300, 2, 8, 4000, 100), (1, 1, 1024, 64, 8), (16384, 1, 16, 3000, 64)])
+def test_much_room_for_few_tokens(tokens, k, experts, capacity, d):
+    """Rows that no token took are set to zero by more work-groups than there are choices for."""
+    g = gen(d)
+    ids = choices(tokens, k, experts, 5, 0.1)
+    x = torch.randn(tokens, d, generator=g, device=DEV).half()
+    rows, ur = guarded(experts * capacity, d, F16, torch.full((experts * capacity, d), GUARD, device=DEV), d + 3, 1)
+    slot, ranges = dispatched(ids, experts, capacity, x, rows)
+    want_slot, want_ranges = R.dispatch(ids.cpu(), experts, capacity)
+    assert torch.equal(ranges.cpu(), want_ranges) and torch.equal(slot.cpu(), want_slot)
+    check_rows(rows, x, slot, capacity)
+    assert ur()
+
+
 def test_dropped_choices_weigh_nothing():
     """NaN weights of dropped choices, and NaN in rows that no token took, reach nothing; a token without an expert gets zeros."""
     ids = torch.tensor([[0, -1], [-1, -1], [1, 0], [0, 0]], dtype=torch.int32, device=DEV)
