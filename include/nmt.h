@@ -428,7 +428,7 @@ int nmt_op_gated_norm_bwd(const nmt_gated_norm* a /*host*/, const nmt_gated_norm
  *   capacity == 0: the experts' rows lie back to back; d_rows has tokens * k rows, and those behind the last are left as they were.
  *   capacity  > 0: expert e has the rows [e * capacity, (e + 1) * capacity) of d_rows, so that products of a size the host knows can be
  *                  enqueued; choices beyond them are dropped, and rows without a token are set to zero.
- * d_slot [tokens, k]: the row of every choice, -1 if it was dropped.  d_ranges [experts, 2]: first row and number of rows of every expert.
+ * d_slot [tokens, k]: the row of every choice, -1 if it was dropped (another buffer than d_expert).  d_ranges [experts, 2]: first row and number of rows of every expert.
  * d_x NULL: the lists alone (d_rows is then NULL too).  d_scratch: scratch_ints >= nmt_op_expert_dispatch_scratch int32 elements.
  * k <= 64, experts <= 1024, tokens * k and experts * capacity <= 2^29, d <= 2^20. */
 int64_t nmt_op_expert_dispatch_scratch(int32_t tokens, int32_t k, int32_t experts);
@@ -473,7 +473,8 @@ typedef struct nmt_adamw nmt_adamw;
 /* Bytes of the device table that nmt_adamw_create fills (host only). */
 int64_t nmt_adamw_table_bytes(int32_t n, const nmt_adamw_tensor* tensors /*host*/);
 /* Checks the tensors and writes the table of their pieces to d_table (16-byte aligned), which belongs to the handle until nmt_adamw_destroy.  Waits for the
- * stream, so it cannot be captured.  `tensors` itself is not kept; the buffers it names must stay where they are.  No two tensors of a list overlap. */
+ * stream, so it cannot be captured.  `tensors` itself is not kept; the buffers it names must stay where they are.  A buffer that a step writes
+ * overlaps no other of the list, so no tensor is in it twice; gradients may be shared. */
 int nmt_adamw_create(int32_t n, const nmt_adamw_tensor* tensors /*host*/, int32_t state_bits, int32_t grad_type, int32_t weights_type,
                      void* d_table, int64_t table_bytes, void* stream, nmt_adamw** out);
 void nmt_adamw_destroy(nmt_adamw* plan);

@@ -432,6 +432,7 @@ def nmt_op_dropout_mask(keep, rows, n_cols, drop, stream=None):
 # to the stream of the tensors' device.  A small call is bound by what is done here, so nothing is looked up twice.
 NMT_F16, NMT_BF16, NMT_F32 = 0, 1, 2
 NMT_NORM_LAYER, NMT_NORM_RMS = 0, 1
+_MOST = 2 ** 31 - 1
 _KINDS = {"layer": NMT_NORM_LAYER, "rms": NMT_NORM_RMS}
 _TYPES = {}          # torch dtypes -> type codes; filled with _FLOAT and _INT when torch is there (load())
 _FLOAT = _INT = _torch = _raw_stream = None
@@ -463,6 +464,8 @@ def _rows_of(t, who, what):
     if t is None or t.dim() != 2:
         _refuse(f"{who}: {what} is a two-dimensional tensor")
     rows, d = t.shape
+    if rows > _MOST or d > _MOST:
+        _refuse(f"{who}: {what} is {tuple(t.shape)}: sizes are of 32 bits")
     return rows, d, t.dtype, t.get_device()
 
 
@@ -551,6 +554,7 @@ def nmt_op_gated_norm_fwd(x, y, h, n, stats=None, post=None, gate=None, pre=None
 
 
 def nmt_op_gated_norm_bwd_scratch(rows, d, rows_per_gate=None):
+    _sizes("nmt_op_gated_norm_bwd_scratch", rows, d, rows_per_gate or 0)
     n = load().nmt_op_gated_norm_bwd_scratch(rows, d, rows_per_gate or max(rows, 1))
     if n < 0:
         _refuse(f"nmt_op_gated_norm_bwd_scratch: {rows} rows of {d}, {rows_per_gate} to a gate")
@@ -598,6 +602,7 @@ def nmt_op_gated_norm_bwd(dh, dn, y, h, stats, dx, dy, scratch, post=None, gate=
 
 
 def nmt_op_expert_dispatch_scratch(tokens, k, experts):
+    _sizes("nmt_op_expert_dispatch_scratch", tokens, k, experts)
     n = load().nmt_op_expert_dispatch_scratch(tokens, k, experts)
     if n < 0:
         _check(int(n))
@@ -608,7 +613,15 @@ def _lists(t, who, what):
     if t is None or t.dim() != 2 or t.dtype is not _INT or not t.is_contiguous():
         _refuse(f"{who}: {what} is a contiguous [tokens, k] tensor of int32")
     tokens, k = t.shape
+    if tokens > _MOST or k > _MOST:
+        _refuse(f"{who}: {what} is {tuple(t.shape)}: sizes are of 32 bits")
     return tokens, k, t.get_device()
+
+
+def _sizes(who, *sizes):
+    for n in sizes:
+        if not 0 <= n <= _MOST:
+            _refuse(f"{who}: {n} is no size of 32 bits")
 
 
 def nmt_op_expert_dispatch(expert, experts, capacity, x, rows, slot, ranges, scratch, stream=None):
@@ -617,6 +630,7 @@ def nmt_op_expert_dispatch(expert, experts, capacity, x, rows, slot, ranges, scr
     lib = _lib or load()
     who = "nmt_op_expert_dispatch"
     tokens, k, device = _lists(expert, who, "expert")
+    _sizes(who, experts, capacity)
     d = code = ld_x = ld_rows = 0
     x_ = rows_ = scratch_ = None
     if x is not None and rows is not None:
@@ -651,6 +665,7 @@ def nmt_op_expert_combine_bwd(dout, rows, slot, weights, drows, dweights, ranges
     lib, who = _lib or load(), "nmt_op_expert_combine_bwd"
     tokens, k, device = _lists(slot, who, "slot")
     n, d, dtype, _ = _rows_of(drows, who, "drows")
+    _sizes(who, capacity)
     drows_, ld_drows = _matrix(drows, n, d, dtype, device, "drows")
     dout_, ld_dout = _matrix(dout, tokens, d, dtype, device, "dout")
     rows_, ld_rows = (None, 0) if rows is None else _matrix(rows, n, d, dtype, device, "rows")

@@ -5,6 +5,7 @@
 // gigabyte: 5.2).  Past the caches 303 and 588 us, through them 355 and 657; one block of 256 elements a wavefront, two, four: 318, 303, 312 us.
 #include "common.h"
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -235,6 +236,21 @@ int count_pieces(const char* who, int32_t n, const nmt_adamw_tensor* tensors, in
   NMT_REQUIRE(*pieces < (1 << 24), "%s: more than 2^24 pieces of %d elements", who, kPiece);  // (a grid has less than 2^32 threads)
   return NMT_OK;
 }
+// What a step writes overlaps neither what else it writes nor what it reads.
+struct Range {
+  uintptr_t begin, end;
+  bool written;
+};
+bool overlap(std::vector<Range>& ranges) {
+  std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  uintptr_t end = 0, written_end = 0;
+  for (const Range& r : ranges) {
+    if (r.begin < (r.written ? end : written_end)) return true;
+    end = std::max(end, r.end);
+    if (r.written) written_end = std::max(written_end, r.end);
+  }
+  return false;
+}
 bool type_ok(int t) { return t == NMT_F16 || t == NMT_BF16 || t == NMT_F32; }
 template <typename T>
 bool aligned_as(const void* p, T size) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)size == 0; }
@@ -278,6 +294,19 @@ extern "C" int nmt_adamw_create(int32_t n, const nmt_adamw_tensor* tensors, int3
   }
   NMT_REQUIRE(aligned16(d_table), "%s: the table must be 16-byte aligned", who);
   try {
+    std::vector<Range> ranges;
+    ranges.reserve(7 * (size_t)n);
+    for (int32_t i = 0; i < n; ++i) {
+      const nmt_adamw_tensor& t = tensors[i];
+      auto add = [&](const void* p, int64_t bytes, bool written) {
+        if (p && bytes) ranges.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes, written});
+      };
+      const int64_t scales = (t.n + kStateBlock - 1) / kStateBlock * 4;
+      add(t.d_master, 4 * t.n, true), add(t.d_m, t.n * (state_bits / 8), true), add(t.d_v, t.n * (state_bits / 8), true);
+      add(t.d_m_scale, scales, true), add(t.d_v_scale, scales, true);
+      add(t.d_weights, t.n * size(weights_type), true), add(t.d_grad, t.n * size(grad_type), false);
+    }
+    NMT_REQUIRE(!overlap(ranges), "%s: what a step writes overlaps another buffer of the list", who);
     std::vector<Piece> host;
     host.reserve((size_t)pieces);
     for (int32_t i = 0; i < n; ++i) {
@@ -313,9 +342,9 @@ extern "C" int nmt_adamw_step(const nmt_adamw* plan, double lr, double beta1, do
   const char* who = "nmt_adamw_step";
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   NMT_REQUIRE(plan, "%s: null argument", who);
-  NMT_REQUIRE(std::isfinite(lr) && lr >= 0, "%s: the learning rate must be finite and not negative", who);
+  NMT_REQUIRE(std::isfinite((float)lr) && lr >= 0, "%s: the learning rate must be finite and not negative", who);
   NMT_REQUIRE(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1, "%s: beta outside [0, 1)", who);
-  NMT_REQUIRE(std::isfinite(eps) && eps > 0 && t >= 1 && std::isfinite(grad_scale), "%s: bad eps, t or grad_scale", who);
+  NMT_REQUIRE(std::isfinite((float)eps) && (float)eps > 0 && t >= 1 && std::isfinite(grad_scale), "%s: bad eps, t or grad_scale", who);
   if (plan->pieces == 0) return NMT_OK;
   const Hyper h = {(float)lr, (float)beta1, (float)(1 - beta1), (float)beta2, (float)(1 - beta2), (float)eps,
                    (float)(1 / (1 - pow(beta1, (double)t))), (float)(1 / (1 - pow(beta2, (double)t))), grad_scale};

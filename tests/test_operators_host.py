@@ -197,3 +197,51 @@ def test_adamw_binding_refuses(change):
     with pytest.raises(A.NmtError) as e:
         A.nmt_adamw_create([t], torch.zeros(1 << 16, dtype=torch.uint8))
     assert e.value.code == A.NMT_EINVAL
+
+
+def far(n, d, dtype=torch.float16):
+    """A tensor of a size that is no int32 and of no memory."""
+    return torch.zeros(1, 1, dtype=dtype).expand(n, d)
+
+
+def test_sizes_that_32_bits_do_not_hold_are_refused():
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    big = 2 ** 32 + 4
+    for call in (lambda: A.nmt_op_gated_norm_fwd(far(big, 16), far(big, 16), None, far(big, 16), pre=(rows(1, 16), None)),
+                 lambda: A.nmt_op_gated_norm_bwd(None, None, None, None, None, far(big, 16), None, None),
+                 lambda: A.nmt_op_gated_norm_bwd_scratch(big, 16), lambda: A.nmt_op_gated_norm_bwd_scratch(4, big), lambda: A.nmt_op_gated_norm_bwd_scratch(4, 16, big),
+                 lambda: A.nmt_op_expert_dispatch_scratch(big, 2, 8), lambda: A.nmt_op_expert_dispatch_scratch(4, 2, big),
+                 lambda: A.nmt_op_expert_dispatch(i(4, 2), 8, 2 ** 32, None, None, i(4, 2), i(8, 2), i(4096)),
+                 lambda: A.nmt_op_expert_combine(far(big, 16), i(4, 2), None, rows(4, 16)),
+                 lambda: A.nmt_op_expert_combine_bwd(rows(4, 16), None, i(4, 2), None, far(big, 16), None),
+                 lambda: A.nmt_op_expert_combine_bwd(rows(4, 16), None, i(4, 2), None, rows(8, 16), None, i(8, 2), 2 ** 32 + 1)):
+        with pytest.raises(A.NmtError, match="32 bits"):
+            call()
+
+
+def test_slots_in_place_of_the_choices_are_refused():
+    """Every work-group of a sort reads all choices."""
+    refused(A.load().nmt_op_expert_dispatch(P, 4, 2, 8, 0, None, 0, 0, 0, None, 0, P, P + 4096, P + 8192, 1 << 20, None), says="in place")
+
+
+AT = dict(d_master=P, d_m=P + 0x1000, d_v=P + 0x2000, d_grad=P + 0x3000, d_weights=P + 0x4000)      # of a tensor of 100 elements
+
+
+@pytest.mark.parametrize("other", [{}, dict(d_master=P + 396), dict(d_m=P + 0x1000), dict(d_v=P + 0x3000 + 196), dict(d_weights=P + 0x4000 + 198), dict(d_grad=P + 398),
+                                   dict(d_weights=P + 0x8000 + 100), dict(d_m=P - 396)])
+def test_adamw_refuses_what_it_would_write_twice(other):
+    """One tensor twice, or buffers that share a few bytes: what a step leaves there would depend on an order that nothing fixes."""
+    second = {f: p + 0x8000 for f, p in AT.items()}
+    second.update(other or AT)
+    lib, arr, out = A.load(), (B.nmt_adamw_tensor * 2)(tensor_of(**AT), tensor_of(**second)), C.c_void_p()
+    for pair in (arr, (B.nmt_adamw_tensor * 2)(arr[1], arr[0])):
+        refused(lib.nmt_adamw_create(2, pair, 32, A.NMT_F16, A.NMT_F16, P << 8, 1 << 20, None, C.byref(out)), says="overlaps")
+        assert not out.value
+
+
+def test_adamw_step_refuses_what_32_bits_make_zero_or_infinite():
+    lib, out = A.load(), C.c_void_p()
+    assert lib.nmt_adamw_create(0, None, 32, 0, 0, None, 0, None, C.byref(out)) == A.NMT_OK
+    refused(lib.nmt_adamw_step(out, 1e39, 0.9, 0.98, 1e-8, 1, 1.0, None, None), says="learning rate")
+    refused(lib.nmt_adamw_step(out, 1e-3, 0.9, 0.98, 1e-50, 1, 1.0, None, None), says="eps")
+    lib.nmt_adamw_destroy(out)
