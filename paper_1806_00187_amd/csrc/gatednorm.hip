@@ -4,8 +4,8 @@
 // reads y, h and the gradients at h and n and writes those at x and y.  A row is held in registers by 8 to 64 lanes (up to 64, 128, 256, 512 columns) or by
 // several wavefronts, each lane's share of it 16 bytes at a time; the next row is in flight while one is worked on.
 // Forward 52701 x 1024 bf16: 73 us, 5.9 TB/s (a copy of a gigabyte: 5.2).  Backward 26001 x 1024 fp16: 74 us, 4.3 TB/s, of which the sums over work-groups take 5;
-// a wavefront per SIMD has its registers full of column sums and two rows.  Backward, fp32 rows of 4097 to 8192 columns do without the second row (3001 x 5000: 120 us for 360 MB), and
-// rows of more than 8192 spill (2001 x 9000 bf16: 316 us for 216 MB).
+// a wavefront per SIMD has its registers full of column sums and two rows.  Backward, fp32 rows of 4097 to 8192 columns do without the second row (3001 x 5000: 100 us for 360 MB), and so
+// do rows of more than 8192, whose shifts' sums are in LDS (2001 x 9000 bf16: 85 us for 216 MB, 1101 x 16384 bf16: 103, fp32, which spill: 209 for 433).
 #include "rowtypes.h"
 
 #include <algorithm>
@@ -289,11 +289,16 @@ __global__ void __launch_bounds__(S::kThreads) gated_norm_fwd_kernel(const NormA
 // rows end it is written if all of them were this worker's, and else left as a partial sum, of which a worker has two at most (of the gate it
 // begins in, if that began before it, and of the one it ends in).
 template <typename S, bool GROUPED, bool SHIFTS>
-__global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 : 1) gated_norm_bwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(S::kThreads, S::kWaves > 12 ? 4 : S::kWaves > 8 ? 3 : S::kE < 16 || S::kWaves == 8 ? 2 : 1) gated_norm_bwd_kernel(const NormArgs a) {
   constexpr int E = S::kE, LANES = S::kLanes, WAVES = S::kWaves, SUMS = SHIFTS ? 4 : 2;
   using V = Share<S>;
   __shared__ float red[4][WAVES];
   __shared__ __attribute__((aligned(16))) float sums[S::kRows > 1 ? SUMS : 1][S::kRows > 1 ? S::kRows * S::kCover : 1];
+  // Twelve wavefronts have 168 registers a lane, sixteen 128: the shifts' sums, which are added up without a product, are in LDS (with all sums in the registers of eight
+  // 2001 x 9000 bf16 took 316 us instead of 85, 1101 x 16384 233 instead of 103; sixteen wavefronts for the former 113).
+  constexpr bool WIDE = WAVES > 8;
+  constexpr int HELD = WIDE ? 2 : SUMS;
+  __shared__ float4 outside[WIDE && SHIFTS ? 2 * E / 4 : 1][WIDE && SHIFTS ? S::kThreads : 1];
   touch(a);
   const int d = a.d;
   const Columns<S> c(d);
@@ -312,11 +317,24 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
     if (a.dn) pre.load(a.pre_gain, 0, c);
   };
   // Where the column sums and a row fill the registers by themselves gains are fetched where they are used, row after row.
-  constexpr bool AHEAD = E * sizeof(typename S::type) <= 32;
+  constexpr bool LATE = WIDE && sizeof(typename S::type) == 4;  // y is not asked for before it is needed, and dx written before (1101 x 16384 275 -> 209 us)
+  constexpr bool AHEAD = !WIDE && E * sizeof(typename S::type) <= 32;
   if (AHEAD) vectors_after(), vectors_before();
-  float sum[SUMS][E], gate_sum[GROUPED ? E : 1];
+  float sum[HELD][E], gate_sum[GROUPED ? E : 1];
 #pragma unroll
-  for (int q = 0; q < SUMS; ++q) fill(sum[q], 0.f);
+  for (int q = 0; q < HELD; ++q) fill(sum[q], 0.f);
+  if constexpr (WIDE && SHIFTS)
+#pragma unroll
+    for (int i = 0; i < 2 * E / 4; ++i) outside[i][threadIdx.x] = float4{0.f, 0.f, 0.f, 0.f};
+  auto add_outside = [&](int q, auto f) {  // (a lane's own)
+    if constexpr (WIDE && SHIFTS)
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) {
+        float4 t = outside[q * (E / 4) + i][threadIdx.x];
+        t.x += f(4 * i), t.y += f(4 * i + 1), t.z += f(4 * i + 2), t.w += f(4 * i + 3);
+        outside[q * (E / 4) + i][threadIdx.x] = t;
+      }
+  };
   GateRows gates;
   int64_t gate_row = -1;  // of the rows at hand
   bool other_gate = false;
@@ -327,7 +345,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
       next_dn.load(a.dn, row * a.ld_dn, c);
     }
     if (a.dh) next_dh.load(a.dh, row * a.ld_dh, c);
-    if (a.y) next_y.load(a.y, row * a.ld_y, c);
+    if (a.y && !LATE) next_y.load(a.y, row * a.ld_y, c);
     if (GROUPED) {
       other_gate = gates.next(row, a.rows_per_gate);
       if (other_gate) next_gate.load(a.gate, gates.row * d, c);
@@ -350,10 +368,17 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
   if (AHEAD && begin < end) ask(begin);
   for (int64_t row = begin; row < end; ++row) {
     if (!AHEAD) {
+      next_dh.fill(0.f), next_dn.fill(0.f), next_h.fill(0.f), next_y.fill(0.f);  // (nothing of a row is kept for the next one, there or not)
+      pre.fill(1.f), gain.fill(1.f), shift.fill(0.f);
+      if (!GROUPED) gate.fill(1.f);
       ask(row);
       vectors_before();
     }
-    const V dh = next_dh, dn = next_dn, h = next_h, y = next_y;
+    V dh = next_dh, dn = next_dn, h = next_h, y = next_y;
+    // Where registers are short nothing formed from these is kept from one use to the next: it is formed again (3001 x 5000 fp32 119 -> 100 us).
+    auto anew = [&](auto&... v) {
+      if constexpr (!AHEAD) (v.arrive(), ...);
+    };
     const float4_any st = next_st;
     if (GROUPED && other_gate) {
       close_gate(row);
@@ -370,10 +395,14 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         sum[0][e] += dn(e) * (h(e) * rstd + off);
-        if (SHIFTS) sum[SUMS - 2][e] += dn(e);
+        if (SHIFTS && !WIDE) sum[HELD - 2][e] += dn(e);
       }
+      add_outside(0, [&](int e) { return dn(e); });
+      anew(dn, h);
       const float m1 = a.kind == NMT_NORM_LAYER ? row_sum<LANES, WAVES>(own_sum<S>(c, [&](int e) { return dn(e) * pre(e); }), red[0]) * inv_d : 0.f;
+      anew(dn, pre);
       const float m2 = row_sum<LANES, WAVES>(own_sum<S>(c, [&](int e) { return dn(e) * pre(e) * (h(e) * rstd + off); }), red[1]) * inv_d;
+      anew(dn, h, pre);
 #pragma unroll
       for (int e = 0; e < E; ++e) g[e] += rstd * (dn(e) * pre(e) - m1 - (h(e) * rstd + off) * m2);
     }
@@ -384,6 +413,12 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
       for (int e = 0; e < E; ++e) out[e] = a.resid_scale * g[e];
       out_x.set(out);
     }
+    if (LATE) {  // (a wait as the one below: dx may lie where dh does)
+      out_x.arrive();
+      __syncthreads();
+      out_x.store(a.dx, row * a.ld_dx, c);
+      if (a.y) y.load(a.y, row * a.ld_y, c);
+    }
     if (!AHEAD) vectors_after();
     if (a.y) {
       const float rstd = st[1], off = -st[0] * st[1];
@@ -393,12 +428,19 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
         if constexpr (GROUPED) gate_sum[e] += g[e] * (SHIFTS ? yhat * gain(e) + shift(e) : yhat * gain(e));
         const float dz = gate(e) * g[e], at = GROUPED ? dz : g[e];
         sum[1][e] += at * yhat;
-        if (SHIFTS) sum[SUMS - 1][e] += at;
-        g[e] = dz * gain(e);
+        if (SHIFTS && !WIDE) sum[HELD - 1][e] += at;
+        if (!WIDE) g[e] = dz * gain(e);
+      }
+      if constexpr (WIDE) {
+        add_outside(1, [&](int e) { return GROUPED ? gate(e) * g[e] : g[e]; });
+#pragma unroll
+        for (int e = 0; e < E; ++e) g[e] = gate(e) * g[e] * gain(e);
       }
       if (a.post_gain) {
+        anew(y);
         const float m3 = a.kind == NMT_NORM_LAYER ? row_sum<LANES, WAVES>(own_sum<S>(c, [&](int e) { return g[e]; }), red[2]) * inv_d : 0.f;
         const float m4 = row_sum<LANES, WAVES>(own_sum<S>(c, [&](int e) { return g[e] * (y(e) * rstd + off); }), red[3]) * inv_d;
+        anew(y);
 #pragma unroll
         for (int e = 0; e < E; ++e) g[e] = rstd * (g[e] - m3 - (y(e) * rstd + off) * m4);
       }
@@ -411,11 +453,11 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
       asm volatile("" : "+v"(next_st));
     }
     if (WAVES > 1) {  // the sums' places are used again; and dx may lie where dh does, dy where dn, of which lanes of two wavefronts may have loaded the same
-      out_x.arrive();
+      if (!LATE) out_x.arrive();
       if (a.y) out_y.arrive();
       __syncthreads();
     }
-    out_x.store(a.dx, row * a.ld_dx, c);
+    if (!LATE) out_x.store(a.dx, row * a.ld_dx, c);
     if (a.y) out_y.store(a.dy, row * a.ld_dy, c);
   }
   close_gate(end);
@@ -423,7 +465,17 @@ __global__ void __launch_bounds__(S::kThreads, S::kE < 16 || S::kWaves == 8 ? 2 
   float* out = a.partial + (int64_t)blockIdx.x * SUMS * a.pitch;
   if constexpr (S::kRows == 1) {
 #pragma unroll
-    for (int q = 0; q < SUMS; ++q) st_sums<S>(out + (int64_t)q * a.pitch, c, sum[q]);
+    for (int q = 0; q < HELD; ++q) st_sums<S>(out + (int64_t)q * a.pitch, c, sum[q]);
+    if constexpr (HELD < SUMS)
+#pragma unroll
+      for (int q = 0; q < SUMS - HELD; ++q) {
+#pragma unroll
+        for (int i = 0; i < E / 4; ++i) {
+          const float4 t = outside[q * (E / 4) + i][threadIdx.x];
+          sum[0][4 * i] = t.x, sum[0][4 * i + 1] = t.y, sum[0][4 * i + 2] = t.z, sum[0][4 * i + 3] = t.w;
+        }
+        st_sums<S>(out + (int64_t)(HELD + q) * a.pitch, c, sum[0]);
+      }
   } else {
 #pragma unroll
     for (int q = 0; q < SUMS; ++q) st_sums<S>(sums[q] + S::worker() * S::kCover, c, sum[q]);
@@ -507,15 +559,16 @@ __global__ void __launch_bounds__(kSumCols* kSumLanes) gated_norm_sums_kernel(co
 }
 
 // What a row of d columns is held by: -1: 16 lanes of one column (of less than a vector), 0 to 3: 8, 16, 32, 64 lanes of 8, 4 to 7: 2 to 16 wavefronts of 8 columns a lane, or, backward and
-// 16-bit, 1 to 8 of 16 (fp32: 8 of 16 instead of 16 of 8), 8: 16 of 16, backward 8 of 32.
+// 16-bit, 1 to 8 of 16 (fp32: 8 of 16 instead of 16 of 8), 8: 16 of 16, backward 12;
+// 9, more than 12288 columns: 16 of 16.
 enum { kForward, kBackward, kBackwardWide };
 int shape_of(int d, int type) {
   if (d < 16 / row_type_bytes(type)) return -1;
   int s = 0;
   for (int most = 64; s < 8 && d > most; ++s) most *= 2;
-  return s;
+  return d > 12288 ? 9 : s;
 }
-int waves_of_row(int shape, int form) { return shape <= 3 ? 1 : form == kForward ? std::min(16, 2 << (shape - 4)) : std::min(8, (form == kBackward ? 1 : 2) << (shape - 4)); }
+int waves_of_row(int shape, int form) { return shape <= 3 ? 1 : shape == 9 ? 16 : shape == 8 ? (form == kForward ? 16 : 12) : form == kForward ? std::min(16, 2 << (shape - 4)) : std::min(8, (form == kBackward ? 1 : 2) << (shape - 4)); }
 int workers_of(int shape, int form) { return shape < 0 ? 16 : shape <= 3 ? 32 >> shape : waves_of_row(shape, form) == 1 ? 4 : 1; }  // of a work-group
 int backward_form(int type) { return type == NMT_F32 ? kBackwardWide : kBackward; }
 
@@ -577,7 +630,8 @@ int64_t scratch_floats(int rows, int d, int rows_per_gate) {
     case 5: NORM_LAUNCH(KERNEL, T, v, 64, 2 * w, __VA_ARGS__) break;                                                     \
     case 6: NORM_LAUNCH(KERNEL, T, v, 64, 4 * w, __VA_ARGS__) break;                                                     \
     case 7: NORM_LAUNCH(KERNEL, T, f ? v8 : 2 * v8, 64, f ? 16 : 8, __VA_ARGS__) break;                                  \
-    default: NORM_LAUNCH(KERNEL, T, f ? 2 * v8 : 4 * v8, 64, f ? 16 : 8, __VA_ARGS__)                                    \
+    case 8: NORM_LAUNCH(KERNEL, T, 2 * v8, 64, f ? 16 : 12, __VA_ARGS__) break;                                          \
+    default: NORM_LAUNCH(KERNEL, T, 2 * v8, 64, 16, __VA_ARGS__)                                                           \
   }
 
 template <typename T>

@@ -249,6 +249,17 @@ def test_gated_norm_backward_in_place_of_its_inputs(d, parts):
     check_backward(300, d, F32, "layer", 9, 0.9, parts, d, in_place=True)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [8193, 10007, 12288, 12289, 14000, 16384])
+def test_gated_norm_of_very_wide_rows(d, dtype):
+    """Some of the column sums are in LDS; more rows than work-groups, gates that two of those share, in place and apart."""
+    for parts, per, kind, place in (("yhpgns", 700, "layer", False), ("yhpgns", 7, "rms", True), ("yhpgn", None, "layer", True), ("hns", None, "rms", False),
+                                    ("yhps", None, "layer", False), ("yhg", 3, "rms", True)):
+        check_backward(530, d, dtype, kind, per, 0.9, parts, d, in_place=place)
+    check_backward(5, d, dtype, "layer", 2, 1.0, "yhpgns", 1, d + 3, 1)
+    check_forward(300, d, dtype, "layer", 9, 0.9, "ypgns", d, in_place=True)
+
+
 def test_gated_norm_scratch_serves_fewer_rows():
     for d in (64, 512, 777, 1024, 2048, 8192):
         for per in (None, 7):
