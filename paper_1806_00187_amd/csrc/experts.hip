@@ -2,7 +2,7 @@
 // sum of a token's rows on the way back, and the gradients.  Bound by memory, the rows that are read and written once, and for few tokens by launches: up to
 // kWhole choices the dispatch is one launch, in which every work-group counts all choices for itself; beyond that counts of segments and their sums over the segments before
 // each are launches of their own (3 us each), and so are the rows.
-// 105402 rows of 1024 bf16 to 64 experts and back: 123 us, 5.3 TB/s (a copy of a gigabyte: 5.2); 7168 of 512 fp16 to 16 experts: 11.6 us.
+// 105402 rows of 1024 bf16 to 64 experts and back: 123 us, 5.3 TB/s (a copy of a gigabyte: 5.2); 7168 of 512 fp16 to 16 experts with room for 8960: 11.2 us.
 #include "rowtypes.h"
 
 #include <algorithm>
