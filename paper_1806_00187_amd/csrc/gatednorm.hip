@@ -575,7 +575,7 @@ int backward_form(int type) { return type == NMT_F32 ? kBackwardWide : kBackward
 // Forward: two rows a worker, so that the second's loads are under way while the first is worked on and gains are fetched half as often, if that still makes
 // kFwdWaves wavefronts, and one otherwise (26001 x 1024 fp16, one row, two, three: 48, 43, 45 us; 2001 x 8000 fp32, one, two: 68, 61).
 // Backward: every work-group leaves a row of column sums, so no more of them than run side by side (kBwdWaves: a wavefront per SIMD with its
-// registers full; 1280, 2048 and 3072 cost 26001 x 1024 fp16 90, 75 and 78 us instead of 74, and 3584 x 512 15, 14 and 15 instead of 13).
+// registers full; 1280 and 2048 cost 26001 x 1024 fp16 90 and 75 us instead of 74, and 3584 x 512 15 and 14 instead of 13).
 constexpr int kFwdWaves = 4096, kBwdWaves = 1024;
 int bwd_groups(int waves) { return std::max(kBwdWaves / waves, device_info().cus); }  // (of wavefronts for a row: one work-group to a compute unit)
 constexpr int64_t kStreamFrom = 64 << 20;  // bytes of a result
