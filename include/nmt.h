@@ -389,7 +389,7 @@ int nmt_op_dropout_mask(uint8_t* d_keep, int32_t rows, int32_t n_cols, const nmt
  * y: the block's output, x: the residual stream before it, n: the next block's input.  n is formed from h before h is
  * rounded.  d_gate NULL: 1; otherwise row r takes row r / rows_per_gate of d_gate [ceil(rows / rows_per_gate), d] (rows_per_gate >= rows: one
  * gate for all; 1: a gate for every element).  Shifts may be NULL (0).  Gains, shifts and gates are contiguous, of the rows' type.
- * d_y NULL: the norm before the first block, n = norm(x) * pre_gain + pre_shift; d_h, d_post_gain, d_gate are then NULL too.
+ * d_y NULL: the norm before the first block, n = norm(x) * pre_gain + pre_shift; d_h, d_post_gain, d_gate are then NULL too, and resid_scale is 1.
  * d_stats: fp32 [rows, 4] = mean and 1 / sqrt(.) of y, then of h (0 and 1 where there is no norm; RMS: mean 0), for the backward call; may be
  * NULL.  d_h may be d_x, and d_n may be d_y, with the same distance between rows; otherwise what is written overlaps nothing else.
  * d <= 16384, rows < 2^31 - 65536. */
@@ -406,7 +406,8 @@ typedef struct nmt_gated_norm {
 int nmt_op_gated_norm_fwd(const nmt_gated_norm* a /*host*/, void* stream);
 
 /* Backward of the above.  Read from `a`: rows, d, type, kind, resid_scale, rows_per_gate, the gains, shifts and gate, d_y, d_h (without d_y: the x
- * of the forward call), ld_y, ld_h and d_stats; its x, n and eps are not used.  d_dh: gradient that reaches h from elsewhere (NULL: none);
+ * of the forward call), ld_y, ld_h and d_stats; its x, n and eps are not used.  Without d_y resid_scale is 1 for the gradient at the forward call's x; a caller that made this x
+ * by itself as some factor times a tensor of its own gives the factor, and d_dx is the gradient at that tensor.  d_dh: gradient that reaches h from elsewhere (NULL: none);
  * d_dn: gradient at n (NULL: none); one of the two is there, and d_pre_gain with d_dn.  Written: d_dx (resid_scale times the gradient at h) and, with d_y, d_dy, of the
  * rows' type, and the gradients of gains, shifts and gate (sums over the rows in fp32, rounded once to the rows' type; each may be NULL).  d_dx may be d_dh and
  * d_dy may be d_dn with the same distance between rows.

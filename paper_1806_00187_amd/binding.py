@@ -535,7 +535,8 @@ def _norm_parts(a, rows, d, dtype, device, post, gate, pre, kind, rows_per_gate,
 
 def nmt_op_gated_norm_fwd(x, y, h, n, stats=None, post=None, gate=None, pre=None, kind="layer", rows_per_gate=None, resid_scale=1.0, eps=1e-5,
                           stream=None):
-    """h = resid_scale * x + gate * post(y), n = pre(h).  post, pre: (gain, shift or None) or None; rows_per_gate None: one gate for all rows."""
+    """h = resid_scale * x + gate * post(y), n = pre(h).  post, pre: (gain, shift or None) or None; rows_per_gate None: one gate for all rows.
+    y None: n = pre(x); resid_scale is then 1."""
     lib = _lib or load()
     rows, d, dtype, device = _rows_of(x, "nmt_op_gated_norm_fwd", "x")
     a = nmt_gated_norm()
@@ -563,7 +564,7 @@ def nmt_op_gated_norm_bwd_scratch(rows, d, rows_per_gate=None):
 
 def nmt_op_gated_norm_bwd(dh, dn, y, h, stats, dx, dy, scratch, post=None, gate=None, pre=None, dpost=None, dgate=None, dpre=None, kind="layer",
                           rows_per_gate=None, resid_scale=1.0, stream=None):
-    """Gradients of nmt_op_gated_norm_fwd (h: its x where there is no y).  dpost, dpre: (of the gain, of the shift or None) or None."""
+    """Gradients of nmt_op_gated_norm_fwd (h: its x where there is no y, and resid_scale what the caller made that x with, if anything).  dpost, dpre: (of the gain, of the shift or None) or None."""
     lib = _lib or load()
     rows, d, dtype, device = _rows_of(dx, "nmt_op_gated_norm_bwd", "dx")
     a, g = nmt_gated_norm(), nmt_gated_norm_grad()

@@ -710,6 +710,7 @@ extern "C" int nmt_op_gated_norm_fwd(const nmt_gated_norm* a, void* stream_) {
   NMT_REQUIRE(!a->d_pre_shift || a->d_pre_gain, "%s: a shift before the next block needs a gain", who);
   NMT_REQUIRE(!a->d_n == !a->d_pre_gain, "%s: the next block's input and its gain belong together", who);
   NMT_REQUIRE(a->d_y ? a->d_h != nullptr : !a->d_h && a->d_n, "%s: with a block's output the sum is written, without one the norm alone", who);
+  NMT_REQUIRE(a->d_y || a->resid_scale == 1.f, "%s: without a block's output nothing is scaled: resid_scale is 1", who);
   NMT_REQUIRE(a->d_x, "%s: null pointer", who);
   NORM_ROWS(a->d_x, a->ld_x, "x");
   NORM_ROWS(a->d_y, a->ld_y, "y");

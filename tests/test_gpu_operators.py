@@ -298,6 +298,34 @@ def test_gated_norm_gradients_are_the_differences_of_its_values(kind):
         assert abs(slope - want) <= 2e-3 * float(out[k].norm() * way[k].norm()) / way[k].numel() ** 0.5 + 2e-3, (k, slope, want)
 
 
+def norm_alone(x, a, dtype, kind, s):
+    """Gradient at x of h = a x and n = pre(h), from the library: the caller forms h, which is a product by a power of two and exact."""
+    h = a * x
+    n, stats, dx = torch.empty_like(h), torch.empty(*h.shape[:1], 4, device=DEV), torch.empty_like(h)
+    A.nmt_op_gated_norm_fwd(h, None, None, n, stats, pre=s["pre"], kind=kind)
+    scratch = torch.empty(A.nmt_op_gated_norm_bwd_scratch(*h.shape), device=DEV)
+    A.nmt_op_gated_norm_bwd(s["dh"], s["dn"], None, h, stats, dx, None, scratch, pre=s["pre"], kind=kind, resid_scale=a)
+    return dx
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("d", [64, 777, 2056, 9000])
+def test_gradient_of_a_norm_without_a_block(d, kind, dtype):
+    """Against the derivative, in 64 bits, of the plain form.  The statistics are the forward call's, off by up to 64 U32 of a row's terms over its deviation: once in the factor
+    of all terms, twice in the normalised values; with the 64 U32 of the backward pass itself 256 U32 of the magnitudes."""
+    s = norm_inputs(37, d, dtype, kind, None, d)
+    for a in (1.0, 2.0):
+        X = s["x"].to(D).requires_grad_()
+        H, N = R.gated_norm(a * X, pre=wide(s["pre"]), kind=kind)
+        ((H * s["dh"].to(D)).sum() + (N * s["dn"].to(D)).sum()).backward()
+        H, t = H.detach(), (s["dn"].to(D) * s["pre"][0].to(D)).abs()
+        hs, r = row_terms(H, kind), R.norm(H, kind, 1e-5)[2]
+        mean = lambda v: v.mean(1, keepdim=True)
+        size = s["dh"].to(D).abs() + r * hs * (t + mean(t) * (1 + hs) + hs * mean(t * hs))
+        within(norm_alone(s["x"], a, dtype, kind, s), X.grad, half_step(dtype) * X.grad.abs() + 256 * U32 * a * size, f"dx, {a} x")
+
+
 def test_gated_norm_keeps_rows_apart():
     """Infinities and NaN in one row reach that row's outputs alone."""
     s = norm_inputs(40, 512, F16, "layer", None, 2)

@@ -245,3 +245,9 @@ def test_adamw_step_refuses_what_32_bits_make_zero_or_infinite():
     refused(lib.nmt_adamw_step(out, 1e39, 0.9, 0.98, 1e-8, 1, 1.0, None, None), says="learning rate")
     refused(lib.nmt_adamw_step(out, 1e-3, 0.9, 0.98, 1e-50, 1, 1.0, None, None), says="eps")
     lib.nmt_adamw_destroy(out)
+
+
+def test_the_norm_before_the_first_block_has_no_residual_scale():
+    """Without a block's output h is x itself: a scale that the forward call left out and the backward call put into dx would be no gradient of it."""
+    alone = dict(d_y=None, d_post_gain=None, d_post_shift=None, d_gate=None, d_h=None, resid_scale=0.9)
+    refused(A.load().nmt_op_gated_norm_fwd(C.byref(block(**alone)), None), says="resid_scale")
