@@ -431,7 +431,7 @@ def nmt_op_dropout_mask(keep, rows, n_cols, drop, stream=None):
 # These take sizes, types and distances between rows from their tensors and refuse tensors that do not fit each other; the call goes
 # to the stream of the tensors' device.  A small call is bound by what is done here, so nothing is looked up twice.
 NMT_F16, NMT_BF16, NMT_F32 = 0, 1, 2
-NMT_NORM_LAYER, NMT_NORM_RMS = 0, 1
+NMT_NORM_LAYER, NMT_NORM_RMS, NMT_ONE_GATE = 0, 1, 2 ** 31 - 1
 _MOST = 2 ** 31 - 1
 _KINDS = {"layer": NMT_NORM_LAYER, "rms": NMT_NORM_RMS}
 _TYPES = {}          # torch dtypes -> type codes; filled with _FLOAT and _INT when torch is there (load())
@@ -506,8 +506,10 @@ def _call(fn, device, stream, *args, out=None):
 
 def _gates(gate, rows, rows_per_gate, who):
     """(rows of the gate, rows_per_gate)"""
+    if rows == 0:       # (no gates, or the one that all rows share: the tensor says which)
+        return (0, 1) if gate.numel() == 0 else (1, NMT_ONE_GATE)
     if rows_per_gate is None or rows_per_gate >= rows:
-        return 1, max(rows, 1)
+        return 1, rows
     if rows_per_gate < 1:
         _refuse(f"{who}: rows_per_gate must be at least 1")
     return -(-rows // rows_per_gate), rows_per_gate

@@ -738,13 +738,13 @@ extern "C" int nmt_op_gated_norm_bwd(const nmt_gated_norm* a, const nmt_gated_no
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   if (const int rc = check_common(a, who); rc != NMT_OK) return rc;
   NMT_REQUIRE(g, "%s: null argument", who);
-  const bool sums = g->d_dpost_gain || g->d_dpost_shift || g->d_dgate || g->d_dpre_gain || g->d_dpre_shift;
-  if (a->rows == 0) {  // (sums over no rows)
-    if (!sums) return NMT_OK;
+  if (a->rows == 0) {  // (sums over no rows; of gates there are none then but the one that all rows share)
     NormArgs k = {};
     k.d = a->d, k.sums = 4;
-    k.dpost_gain = g->d_dpost_gain, k.dpost_shift = g->d_dpost_shift, k.dgate = g->d_dgate;
+    k.dpost_gain = g->d_dpost_gain, k.dpost_shift = g->d_dpost_shift;
+    k.dgate = a->d_gate && a->rows_per_gate == NMT_ONE_GATE ? g->d_dgate : nullptr;
     k.dpre_gain = g->d_dpre_gain, k.dpre_shift = g->d_dpre_shift;
+    if (!k.dpost_gain && !k.dpost_shift && !k.dgate && !k.dpre_gain && !k.dpre_shift) return NMT_OK;
     return launch_sums(k, a->type, false, stream);
   }
   if (const int rc = check_block(a, who); rc != NMT_OK) return rc;
@@ -783,5 +783,6 @@ extern "C" int nmt_op_gated_norm_bwd(const nmt_gated_norm* a, const nmt_gated_no
   else if (a->type == NMT_BF16) launch_bwd<bf16_t>(k, grid, shape, grouped, stream);
   else launch_bwd<float>(k, grid, shape, grouped, stream);
   NMT_LAUNCH_CHECK();
+  const bool sums = g->d_dpost_gain || g->d_dpost_shift || g->d_dgate || g->d_dpre_gain || g->d_dpre_shift;
   return sums ? launch_sums(k, a->type, grouped, stream) : NMT_OK;
 }

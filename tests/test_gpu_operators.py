@@ -369,6 +369,20 @@ def test_gated_norm_of_no_rows_leaves_zero_gradients():
     assert all((x == 0).all() for x in v) and (dgate == 0).all()
 
 
+@pytest.mark.parametrize("per,gates", [(1, 0), (27, 0), (27, 1), (None, 1), (None, 0)])
+def test_gated_norm_of_no_rows_leaves_what_lies_behind_its_gates(per, gates):
+    """The gradient of no gates is an empty stretch of a larger buffer; that of the one that all rows share is zero."""
+    e, one, stats = torch.empty(0, 64, dtype=F16, device=DEV), torch.ones(64, dtype=F16, device=DEV), torch.empty(0, 4, device=DEV)
+    flat = torch.full((320,), GUARD, dtype=F16, device=DEV)
+    dgate, v = flat[128:128 + 64 * gates].view(gates, 64), [torch.full((64,), GUARD, dtype=F16, device=DEV) for _ in range(4)]
+    a = dict(post=(one, one), gate=torch.ones(gates, 64, dtype=F16, device=DEV), pre=(one, one), rows_per_gate=per)
+    A.nmt_op_gated_norm_fwd(e, e, e, e, stats, **a)
+    A.nmt_op_gated_norm_bwd(e, e, e, e, stats, e, e, None, dpost=v[:2], dgate=dgate, dpre=v[2:], **a)
+    torch.cuda.synchronize()
+    assert all((x == 0).all() for x in v) and (dgate == 0).all()
+    assert (flat[:128] == GUARD).all() and (flat[128 + 64 * gates:] == GUARD).all()
+
+
 def test_gated_norm_of_rows_more_than_32_bits_apart():
     """Rows 2^30 + 5 elements apart: the third begins behind 2^31 elements."""
     ld, d = 2 ** 30 + 5, 520

@@ -251,3 +251,27 @@ def test_the_norm_before_the_first_block_has_no_residual_scale():
     """Without a block's output h is x itself: a scale that the forward call left out and the backward call put into dx would be no gradient of it."""
     alone = dict(d_y=None, d_post_gain=None, d_post_shift=None, d_gate=None, d_h=None, resid_scale=0.9)
     refused(A.load().nmt_op_gated_norm_fwd(C.byref(block(**alone)), None), says="resid_scale")
+
+
+@pytest.mark.parametrize("per", [1, 27, 2 ** 31 - 2])
+def test_no_rows_have_no_gates_per_group_of_rows(per):
+    """ceil(0 / rows_per_gate) gates: their gradient is an array of nothing, wherever it begins.  (Nothing is launched.)"""
+    g = grads(d_dpost_gain=None, d_dpost_shift=None, d_dpre_gain=None, d_dpre_shift=None)
+    for gate in (P, None):
+        assert A.load().nmt_op_gated_norm_bwd(C.byref(block(rows=0, rows_per_gate=per, d_gate=gate)), C.byref(g), None) == A.NMT_OK
+
+
+@pytest.mark.parametrize("per", [1, 27, None, 0])
+@pytest.mark.parametrize("gates", [0, 1])
+def test_binding_takes_the_gates_of_no_rows(gates, per):
+    """None, or the one that all rows share; more do not belong to no rows."""
+    e, v = rows(0, 16), torch.ones(16, dtype=torch.float16)
+    a = dict(post=(v, None), pre=(v, None), rows_per_gate=per)
+    with pytest.raises(A.NmtError, match="not on a GPU"):
+        A.nmt_op_gated_norm_fwd(e, e, e, e, torch.zeros(0, 4), gate=rows(gates, 16), **a)
+    with pytest.raises(A.NmtError, match="not on a GPU"):
+        A.nmt_op_gated_norm_bwd(e, e, e, e, torch.zeros(0, 4), e, e, None, gate=rows(gates, 16), dgate=rows(gates, 16), **a)
+    with pytest.raises(A.NmtError, match="gate"):
+        A.nmt_op_gated_norm_fwd(e, e, e, e, torch.zeros(0, 4), gate=rows(2, 16), **a)
+    with pytest.raises(A.NmtError, match="gate"):
+        A.nmt_op_gated_norm_bwd(e, e, e, e, torch.zeros(0, 4), e, e, None, gate=rows(gates, 16), dgate=rows(1 - gates, 16), **a)
