@@ -405,6 +405,8 @@ typedef struct nmt_gated_norm {
   float* d_stats;
 } nmt_gated_norm;
 int nmt_op_gated_norm_fwd(const nmt_gated_norm* a /*host*/, void* stream);
+/* Host only.  Debug export: the work-groups of that call's launch and the threads of each, for tests of sizes that no test can allocate. */
+int nmt_debug_gated_norm_grid(int32_t rows, int32_t d, int32_t type, int64_t* groups, int32_t* threads);
 
 /* Backward of the above.  Read from `a`: rows, d, type, kind, resid_scale, rows_per_gate, the gains, shifts and gate, d_y, d_h (without d_y: the x
  * of the forward call), ld_y, ld_h and d_stats; its x, n and eps are not used.  Without d_y resid_scale is 1 for the gradient at the forward call's x; a caller that made this x

@@ -110,6 +110,7 @@ _SIGNATURES = {
     "nmt_op_adam": (C.c_int, [_P, _P, _P, _P, _F, _P, _I64, _F, _F, _F, _F, _I32, _P, _P]),
     "nmt_op_dropout_mask": (C.c_int, [_P, _I32, _I32, _DP, _P]),
     "nmt_op_gated_norm_fwd": (C.c_int, [C.POINTER(nmt_gated_norm), _P]),
+    "nmt_debug_gated_norm_grid": (C.c_int, [_I32, _I32, _I32, C.POINTER(_I64), C.POINTER(_I32)]),
     "nmt_op_gated_norm_bwd_scratch": (_I64, [_I32, _I32, _I32]),
     "nmt_op_gated_norm_bwd": (C.c_int, [C.POINTER(nmt_gated_norm), C.POINTER(nmt_gated_norm_grad), _P]),
     "nmt_op_expert_dispatch_scratch": (_I64, [_I32, _I32, _I32]),
@@ -554,6 +555,13 @@ def nmt_op_gated_norm_fwd(x, y, h, n, stats=None, post=None, gate=None, pre=None
     if stats is not None:
         a.d_stats = _vector(stats, 4 * rows, _FLOAT, device, "stats")
     _call(lib.nmt_op_gated_norm_fwd, device, stream, a)
+
+
+def nmt_debug_gated_norm_grid(rows, d, dtype):
+    """(work-groups, threads of each) of nmt_op_gated_norm_fwd's launch."""
+    lib, groups, threads = _lib or load(), C.c_int64(), C.c_int32()
+    _check(lib.nmt_debug_gated_norm_grid(rows, d, _type_code(dtype, "nmt_debug_gated_norm_grid"), C.byref(groups), C.byref(threads)))
+    return groups.value, threads.value
 
 
 def nmt_op_gated_norm_bwd_scratch(rows, d, rows_per_gate=None):

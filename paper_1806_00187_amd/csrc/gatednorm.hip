@@ -50,6 +50,9 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
   return v;
 }
 
+// Of a work-group whose rows are held by `waves` wavefronts each.
+constexpr int threads_of(int waves) { return waves > 4 ? 64 * waves : waves == 2 ? 128 : 256; }
+
 // LANES lanes of each of WAVES wavefronts hold a row: every LANES * WAVES-th of its vectors of 16 bytes, VECS a lane (or none, and an element each, of rows
 // shorter than that).  RAGGED: d is no multiple of a vector; the last one then ends with the row and has elements in common with the one before.  A lane to
 // which nothing is left takes the last vector once more.  What lanes have in common they compute and store alike, bit for bit, and one of them adds it to
@@ -60,7 +63,7 @@ struct Shape {
   static constexpr bool RAGGED = RAGGED_;
   static constexpr int kVec = VECS ? Row<T>::kVec : 1, kN = VECS ? VECS : 1, kStep = LANES * WAVES * kVec, kE = kN * kVec;  // kE: elements of a lane
   static constexpr int kLanes = LANES, kWaves = WAVES, kCover = kN * kStep;
-  static constexpr int kThreads = WAVES > 4 ? 64 * WAVES : WAVES == 2 ? 128 : 256;
+  static constexpr int kThreads = threads_of(WAVES);
   static constexpr int kRows = kThreads / (LANES * WAVES);  // workers of a work-group
   typedef T vec __attribute__((ext_vector_type(kVec), aligned(sizeof(T))));
   static __device__ __forceinline__ int worker() { return WAVES > 1 ? 0 : threadIdx.x / LANES; }
@@ -579,6 +582,7 @@ int backward_form(int type) { return type == NMT_F32 ? kBackwardWide : kBackward
 constexpr int kFwdWaves = 4096, kBwdWaves = 1024;
 int bwd_groups(int waves) { return std::max(kBwdWaves / waves, device_info().cus); }  // (of wavefronts for a row: one work-group to a compute unit)
 constexpr int64_t kStreamFrom = 64 << 20;  // bytes of a result
+constexpr int kMostGroups = (1 << 22) - 1;  // a grid has less than 2^32 threads, of which a work-group has 1024 at most
 
 struct Split {
   int chunk, groups, workers, pitch;
@@ -587,7 +591,7 @@ Split split_rows(int rows, int d, int type, int form, int rows_per_gate) {
   const int shape = shape_of(d, type), at_once = workers_of(shape, form), waves = std::max(at_once > 1 ? 4 : 1, waves_of_row(shape, form));
   Split p;
   if (form == kForward) {
-    p.chunk = (int64_t)rows * waves >= (int64_t)2 * kFwdWaves * at_once ? std::max(2, ceil_div(rows, (int64_t)at_once << 22)) : 1;  // (a grid has less than 2^32 threads)
+    p.chunk = (int64_t)rows * waves >= (int64_t)2 * kFwdWaves * at_once ? std::max(2, ceil_div(rows, (int64_t)at_once * kMostGroups)) : 1;
   } else {
     p.chunk = ceil_div(rows, bwd_groups(waves) * at_once);
     if (rows_per_gate < rows && rows_per_gate <= 2 * (int64_t)p.chunk) p.chunk = ceil_div(p.chunk, rows_per_gate) * rows_per_gate;  // no gate's rows are two workers' then
@@ -725,6 +729,14 @@ extern "C" int nmt_op_gated_norm_fwd(const nmt_gated_norm* a, void* stream_) {
   else if (a->type == NMT_BF16) launch_fwd<bf16_t>(k, dim3(p.groups), shape, grouped, stream);
   else launch_fwd<float>(k, dim3(p.groups), shape, grouped, stream);
   NMT_LAUNCH_CHECK();
+  return NMT_OK;
+}
+
+extern "C" int nmt_debug_gated_norm_grid(int32_t rows, int32_t d, int32_t type, int64_t* groups, int32_t* threads) {
+  const char* who = "nmt_debug_gated_norm_grid";
+  NMT_REQUIRE(rows >= 1 && rows <= kMaxRows && d >= 1 && d <= kMaxCols && row_type_ok(type) && groups && threads, "%s: bad argument", who);
+  *groups = split_rows(rows, d, type, kForward, rows).groups;
+  *threads = threads_of(waves_of_row(shape_of(d, type), kForward));
   return NMT_OK;
 }
 

@@ -275,3 +275,13 @@ def test_binding_takes_the_gates_of_no_rows(gates, per):
         A.nmt_op_gated_norm_fwd(e, e, e, e, torch.zeros(0, 4), gate=rows(2, 16), **a)
     with pytest.raises(A.NmtError, match="gate"):
         A.nmt_op_gated_norm_bwd(e, e, e, e, torch.zeros(0, 4), e, e, None, gate=rows(gates, 16), dgate=rows(1 - gates, 16), **a)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+@pytest.mark.parametrize("d", [1, 64, 100, 256, 512, 1024, 2048, 4096, 4100, 8192, 8200, 12289, 16384])
+def test_forward_grids_have_less_than_2_to_the_32_threads(d, dtype):
+    """A launch of as many is refused.  Rows around all multiples of 2^22, where a run gets another row, and the most there may be."""
+    most = 2 ** 31 - 1 - 65536
+    for rows in {max(1, min(most, (m << 22) + off)) for m in range(513) for off in (-2, -1, 0, 1, 2)}:
+        groups, threads = A.nmt_debug_gated_norm_grid(rows, d, dtype)
+        assert groups * threads < 2 ** 32, (rows, groups, threads)
