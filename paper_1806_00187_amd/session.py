@@ -29,6 +29,10 @@ class Session:
         weights: dict name -> float16 numpy array (initial fp16 weights = initial master values).
         weight_decay > 0 or state_bits = 8: the updates are AdamW's (nmt_adamw_step) instead of Adam's, with weight decay on matrices and none
         on biases and LayerNorm vectors; 8 bits: the moments take one byte each (float8_e4m3fn m and v, with scales m_scale and v_scale per 256 elements)."""
+        if state_bits not in (8, 32):
+            raise ValueError(f"state_bits = {state_bits}: 8 or 32")
+        if not 0 <= weight_decay <= float(np.finfo(np.float32).max):
+            raise ValueError(f"weight_decay = {weight_decay}: finite and not negative")
         self.device = torch.device(device)
         self.model = dict(model)
         self.n_pipes = n_pipes
@@ -54,8 +58,6 @@ class Session:
         if optimizer:
             self.master = self.w16.float()
             self.acc = torch.zeros(self.P, dtype=torch.float32, device=self.device)
-            if state_bits not in (8, 32):
-                raise ValueError(f"state_bits = {state_bits}: 8 or 32")
             state = torch.float8_e4m3fn if state_bits == 8 else torch.float32
             self.m, self.v = (torch.zeros(self.P, dtype=torch.uint8 if state_bits == 8 else state, device=self.device).view(state) for _ in range(2))
         else:

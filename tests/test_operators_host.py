@@ -285,3 +285,17 @@ def test_forward_grids_have_less_than_2_to_the_32_threads(d, dtype):
     for rows in {max(1, min(most, (m << 22) + off)) for m in range(513) for off in (-2, -1, 0, 1, 2)}:
         groups, threads = A.nmt_debug_gated_norm_grid(rows, d, dtype)
         assert groups * threads < 2 ** 32, (rows, groups, threads)
+
+
+# ---- sessions ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("optimizer", [True, False])
+@pytest.mark.parametrize("bad", [dict(state_bits=16), dict(state_bits=0), dict(weight_decay=-0.01), dict(weight_decay=float("nan")), dict(weight_decay=float("inf")),
+                                 dict(weight_decay=1e39)])
+def test_sessions_refuse_bad_optimizer_settings_before_they_make_anything(bad, optimizer, monkeypatch):
+    import nmt_inputs as I
+    from paper_1806_00187_amd import session
+    made = []
+    monkeypatch.setattr(session.nmt, "nmt_create", lambda **cfg: made.append(cfg))
+    with pytest.raises(ValueError):
+        session.Session(I.MODELS["tiny"], {}, device="cpu", optimizer=optimizer, **bad)
+    assert not made
