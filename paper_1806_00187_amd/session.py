@@ -337,7 +337,9 @@ class Session:
         return flat[off:off + rows * cols].reshape(rows, cols) if rows > 1 else flat[off:off + cols]
 
     def named(self, flat):
-        host = flat.detach().cpu().numpy()
+        """numpy views of the layout's tensors; of moments in 8 bits, which numpy does not have, their values in 32, still without their scales."""
+        host = flat.detach().cpu()
+        host = (host.float() if host.dtype is torch.float8_e4m3fn else host).numpy()
         return {name: self.tensor(host, name) for name in self.layout}
 
 

@@ -299,3 +299,12 @@ def test_sessions_refuse_bad_optimizer_settings_before_they_make_anything(bad, o
     with pytest.raises(ValueError):
         session.Session(I.MODELS["tiny"], {}, device="cpu", optimizer=optimizer, **bad)
     assert not made
+
+
+def test_sessions_name_moments_of_8_bits():
+    from paper_1806_00187_amd.session import Session
+    s = object.__new__(Session)
+    s.layout = {"w": (0, 2, 3), "b": (8, 1, 4)}
+    flat = torch.arange(-6, 6).float().to(torch.float8_e4m3fn)
+    named = s.named(flat)
+    assert named["w"].shape == (2, 3) and named["w"].tolist() == [[-6, -5, -4], [-3, -2, -1]] and named["b"].tolist() == [2, 3, 4, 5]
