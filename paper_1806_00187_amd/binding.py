@@ -752,7 +752,7 @@ def nmt_adamw_create(tensors, table, stream=None):
     size = table.numel() * table.element_size()
     _call(lib.nmt_adamw_create, device, stream, len(tensors), arr, bits, _type_code(grad_type, who), _type_code(weights_type, who),
           _vector(table, table.numel(), table.dtype, device, "the table"), size, out=out)
-    return AdamwPlan(out, device, (list(tensors), table))
+    return AdamwPlan(out, device, ([dict(t) for t in tensors], table))
 
 
 def nmt_adamw_destroy(plan):

@@ -308,3 +308,18 @@ def test_sessions_name_moments_of_8_bits():
     flat = torch.arange(-6, 6).float().to(torch.float8_e4m3fn)
     named = s.named(flat)
     assert named["w"].shape == (2, 3) and named["w"].tolist() == [[-6, -5, -4], [-3, -2, -1]] and named["b"].tolist() == [2, 3, 4, 5]
+
+
+def test_adamw_plans_keep_the_tensors_they_were_made_for(monkeypatch):
+    """Whatever becomes of the caller's list and its dicts: the device table holds those tensors' addresses."""
+    import weakref
+    monkeypatch.setattr(B, "_call", lambda *args, **kw: None)      # (of tensors on the CPU)
+    t = dict(master=torch.zeros(100), m=torch.zeros(100), v=torch.zeros(100), grad=torch.zeros(100), weights=torch.zeros(100))
+    seen, tensors = [weakref.ref(x) for x in t.values()], [t]
+    plan = A.nmt_adamw_create(tensors, torch.zeros(1 << 16, dtype=torch.uint8))
+    for name in ("grad", "weights"):
+        t[name] = None
+    t.clear(), tensors.clear()
+    assert all(ref() is not None for ref in seen)
+    A.nmt_adamw_destroy(plan)
+    assert all(ref() is None for ref in seen)
