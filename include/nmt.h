@@ -478,7 +478,7 @@ typedef struct nmt_adamw nmt_adamw;
 int64_t nmt_adamw_table_bytes(int32_t n, const nmt_adamw_tensor* tensors /*host*/);
 /* Checks the tensors and writes the table of their pieces to d_table (16-byte aligned), which belongs to the handle until nmt_adamw_destroy.  Waits for the
  * stream, so it cannot be captured.  `tensors` itself is not kept; the buffers it names must stay where they are.  A buffer that a step writes
- * overlaps no other of the list, so no tensor is in it twice; gradients may be shared. */
+ * overlaps no other of the list, so no tensor is in it twice; gradients may be shared.  The table overlaps none of them. */
 int nmt_adamw_create(int32_t n, const nmt_adamw_tensor* tensors /*host*/, int32_t state_bits, int32_t grad_type, int32_t weights_type,
                      void* d_table, int64_t table_bytes, void* stream, nmt_adamw** out);
 void nmt_adamw_destroy(nmt_adamw* plan);

@@ -295,18 +295,19 @@ extern "C" int nmt_adamw_create(int32_t n, const nmt_adamw_tensor* tensors, int3
   NMT_REQUIRE(aligned16(d_table), "%s: the table must be 16-byte aligned", who);
   try {
     std::vector<Range> ranges;
-    ranges.reserve(7 * (size_t)n);
+    ranges.reserve(7 * (size_t)n + 1);
+    auto add = [&](const void* p, int64_t bytes, bool written) {
+      if (p && bytes) ranges.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes, written});
+    };
+    add(d_table, pieces * (int64_t)sizeof(Piece), true);  // (gradients, which others write, must not lie there either)
     for (int32_t i = 0; i < n; ++i) {
       const nmt_adamw_tensor& t = tensors[i];
-      auto add = [&](const void* p, int64_t bytes, bool written) {
-        if (p && bytes) ranges.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes, written});
-      };
       const int64_t scales = (t.n + kStateBlock - 1) / kStateBlock * 4;
       add(t.d_master, 4 * t.n, true), add(t.d_m, t.n * (state_bits / 8), true), add(t.d_v, t.n * (state_bits / 8), true);
       add(t.d_m_scale, scales, true), add(t.d_v_scale, scales, true);
       add(t.d_weights, t.n * size(weights_type), true), add(t.d_grad, t.n * size(grad_type), false);
     }
-    NMT_REQUIRE(!overlap(ranges), "%s: what a step writes overlaps another buffer of the list", who);
+    NMT_REQUIRE(!overlap(ranges), "%s: the table or what a step writes overlaps another buffer of the list", who);
     std::vector<Piece> host;
     host.reserve((size_t)pieces);
     for (int32_t i = 0; i < n; ++i) {

@@ -323,3 +323,11 @@ def test_adamw_plans_keep_the_tensors_they_were_made_for(monkeypatch):
     assert all(ref() is not None for ref in seen)
     A.nmt_adamw_destroy(plan)
     assert all(ref() is None for ref in seen)
+
+
+@pytest.mark.parametrize("at", [P, P + 0x2000 + 384, P - 16, P + 0x3000, P + 0x4000])
+def test_adamw_refuses_a_table_among_its_buffers(at):
+    """The kernel takes its addresses from the table, which neither a step nor a backward pass may write over."""
+    lib, arr, out = A.load(), (B.nmt_adamw_tensor * 1)(tensor_of(**AT)), C.c_void_p()
+    refused(lib.nmt_adamw_create(1, arr, 32, A.NMT_F16, A.NMT_F16, at, lib.nmt_adamw_table_bytes(1, arr), None, C.byref(out)), says="overlaps")
+    assert not out.value
