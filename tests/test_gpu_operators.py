@@ -554,6 +554,37 @@ def test_much_room_for_few_tokens(tokens, k, experts, capacity, d):
     assert ur()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,k,experts,capacity,d", [(16385, 1, 16, 0, 1), (8200, 2, 8, 0, 64), (8193, 2, 16, 1200, 100), (9000, 2, 300, 0, 41), (9001, 2, 300, 70, 100),
+                                                         (20000, 1, 1024, 0, 24), (4100, 4, 7, 3000, 777), (300, 64, 9, 0, 2056), (260, 64, 500, 50, 4100), (17000, 1, 3, 6000, 520)])
+def test_many_tokens_go_to_their_experts_and_back(tokens, k, experts, capacity, d, dtype):
+    """More choices than one launch takes: counts of segments, added up where they are used or by a scan, and rows copied by a launch of their own."""
+    test_tokens_go_to_their_experts_and_back(tokens, k, experts, capacity, d, dtype)
+
+
+@pytest.mark.parametrize("tokens,k,experts,capacity,d,dtype", [(25001, 2, 8, 0, 1030, F16), (25001, 2, 8, 7000, 1030, BF16), (13003, 4, 128, 0, 1024, F16), (24600, 1, 5, 0, 1027, F32),
+                                                               (5000, 5, 64, 0, 2057, F16), (6200, 2, 3, 4500, 2052, F32), (8191, 3, 400, 0, 2051, BF16)])
+def test_rows_past_the_caches_go_to_their_experts_and_back(tokens, k, experts, capacity, d, dtype):
+    """96 MB of the experts' rows and more."""
+    assert tokens * k * d * dtype.itemsize >= 96 << 20
+    test_tokens_go_to_their_experts_and_back(tokens, k, experts, capacity, d, dtype)
+
+
+@pytest.mark.parametrize("skew", ["all", "nine tenths"])
+@pytest.mark.parametrize("capacity", [0, 500])
+def test_many_one_sided_choices(capacity, skew):
+    """One expert's list spans every segment."""
+    T, k, E, d = 30000, 2, 12, 72
+    ids = torch.full((T, k), 7, dtype=torch.int32, device=DEV)
+    if skew != "all":
+        ids = torch.where(torch.rand(T, k, generator=gen(3), device=DEV) < 0.9, ids, choices(T, k, E, 4, 0.1))
+    x, rows = torch.randn(T, d, generator=gen(5), device=DEV).half(), torch.full((E * capacity or T * k, d), GUARD, dtype=F16, device=DEV)
+    slot, ranges = dispatched(ids, E, capacity, x, rows)
+    want_slot, want_ranges = R.dispatch(ids.cpu(), E, capacity)
+    assert torch.equal(ranges.cpu(), want_ranges) and torch.equal(slot.cpu(), want_slot)
+    check_rows(rows, x, slot, capacity)
+
+
 def test_dropped_choices_weigh_nothing():
     """NaN weights of dropped choices, and NaN in rows that no token took, reach nothing; a token without an expert gets zeros."""
     ids = torch.tensor([[0, -1], [-1, -1], [1, 0], [0, 0]], dtype=torch.int32, device=DEV)
