@@ -151,6 +151,25 @@ def test_gated_norm_forward_in_place_of_its_inputs(d, parts):
     check_forward(300, d, F16, "rms", 9, 0.9, parts, d, in_place=True)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,d", [(32769 * 4, 5), (65600, 64), (65537, 50), (32801, 100), (16387, 256), (8193, 512), (8195, 300), (4097, 1024), (4099, 1030), (2049, 2048), (2051, 1500), (1027, 4000),
+                                    (1025, 4096), (515, 8192), (513, 5000), (515, 9000), (517, 16384)])
+def test_gated_norm_forward_of_two_rows_a_worker(rows, d, dtype):
+    """The second row is in flight while the first is worked on, in place of its inputs too; an odd number leaves the last worker one."""
+    check_forward(rows, d, dtype, "layer", None, 0.9, "ypgns", d, in_place=True)
+    check_forward(rows, d, dtype, "rms", 7, 1.0, "ypgn", d + 1)
+
+
+@pytest.mark.parametrize("rows,d,dtype", [(530001, 64, F16), (270001, 127, BF16), (140001, 125, F32), (33001, 1030, BF16), (22001, 777, F32), (8301, 4100, F16), (2101, 8200, F32), (2101, 16384, BF16)])
+def test_gated_norm_forward_past_the_caches(rows, d, dtype):
+    """Results of 64 MB and more, in place and apart, rows of whole vectors and others."""
+    assert rows * d * dtype.itemsize >= 64 << 20
+    check_forward(rows, d, dtype, "layer", None, 0.9, "ypgns", d)
+    check_forward(rows, d, dtype, "rms", 27, 0.9, "ypgn", d, in_place=True)
+    check_forward(rows, d, dtype, "layer", None, 0.9, "yg", d, in_place=True)
+    check_forward(rows, d, dtype, "layer", None, 1.0, "ns", d)
+
+
 def check_backward(rows, d, dtype, kind, per, resid, parts, seed, ld=None, shift=0, in_place=False):
     s = norm_inputs(rows, d, dtype, kind, per, seed, "s" in parts)
     post, gate, pre = s["post"] if "p" in parts else None, s["gate"] if "g" in parts else None, s["pre"] if "n" in parts else None
@@ -734,6 +753,17 @@ def test_adamw_over_more_pieces_than_work_groups(bits):
     plan = A.nmt_adamw_create(tensors, torch.empty(A.nmt_adamw_table_bytes(tensors), dtype=torch.uint8, device=DEV))
     check_step(tensors, bits, 9, plan)
     A.nmt_adamw_destroy(plan)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("sizes", [[(16 << 20) - 1], [(16 << 20) - 514, 513], [16 << 20], [(16 << 20) - 513, 514]])
+def test_adamw_through_the_caches_and_past_them(sizes, bits):
+    """Lists of 2^24 elements and more go past the caches, with a last piece that is not whole, those of one less through them."""
+    tensors, ok = adamw_tensors(sizes, bits, F16, F16, 9)
+    plan = A.nmt_adamw_create(tensors, torch.empty(A.nmt_adamw_table_bytes(tensors), dtype=torch.uint8, device=DEV))
+    check_step(tensors, bits, 9, plan)
+    A.nmt_adamw_destroy(plan)
+    assert ok()
 
 
 @pytest.mark.parametrize("bits", [32, 8])
