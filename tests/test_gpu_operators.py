@@ -254,6 +254,14 @@ def test_gated_norm_backward_of_any_rows_and_gates(rows, per):
     check_backward(rows, 648, BF16, "rms", per, 2.5, "yhpgn", rows)
 
 
+@pytest.mark.parametrize("rows,d,per", [(26001, 1024, 27), (26001, 1024, 40), (26001, 1024, 52), (26001, 1024, 53), (3584, 512, 7), (3584, 512, 15), (52000, 64, 13), (52000, 64, 15),
+                                        (2001, 8192, 16), (2001, 8192, 17)])
+def test_gated_norm_backward_of_gates_on_both_sides_of_a_run(rows, d, per):
+    """Rows a gate up to twice a worker's run, which is then rounded to whole gates, and beyond, where two workers share a gate.  A sum has less than 128 additions in a row."""
+    check_backward(rows, d, F16, "layer", per, 0.9, "yhpgns", per)
+    check_backward(rows, d, BF16, "rms", per, 0.9, "yhpgn", per, in_place=True)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("d,ld,shift", [(64, 65, 1), (100, 131, 3), (512, 777, 5), (1024, 1025, 7), (2049, 2051, 1)])
 def test_gated_norm_backward_of_rows_anywhere(d, ld, shift, dtype):
