@@ -1077,3 +1077,25 @@ def test_sessions_without_decay_in_32_bits_keep_adam():
     sess.close()
     with pytest.raises(ValueError):
         Session(model, I.init_weights(seed=0, **model), state_bits=16)
+
+
+@pytest.mark.parametrize("state_bits", [32, 8])
+def test_sessions_of_several_pipes_update_with_adamw(state_bits):
+    """The step over the shared accumulator, from what that held: the first update's moments are (1 - beta) g and (1 - beta) g^2."""
+    import nmt_inputs as I
+    from paper_1806_00187_amd.session import Session
+    model = I.MODELS["tiny"]
+    sess = Session(model, I.init_weights(seed=0, **model), max_sentences=8, n_pipes=2, auto_streams=False, weight_decay=0.02, state_bits=state_bits)
+    batches = [sess.to_device(I.tiny_batch(seed=s)) for s in (1001, 1002, 1003)]
+    before = sess.master.to(D)
+    _, ntok, flag = sess.update(batches, 128.0, 1e-3, 1)
+    assert flag == 0
+    for name, (off, rows, cols) in sess.layout.items():
+        n = rows * cols
+        w0, g = before[off:off + n], sess.acc[off:off + n].to(D) / (128.0 * ntok)
+        assert float(g.abs().max()) > 0, name
+        w, _, _ = R.adamw(w0, torch.zeros_like(g), torch.zeros_like(g), g, 1e-3, 0.9, 0.98, 1e-8, 1, 0.02 if rows > 1 else 0.0)
+        # (as in test_sessions_update_with_adamw; a first step has |m| / root v = 1)
+        within(sess.master[off:off + n], w, 2 * U32 * w.abs() + 64 * U32 * 1e-3 * 9, name)
+    assert torch.equal(sess.w16, sess.master.half())
+    sess.close()
