@@ -1,8 +1,9 @@
 // AdamW over many tensors in one launch, states in 32 bits or in 8.  Bound by memory: master weights and states read and written,
 // gradients read, weights written once.  A table in device memory holds one record for each piece of kPiece elements of
 // every tensor, so that a work-group finds its pointers in one trip.
-// 61 million parameters, states in 32 bits, fp32 gradients: 303 us, 6.0 TB/s.  210 million, states in 8 bits, fp16 gradients: 588 us, 5.7 TB/s (a copy of a
-// gigabyte: 5.2).  Past the caches 303 and 588 us, through them 355 and 657; one block of 256 elements a wavefront, two, four: 318, 303, 312 us.
+// 61 million parameters, states in 32 bits, fp32 gradients: 299 us, 6.1 TB/s.  210 million, states in 8 bits, fp16 gradients: 593 us, 5.7 TB/s (a copy of a
+// gigabyte: 5.2), one step after another; from an idle card the first three take 555 to 585, the next up to 900, and some fifty later they are back.  In turn with other forms: past the caches 303
+// and 588 us, through them 355 and 657; one block of 256 elements a wavefront, two, four: 318, 303, 312 us.
 #include "common.h"
 
 #include <algorithm>
@@ -15,7 +16,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kStateBlock = 256;           // elements that share a scale: a wavefront's, four a lane
 constexpr int kAhead = 2;                  // blocks that a wavefront has in flight
-constexpr int kPiece = 4 * kThreads * kAhead;  // elements of a work-group's turn
+constexpr int kPiece = 4 * kThreads * kAhead;  // elements of a work-group, which takes one piece
 constexpr int64_t kStreamFrom = 16 << 20;  // elements from which master weights and states of 32 bits exceed the last-level cache
 constexpr float kTop = 448.f;              // the largest e4m3 value
 constexpr float kTiny = 0x1p-100f;         // blocks of nothing larger are zero

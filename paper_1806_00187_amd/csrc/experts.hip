@@ -2,7 +2,9 @@
 // sum of a token's rows on the way back, and the gradients.  Bound by memory, the rows that are read and written once, and for few tokens by launches: up to
 // kWhole choices the dispatch is one launch, in which every work-group counts all choices for itself; beyond that counts of segments and their sums over the segments before
 // each are launches of their own (3 us each), and so are the rows.
-// 105402 rows of 1024 bf16 to 64 experts and back: 123 us, 5.3 TB/s (a copy of a gigabyte: 5.2); 7168 of 512 fp16 to 16 experts with room for 8960: 11.2 us.
+// 105402 rows of 1024 bf16 to 64 experts and back: 123 us, 5.3 TB/s (a copy of a gigabyte: 5.2); 7168 of 512 fp16 to 16 experts with room for 8960: 11.6 us in the two kernels.
+// A choice is an addition in LDS to its expert's count, so one-sided choices meet at one address: nine tenths of 7168 to one of 16 experts 7.9 -> 12.2 us of dispatch, of 16384 11.5 -> 21.9; of 105402,
+// whose segments are counted once, 71.6 and 71.1.
 #include "rowtypes.h"
 
 #include <algorithm>

@@ -3,7 +3,7 @@
 // Bound by memory: forward reads x, y and writes h, n (n needs h's statistics, which are there while h is still in registers), backward
 // reads y, h and the gradients at h and n and writes those at x and y.  A row is held in registers by 8 to 64 lanes (up to 64, 128, 256, 512 columns) or by
 // several wavefronts, each lane's share of it 16 bytes at a time; the next row is in flight while one is worked on.
-// Forward 52701 x 1024 bf16: 73 us, 5.9 TB/s (a copy of a gigabyte: 5.2).  Backward 26001 x 1024 fp16: 74 us, 4.3 TB/s, of which the sums over work-groups take 5;
+// Forward 52701 x 1024 bf16: 72 us, 6.0 TB/s (a copy of a gigabyte: 5.2).  Backward 26001 x 1024 fp16 with one gate: 73 us for 320 MB, 4.7 TB/s in the main kernel, 5 us of sums over work-groups;
 // a wavefront per SIMD has its registers full of column sums and two rows.  Backward, fp32 rows of 4097 to 8192 columns do without the second row (3001 x 5000: 100 us for 360 MB), and so
 // do rows of more than 8192, whose shifts' sums are in LDS (2001 x 9000 bf16: 85 us for 216 MB, 1101 x 16384 bf16: 103, fp32, which spill: 209 for 433).
 #include "rowtypes.h"
@@ -594,7 +594,10 @@ Split split_rows(int rows, int d, int type, int form, int rows_per_gate) {
     p.chunk = (int64_t)rows * waves >= (int64_t)2 * kFwdWaves * at_once ? std::max(2, ceil_div(rows, (int64_t)at_once * kMostGroups)) : 1;
   } else {
     p.chunk = ceil_div(rows, bwd_groups(waves) * at_once);
-    if (rows_per_gate < rows && rows_per_gate <= 2 * (int64_t)p.chunk) p.chunk = ceil_div(p.chunk, rows_per_gate) * rows_per_gate;  // no gate's rows are two workers' then
+    // Whole gates, so that no gate's rows are two workers' and none leaves a partial sum, if a gate has at most two runs' rows.  26001 x 1024 fp16, a run being 26 rows, with 27, 30, 40, 52 rows a gate:
+    // 72, 73, 75, 83 us, and 78, 78, 77, 75 without; 2001 x 8192 with 16: 56 and 58.  Where a run nearly doubles the work-groups halve, and that costs more than it saves: the 52 above, and of
+    // smaller calls 3584 x 512 with 8: 14.7 and 12.7, 52000 x 64 with 13: 17.4 and 15.8.
+    if (rows_per_gate < rows && rows_per_gate <= 2 * (int64_t)p.chunk) p.chunk = ceil_div(p.chunk, rows_per_gate) * rows_per_gate;
   }
   p.groups = ceil_div(rows, p.chunk * at_once);
   p.workers = p.groups * at_once;
