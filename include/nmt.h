@@ -389,7 +389,7 @@ int nmt_op_dropout_mask(uint8_t* d_keep, int32_t rows, int32_t n_cols, const nmt
  *   n = norm(h) * pre_gain + pre_shift                                              (not wanted if d_n is NULL)
  * y: the block's output, x: the residual stream before it, n: the next block's input.  n is formed from h before h is
  * rounded.  d_gate NULL: 1; otherwise row r takes row r / rows_per_gate of d_gate [ceil(rows / rows_per_gate), d] (rows_per_gate >= rows: one
- * gate for all; 1: a gate for every element).  No rows have no gates and nothing is written to their gradient, unless rows_per_gate is NMT_ONE_GATE: then it is one, of zeros.  Shifts may be NULL (0).  Gains, shifts and gates are contiguous, of the rows' type.
+ * gate for all; 1: a gate for every element).  No rows have no gates and nothing is written to their gradient, unless rows_per_gate is NMT_ONE_GATE: then there is one, whose gradient is zero.  Shifts may be NULL (0).  Gains, shifts and gates are contiguous, of the rows' type.
  * d_y NULL: the norm before the first block, n = norm(x) * pre_gain + pre_shift; d_h, d_post_gain, d_gate are then NULL too, and resid_scale is 1.
  * d_stats: fp32 [rows, 4] = mean and 1 / sqrt(.) of y, then of h (0 and 1 where there is no norm; RMS: mean 0), for the backward call; may be
  * NULL.  d_h may be d_x, and d_n may be d_y, with the same distance between rows; otherwise what is written overlaps nothing else.
