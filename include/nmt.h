@@ -487,6 +487,89 @@ void nmt_adamw_destroy(nmt_adamw* plan);
 int nmt_adamw_step(const nmt_adamw* plan, double lr, double beta1, double beta2, double eps, int32_t t, float grad_scale,
                    const int32_t* d_flag, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Matrices held in 8 bits.  A matrix [rows, d] is codes in OCP e4m3 (4 exponent and 3 mantissa bits, no infinity), one byte each, rows `ld` bytes apart, and
+ * fp32 scales: value = code * scale.  128 elements of a row share a scale (the last block of a row may be shorter), scale (row r, block b) at b * ld_scales + r:
+ * the scales of one block of columns lie side by side.  Or, `square`, 128 x 128 elements share one: that of rows 128 q ... and block b at b * ld_scales + q.
+ * Bytes behind a row's last code are neither written nor looked at.
+ * ------------------------------------------------------------------------------------------ */
+
+/* x (fp16, bf16 or fp32, any distance between rows, any address) into 8 bits.  scale = the block's largest magnitude / 448, code = x / scale, nearest, ties to
+ * even; a block of nothing larger than 2^-100 is zeros.  What is inf or NaN becomes NaN in its own element and does not count for the scale.
+ * d_codes, d_scales: as x lies.  d_codes_t [d, rows], d_scales_t: its transpose, whose blocks are 128 rows of x in one column (square: the same codes and scales, transposed); what
+ * the products of a backward pass read.  Either pair may be NULL.  What is written overlaps nothing else. */
+int nmt_op_quantize8(const void* d_x, int64_t ld_x, int32_t rows, int32_t d, int32_t type, int32_t square, void* d_codes, int64_t ld_codes,
+                     float* d_scales, int64_t ld_scales, void* d_codes_t, int64_t ld_codes_t, float* d_scales_t, int64_t ld_scales_t, void* stream);
+
+/* The norm before a block whose products take 8 bits, with the residual's addition, row by row:
+ *   h = resid_scale * x + y,  n = norm(h) * gain + shift,
+ * n in 8 bits to d_codes, d_scales (blocks of a row) as nmt_op_quantize8 makes them of n before it is rounded, and, if d_n is not NULL, rounded to the rows' type as well.  n is formed from h before h is
+ * rounded.  d_y NULL: h is x, resid_scale is 1 and d_h NULL.  d_h may be NULL: not wanted.  d_shift may be NULL.  d_stats: fp32 [rows, 4] = 0, 1, mean and 1 / sqrt(.) of h (RMS:
+ * mean 0), may be NULL: what nmt_op_gated_norm_bwd takes, with d_y as its block's output without norm or gate; the gradient passes the rounding to
+ * 8 bits as if it were none.  d_h may be d_x, and d_n may be d_y, with the same distance between rows; otherwise what is written overlaps nothing else.
+ * d <= 16384, rows < 2^31 - 65536. */
+typedef struct nmt_norm8 {
+  int32_t rows, d, type, kind; /* type: NMT_F16 / NMT_BF16 / NMT_F32; kind: NMT_NORM_LAYER / NMT_NORM_RMS */
+  float eps, resid_scale;
+  int64_t ld_x, ld_y, ld_h, ld_n, ld_codes, ld_scales;
+  const void *d_x, *d_y, *d_gain, *d_shift;
+  void *d_h, *d_n, *d_codes;
+  float *d_scales, *d_stats;
+} nmt_norm8;
+int nmt_op_norm8(const nmt_norm8* a /*host*/, void* stream);
+
+/* C[M, N] = A B^T + bias + add for A [M, K] and B [N, K] in 8 bits: products of codes are summed in fp32 over each block of 128 k and times its scales added up in fp32, in increasing k
+ * (a long contraction of a small C in pieces, in a fixed order), rounded once to `type`.  a_square, b_square: whether 128 x 128 elements share a scale.  d_bias [N] and d_add [M, N], of C's type, may be
+ * NULL; d_add may be d_c with the same distances.  y = x W^T: A = x, B = W; the input's gradient: A = dy, B = W transposed; the weight's: A = dy transposed, B = x transposed.
+ * batch products lie stride_* apart (bytes of A and B, elements of the others; 0: the same for all; of C not).
+ * d_ranges NULL: `batch` products of M x N x K each.  Otherwise d_ranges [batch, 2] (nmt_op_expert_dispatch): expert e's rows are the ranges[e, 1] rows of A, of the scales and of C from ranges[e, 0] on, M is
+ * the number of rows of A and C in all, its B, scales of B and bias lie e strides on, the other strides are not used, and a_square is 0.  Rows that no expert has are left as they
+ * were; ranges do not overlap, and what of them lies outside [0, M) is cut off.
+ * Rows of A and B begin at multiples of 16 bytes; C, bias and add have any address that their type allows and any distance.  K = 0: bias + add.  batch <= 1024; lda, ldb <= 2^27.
+ * d_scratch: 16-byte aligned, scratch_floats >= nmt_op_gemm8_scratch(M, N, K, batch, ranges != NULL), which may be 0. */
+typedef struct nmt_gemm8 {
+  int32_t M, N, K, batch, type, a_square, b_square;
+  int64_t lda, ldb, ldc, ld_add, ld_sa, ld_sb;
+  int64_t stride_a, stride_b, stride_c, stride_add, stride_bias, stride_sa, stride_sb;
+  const void *d_a, *d_b;
+  const float *d_sa, *d_sb;
+  const void *d_bias, *d_add;
+  void* d_c;
+  const int32_t* d_ranges;
+  float* d_scratch;
+  int64_t scratch_floats;
+} nmt_gemm8;
+int64_t nmt_op_gemm8_scratch(int32_t M, int32_t N, int32_t K, int32_t batch, int32_t ranges);
+int nmt_op_gemm8(const nmt_gemm8* a /*host*/, void* stream);
+
+/* A sparse layer as a whole over few tokens (at most 64; more: nmt_op_expert_dispatch, nmt_op_gemm8, nmt_op_expert_combine), as when one token of each sentence is at hand:
+ *   hidden[t, j] = act(up[expert[t, j]] x[t]),  out[t] = add[t] + sum over j of weights[t, j] * down[expert[t, j]] hidden[t, j].
+ * act NMT_ACT_RELU: up [experts, ff, d], max(., 0).  NMT_ACT_SILU_GATE: up [experts, 2 ff, d], g / (1 + exp(-g)) * u of its rows r (g) and ff + r (u).  down [experts, d, ff].  Weights in 8 bits with
+ * square scales, experts stride_* apart (bytes; floats of the scales), rows at multiples of 16 bytes.  x, add and out are of `type`; products, hidden and sums fp32, with the inputs as they are (not in
+ * 8 bits), out rounded once.  d_expert [tokens, k]: a value outside [0, experts) is none and adds nothing, whatever its weight; only experts that are chosen are read.
+ * d_weights fp32 [tokens, k], NULL: 1.  d_add may be NULL, or d_out with the same distance.
+ * d_scratch: 16-byte aligned, scratch_floats >= nmt_op_expert_layer8_scratch.  k <= 64, experts <= 1024, d and ff <= 2^20. */
+#define NMT_ACT_RELU 0
+#define NMT_ACT_SILU_GATE 1
+typedef struct nmt_expert_layer8 {
+  int32_t tokens, k, experts, d, ff, type, act;
+  int64_t ld_x, ld_add, ld_out;
+  int64_t ld_up, stride_up, ld_up_scales, stride_up_scales, ld_down, stride_down, ld_down_scales, stride_down_scales;
+  const void* d_x;
+  const int32_t* d_expert;
+  const float* d_weights;
+  const void* d_up;
+  const float* d_up_scales;
+  const void* d_down;
+  const float* d_down_scales;
+  const void* d_add;
+  void* d_out;
+  float* d_scratch;
+  int64_t scratch_floats;
+} nmt_expert_layer8;
+int64_t nmt_op_expert_layer8_scratch(int32_t tokens, int32_t k, int32_t experts, int32_t d, int32_t ff);
+int nmt_op_expert_layer8(const nmt_expert_layer8* a /*host*/, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -58,6 +58,31 @@ class nmt_adamw_tensor(C.Structure):
                 ("d_v", C.c_void_p), ("d_m_scale", C.c_void_p), ("d_v_scale", C.c_void_p), ("d_grad", C.c_void_p), ("d_weights", C.c_void_p)]
 
 
+class nmt_norm8(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("d", C.c_int32), ("type", C.c_int32), ("kind", C.c_int32), ("eps", C.c_float), ("resid_scale", C.c_float),
+                ("ld_x", C.c_int64), ("ld_y", C.c_int64), ("ld_h", C.c_int64), ("ld_n", C.c_int64), ("ld_codes", C.c_int64), ("ld_scales", C.c_int64),
+                ("d_x", C.c_void_p), ("d_y", C.c_void_p), ("d_gain", C.c_void_p), ("d_shift", C.c_void_p), ("d_h", C.c_void_p), ("d_n", C.c_void_p),
+                ("d_codes", C.c_void_p), ("d_scales", C.c_void_p), ("d_stats", C.c_void_p)]
+
+
+class nmt_gemm8(C.Structure):
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("batch", C.c_int32), ("type", C.c_int32), ("a_square", C.c_int32),
+                ("b_square", C.c_int32), ("lda", C.c_int64), ("ldb", C.c_int64), ("ldc", C.c_int64), ("ld_add", C.c_int64), ("ld_sa", C.c_int64),
+                ("ld_sb", C.c_int64), ("stride_a", C.c_int64), ("stride_b", C.c_int64), ("stride_c", C.c_int64), ("stride_add", C.c_int64),
+                ("stride_bias", C.c_int64), ("stride_sa", C.c_int64), ("stride_sb", C.c_int64), ("d_a", C.c_void_p), ("d_b", C.c_void_p),
+                ("d_sa", C.c_void_p), ("d_sb", C.c_void_p), ("d_bias", C.c_void_p), ("d_add", C.c_void_p), ("d_c", C.c_void_p),
+                ("d_ranges", C.c_void_p), ("d_scratch", C.c_void_p), ("scratch_floats", C.c_int64)]
+
+
+class nmt_expert_layer8(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("k", C.c_int32), ("experts", C.c_int32), ("d", C.c_int32), ("ff", C.c_int32), ("type", C.c_int32),
+                ("act", C.c_int32), ("ld_x", C.c_int64), ("ld_add", C.c_int64), ("ld_out", C.c_int64), ("ld_up", C.c_int64), ("stride_up", C.c_int64),
+                ("ld_up_scales", C.c_int64), ("stride_up_scales", C.c_int64), ("ld_down", C.c_int64), ("stride_down", C.c_int64),
+                ("ld_down_scales", C.c_int64), ("stride_down_scales", C.c_int64), ("d_x", C.c_void_p), ("d_expert", C.c_void_p),
+                ("d_weights", C.c_void_p), ("d_up", C.c_void_p), ("d_up_scales", C.c_void_p), ("d_down", C.c_void_p), ("d_down_scales", C.c_void_p),
+                ("d_add", C.c_void_p), ("d_out", C.c_void_p), ("d_scratch", C.c_void_p), ("scratch_floats", C.c_int64)]
+
+
 _P, _I32, _I64, _F, _U32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_uint32
 _DP = C.POINTER(nmt_dropout)
 _SP = C.POINTER(nmt_segment)
@@ -120,6 +145,12 @@ _SIGNATURES = {
     "nmt_adamw_table_bytes": (_I64, [_I32, C.POINTER(nmt_adamw_tensor)]),
     "nmt_adamw_create": (C.c_int, [_I32, C.POINTER(nmt_adamw_tensor), _I32, _I32, _I32, _P, _I64, _P, C.POINTER(_P)]),
     "nmt_adamw_destroy": (None, [_P]),
+    "nmt_op_quantize8": (C.c_int, [_P, _I64, _I32, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
+    "nmt_op_norm8": (C.c_int, [C.POINTER(nmt_norm8), _P]),
+    "nmt_op_gemm8_scratch": (_I64, [_I32, _I32, _I32, _I32, _I32]),
+    "nmt_op_gemm8": (C.c_int, [C.POINTER(nmt_gemm8), _P]),
+    "nmt_op_expert_layer8_scratch": (_I64, [_I32, _I32, _I32, _I32, _I32]),
+    "nmt_op_expert_layer8": (C.c_int, [C.POINTER(nmt_expert_layer8), _P]),
     "nmt_adamw_step": (C.c_int, [_P, C.c_double, C.c_double, C.c_double, C.c_double, _I32, _F, _P, _P]),
 }
 
@@ -436,17 +467,17 @@ NMT_NORM_LAYER, NMT_NORM_RMS, NMT_ONE_GATE = 0, 1, 2 ** 31 - 1
 _MOST = 2 ** 31 - 1
 _KINDS = {"layer": NMT_NORM_LAYER, "rms": NMT_NORM_RMS}
 _TYPES = {}          # torch dtypes -> type codes; filled with _FLOAT and _INT when torch is there (load())
-_FLOAT = _INT = _torch = _raw_stream = None
+_FLOAT = _INT = _E4M3 = _torch = _raw_stream = None
 
 
 def _torch_types():
-    global _FLOAT, _INT, _torch, _raw_stream
+    global _FLOAT, _INT, _E4M3, _torch, _raw_stream
     import torch
     _torch = torch
     # (what torch.cuda.current_stream looks up, without the Stream object around it: 0.1 us instead of 1)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
     _TYPES.update({torch.float16: NMT_F16, torch.bfloat16: NMT_BF16, torch.float32: NMT_F32})
-    _FLOAT, _INT = torch.float32, torch.int32
+    _FLOAT, _INT, _E4M3 = torch.float32, torch.int32, torch.float8_e4m3fn
 
 
 def _refuse(msg, code=NMT_EINVAL):
@@ -766,3 +797,163 @@ def nmt_adamw_step(plan, lr, beta1, beta2, eps, t, grad_scale=1.0, flag=None, st
         _refuse("nmt_adamw_step: the plan has been given back")
     _call(_lib.nmt_adamw_step, plan.device, stream, plan.handle, lr, beta1, beta2, eps, t, grad_scale,
           None if flag is None else _vector(flag, 1, _INT, plan.device, "flag"))
+
+
+# ---- matrices held in 8 bits -----------------------------------------------------------------------
+# Codes are float8_e4m3fn [rows, d], scales fp32 [blocks of 128 columns, rows], or [blocks of columns, blocks of 128 rows] where 128 x 128 elements share one.
+NMT_ACT_RELU, NMT_ACT_SILU_GATE = 0, 1
+_ACTS = {"relu": NMT_ACT_RELU, "silu_gate": NMT_ACT_SILU_GATE}
+
+
+def nmt_op_quantize8(x, codes=None, scales=None, codes_t=None, scales_t=None, square=False, stream=None):
+    """x [rows, d] into codes [rows, d] with scales [ceil(d / 128), rows], and into codes_t [d, rows] with scales_t [ceil(rows / 128), d], its transpose; either pair may be None.
+    square: scales [ceil(d / 128), ceil(rows / 128)], and transposed."""
+    lib, who = _lib or load(), "nmt_op_quantize8"
+    rows, d, dtype, device = _rows_of(x, who, "x")
+    x_, ld_x = _matrix(x, rows, d, dtype, device, "x")
+    down, across = -(-rows // 128), -(-d // 128)
+    codes_ = scales_ = codes_t_ = scales_t_ = None
+    ld_codes = ld_scales = ld_codes_t = ld_scales_t = 0
+    if codes is not None:
+        codes_, ld_codes = _matrix(codes, rows, d, _E4M3, device, "codes")
+    if scales is not None:
+        scales_, ld_scales = _matrix(scales, across, down if square else rows, _FLOAT, device, "scales")
+    if codes_t is not None:
+        codes_t_, ld_codes_t = _matrix(codes_t, d, rows, _E4M3, device, "codes_t")
+    if scales_t is not None:
+        scales_t_, ld_scales_t = _matrix(scales_t, down, across if square else d, _FLOAT, device, "scales_t")
+    _call(lib.nmt_op_quantize8, device, stream, x_, ld_x, rows, d, _type_code(dtype, who), 1 if square else 0, codes_, ld_codes, scales_, ld_scales,
+          codes_t_, ld_codes_t, scales_t_, ld_scales_t)
+
+
+def nmt_op_norm8(x, y, h, codes, scales, gain, shift=None, n=None, stats=None, kind="rms", resid_scale=1.0, eps=1e-5, stream=None):
+    """h = resid_scale * x + y, n = norm(h) * gain + shift in 8 bits: codes [rows, d], scales [ceil(d / 128), rows]; n itself as well if a tensor is given.  y None: h is x, and
+    h None."""
+    lib, who = _lib or load(), "nmt_op_norm8"
+    rows, d, dtype, device = _rows_of(x, who, "x")
+    if kind not in _KINDS:
+        _refuse(f"{who}: kind {kind!r}: 'layer' or 'rms'")
+    a = nmt_norm8()
+    a.rows, a.d, a.type, a.kind, a.resid_scale, a.eps = rows, d, _type_code(dtype, who), _KINDS[kind], resid_scale, eps
+    a.d_x, a.ld_x = _matrix(x, rows, d, dtype, device, "x")
+    if y is not None:
+        a.d_y, a.ld_y = _matrix(y, rows, d, dtype, device, "y")
+    if h is not None:
+        a.d_h, a.ld_h = _matrix(h, rows, d, dtype, device, "h")
+    if n is not None:
+        a.d_n, a.ld_n = _matrix(n, rows, d, dtype, device, "n")
+    a.d_gain = _vector(gain, d, dtype, device, "the gain")
+    if shift is not None:
+        a.d_shift = _vector(shift, d, dtype, device, "the shift")
+    a.d_codes, a.ld_codes = _matrix(codes, rows, d, _E4M3, device, "codes")
+    a.d_scales, a.ld_scales = _matrix(scales, -(-d // 128), rows, _FLOAT, device, "scales")
+    if stats is not None:
+        a.d_stats = _vector(stats, 4 * rows, _FLOAT, device, "stats")
+    _call(lib.nmt_op_norm8, device, stream, a)
+
+
+def _stack(t, batch, rows, d, dtype, device, what):
+    """(address, distance between rows, distance between matrices) of a [rows, d] tensor, or of a [batch, rows, d] one."""
+    if t.dtype is not dtype or t.get_device() != device or t.shape not in ((rows, d), (batch, rows, d)) or (batch != 1 and t.dim() == 2):
+        _refuse(f"{what} is {tuple(t.shape)} {t.dtype} on {t.device}, not ({batch}, {rows}, {d}) {dtype} on device {device}")
+    *many, ld, step = t.stride()
+    if rows <= 1:
+        ld = d
+    stride = many[0] if many and batch > 1 else 0
+    if (step != 1 and d > 1) or ld < d or stride < 0:
+        _refuse(f"{what} has strides {t.stride()}: rows whose elements lie side by side and that do not overlap are taken")
+    return t.data_ptr(), ld, stride
+
+
+def _scale_lines(scales, rows, what):
+    """Whether these are the scales of 128 x 128 elements each."""
+    lines = scales.shape[-1] if scales.dim() in (2, 3) else -1
+    if lines == rows:
+        return 0
+    if lines != -(-rows // 128):
+        _refuse(f"{what} are {tuple(scales.shape)}: a column for each of {rows} rows, or for each 128 of them")
+    return 1
+
+
+def nmt_op_gemm8_scratch(M, N, K, batch=1, ranges=False):
+    _sizes("nmt_op_gemm8_scratch", M, N, K, batch)
+    n = load().nmt_op_gemm8_scratch(M, N, K, batch, 1 if ranges else 0)
+    if n < 0:
+        _check(int(n))
+    return n
+
+
+def nmt_op_gemm8(a, a_scales, b, b_scales, c, bias=None, add=None, ranges=None, scratch=None, stream=None):
+    """c = a b^T + bias + add: a [M, K] and b [N, K] in 8 bits, c and add [M, N], bias [N]; or a, b, c, add and their scales with a dimension of products in front (bias then [batch, N]).
+    ranges [experts, 2]: a, c and add are [M, .], expert e's rows those of its range, b [experts, N, K] and bias [experts, N]."""
+    lib, who = _lib or load(), "nmt_op_gemm8"
+    if c is None or c.dim() not in (2, 3) or a is None or a.dim() not in (2, 3) or b is None or b.dim() not in (2, 3):
+        _refuse(f"{who}: a, b and c are tensors of two or three dimensions")
+    device, dtype = c.get_device(), c.dtype
+    (M, N), K = c.shape[-2:], a.shape[-1]
+    batch = b.shape[0] if ranges is not None and b.dim() == 3 else 1 if ranges is not None or c.dim() == 2 else c.shape[0]
+    _sizes(who, M, N, K, batch)
+    rows_batch = 1 if ranges is not None else batch
+    if ranges is not None and (c.dim() == 3 or a.dim() == 3):
+        _refuse(f"{who}: experts' rows lie in one matrix")
+    g = nmt_gemm8()
+    g.M, g.N, g.K, g.batch, g.type = M, N, K, batch, _type_code(dtype, who)
+    g.d_a, g.lda, g.stride_a = _stack(a, rows_batch, M, K, _E4M3, device, "a")
+    g.d_b, g.ldb, g.stride_b = _stack(b, batch, N, K, _E4M3, device, "b")
+    g.lda, g.ldb = (-(-K // 16) * 16 if M <= 1 else g.lda), (-(-K // 16) * 16 if N <= 1 else g.ldb)
+    g.d_c, g.ldc, g.stride_c = _stack(c, rows_batch, M, N, dtype, device, "c")
+    blocks = -(-K // 128)
+    g.a_square, g.b_square = _scale_lines(a_scales, M, "a's scales"), _scale_lines(b_scales, N, "b's scales")
+    g.d_sa, g.ld_sa, g.stride_sa = _stack(a_scales, rows_batch, blocks, -(-M // 128) if g.a_square else M, _FLOAT, device, "a's scales")
+    g.d_sb, g.ld_sb, g.stride_sb = _stack(b_scales, batch, blocks, -(-N // 128) if g.b_square else N, _FLOAT, device, "b's scales")
+    if add is not None:
+        g.d_add, g.ld_add, g.stride_add = _stack(add, rows_batch, M, N, dtype, device, "add")
+    if bias is not None:
+        g.d_bias, _, g.stride_bias = _stack(bias.unsqueeze(-2) if bias.dim() == 2 else bias.unsqueeze(0), batch, 1, N, dtype, device, "bias")
+    if ranges is not None:
+        g.d_ranges = _vector(ranges, 2 * batch, _INT, device, "ranges")
+    if scratch is not None:
+        g.scratch_floats = scratch.numel()
+        g.d_scratch = _vector(scratch, g.scratch_floats, _FLOAT, device, "scratch")
+    _call(lib.nmt_op_gemm8, device, stream, g)
+
+
+def nmt_op_expert_layer8_scratch(tokens, k, experts, d, ff):
+    _sizes("nmt_op_expert_layer8_scratch", tokens, k, experts, d, ff)
+    n = load().nmt_op_expert_layer8_scratch(tokens, k, experts, d, ff)
+    if n < 0:
+        _check(int(n))
+    return n
+
+
+def nmt_op_expert_layer8(x, expert, weights, up, up_scales, down, down_scales, out, scratch, add=None, act="relu", stream=None):
+    """out[t] = add[t] + sum over j of weights[t, j] * down[e] act(up[e] x[t]), e = expert[t, j]: x, out, add [tokens, d], expert int32 and weights fp32 (or None: 1) [tokens, k], up [experts,
+    ff, d] (act "silu_gate": [experts, 2 ff, d]) and down [experts, d, ff] in 8 bits with scales of 128 x 128."""
+    lib, who = _lib or load(), "nmt_op_expert_layer8"
+    tokens, d, dtype, device = _rows_of(x, who, "x")
+    n, k, _ = _lists(expert, who, "expert")
+    if act not in _ACTS:
+        _refuse(f"{who}: act {act!r}: 'relu' or 'silu_gate'")
+    if n != tokens or down is None or down.dim() != 3 or up is None or up.dim() != 3:
+        _refuse(f"{who}: experts of {n} tokens of {tokens}, up and down of three dimensions")
+    experts, _, ff = down.shape
+    _sizes(who, experts, ff)
+    wide = 2 * ff if act == "silu_gate" else ff
+    p = nmt_expert_layer8()
+    p.tokens, p.k, p.experts, p.d, p.ff, p.type, p.act = tokens, k, experts, d, ff, _type_code(dtype, who), _ACTS[act]
+    p.d_x, p.ld_x = _matrix(x, tokens, d, dtype, device, "x")
+    p.d_expert = _vector(expert, tokens * k, _INT, device, "expert")
+    if weights is not None:
+        p.d_weights = _vector(weights, tokens * k, _FLOAT, device, "weights")
+    p.d_up, p.ld_up, p.stride_up = _stack(up, experts, wide, d, _E4M3, device, "up")
+    p.d_down, p.ld_down, p.stride_down = _stack(down, experts, d, ff, _E4M3, device, "down")
+    p.ld_up, p.ld_down = (-(-d // 16) * 16 if wide <= 1 else p.ld_up), (-(-ff // 16) * 16 if d <= 1 else p.ld_down)
+    p.d_up_scales, p.ld_up_scales, p.stride_up_scales = _stack(up_scales, experts, -(-d // 128), -(-wide // 128), _FLOAT, device, "up's scales")
+    p.d_down_scales, p.ld_down_scales, p.stride_down_scales = _stack(down_scales, experts, -(-ff // 128), -(-d // 128), _FLOAT, device, "down's scales")
+    p.d_out, p.ld_out = _matrix(out, tokens, d, dtype, device, "out")
+    if add is not None:
+        p.d_add, p.ld_add = _matrix(add, tokens, d, dtype, device, "add")
+    if scratch is not None:
+        p.scratch_floats = scratch.numel()
+        p.d_scratch = _vector(scratch, p.scratch_floats, _FLOAT, device, "scratch")
+    _call(lib.nmt_op_expert_layer8, device, stream, p)
