@@ -29,12 +29,27 @@ struct Gemm8Args {
   const int32_t* ranges;
   int64_t lda, ldb, ldc, ld_add, ld_sa, ld_sb, stride_a, stride_b, stride_c, stride_add, stride_bias, stride_sa, stride_sb;
   int M, N, K, batch, type, shift_a, shift_b;  // shift: 7 where 128 rows share a scale
-  int k_chunk, splits, tiles_m, tiles_n;
-  int64_t groups;
+  int k_chunk, splits;
+  uint32_t groups, run, rest;  // work-groups; a die's of them (rest: how many dies have one more)
+  Divisor by_n, by_m, by_splits;
 };
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* p, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
+// One wave instruction: lane L's SIZE bytes at byte offset `at` of the `bytes` from p on land at lds + SIZE L; what lies behind them arrives as zero.  Written as an
+// instruction because the compiler holds every read of LDS up until all such requests have arrived; whoever reads what this brings waits for it (arrived()).
+template <int SIZE>
+__device__ __forceinline__ void request_to_lds(const void* p, uint32_t bytes, const void* lds, uint32_t at) {
+  typedef uint32_t rsrc_t __attribute__((ext_vector_type(4)));
+  const uint64_t base = (uint64_t)p;
+  const rsrc_t rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, bytes, 0x00020000u};
+  const uint32_t to = (uint32_t)(uintptr_t)(lds_void_ptr)lds;
+  if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(rsrc), "s"(to) : "memory");
+  else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(at), "s"(rsrc), "s"(to) : "memory");
+}
+// All of a wavefront's requests and reads of LDS have arrived; with the barrier behind it, all wavefronts'.
+__device__ __forceinline__ void arrived() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // An operand's tile: R rows of 128 bytes in LDS, chunk p of 16 bytes of row r at p ^ (r >> 1 & 7), so that the 16 rows that a read touches lie on all banks.
@@ -43,28 +58,40 @@ template <int R, int NW>
 struct Operand {
   static constexpr int BYTES = R * BK, NV = R / (8 * NW);  // wave instructions of a wavefront and stage
   static_assert(NV >= 1, "");
-  const uint8_t* base;  // of the tile's first row, k = 0
-  int64_t ld;
-  int rows, K, wave;
+  const uint8_t* at;  // of this wavefront's first row, k = 0
+  int64_t step;       // bytes from one wave instruction's rows to the next's
+  int extent[NV];     // bytes from an instruction's first row to the end of 128 bytes of its last; 0: there is none
+  int wave;
   uint32_t voff, chunk;
-  __device__ __forceinline__ void init(const uint8_t* first, int64_t ld_, int rows_, int K_) {
-    base = first, ld = ld_, rows = rows_, K = K_;
-    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __device__ __forceinline__ void init(const uint8_t* first, int64_t ld, int rows, int wave_) {
+    wave = wave_;
     const int lane = threadIdx.x & 63, row = lane >> 3;
     chunk = ((lane & 7) ^ (((8 * wave + row) >> 1) & 7)) * 16;
     voff = (uint32_t)(row * ld) + chunk;
+    at = first + 8 * wave * ld;
+    step = 8 * NW * ld;
+#pragma unroll
+    for (int it = 0; it < NV; ++it) {
+      const int left = min(rows - 8 * (wave + NW * it), 8);
+      extent[it] = left > 0 ? (left - 1) * (int)ld + BK : 0;
+    }
   }
-  __device__ __forceinline__ void request(unsigned char* stage, int k, int it) const {
-    const int r0 = 8 * (wave + NW * it), left = min(rows - r0, 8), k_left = K - k;
+  // k_left: of the whole contraction from k on
+  __device__ __forceinline__ void request(unsigned char* stage, int k, int k_left, int it) const {
     // (to the end of the 16 bytes in which the last row's last code lies)
-    const uint32_t bytes = left > 0 && k_left > 0 ? (uint32_t)((left - 1) * ld) + (uint32_t)((min(k_left, BK) + 15) & ~15) : 0u;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(base + r0 * ld + k, bytes), (lds_void_ptr)(stage + (wave + NW * it) * 1024), 16,
-                                             (int)((int)chunk < k_left ? voff : kOob), 0, 0, 0);
+    const int cut = BK - min(max((k_left + 15) & ~15, 0), BK), bytes = k_left > 0 ? max(extent[it] - cut, 0) : 0;
+    int w = wave;
+    asm volatile("" : "+s"(w));  // (all of these addresses ahead of the loop would fill the scalar registers)
+    request_to_lds<16>(at + it * step + k, (uint32_t)bytes, stage + (w + NW * it) * 1024, (int)chunk < k_left ? voff : kOob);
   }
-  __device__ __forceinline__ static frag_t fragment(const unsigned char* stage, int row0, int lane) {
-    const int row = row0 + (lane & 15), s = (row >> 1) & 7, g = lane >> 4;
-    const code4_t lo = *reinterpret_cast<const code4_t*>(stage + row * BK + ((g ^ s) << 4));
-    const code4_t hi = *reinterpret_cast<const code4_t*>(stage + row * BK + (((g + 4) ^ s) << 4));
+  // Where a lane reads its part of the fragment of 16 rows; rows 16 on lie 16 * BK on.
+  __device__ __forceinline__ static int fragment_at(int row0, int lane) {
+    const int row = row0 + (lane & 15);
+    return row * BK + (((lane >> 4) ^ ((row >> 1) & 7)) << 4);
+  }
+  __device__ __forceinline__ static frag_t fragment(const unsigned char* stage, int at, int i) {
+    const code4_t lo = *reinterpret_cast<const code4_t*>(stage + at + i * 16 * BK);
+    const code4_t hi = *reinterpret_cast<const code4_t*>(stage + (at ^ 64) + i * 16 * BK);
     return frag_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   }
   // The codes behind K of the 16 bytes in which K ends become zero: they belong to nobody.
@@ -80,31 +107,47 @@ struct Operand {
   }
 };
 
-// Scales of R rows for one block of k, in LDS; 64 to a wave instruction.
-template <int R>
-__device__ __forceinline__ void request_scales(const float* s, int64_t ld, int shift, int row0, int rows, int block, bool there, float* lds, int part) {
-  const int lane = threadIdx.x & 63, r = 64 * part + lane;
-  const uint32_t at = (uint32_t)(((row0 + r) >> shift) - (row0 >> shift)) * 4u;
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(s + block * ld + (row0 >> shift), there ? 4u * R : 0u), (lds_void_ptr)(lds + 64 * part), 4,
-                                           (int)(r < rows ? at : kOob), 0, 0, 0);
-}
+// The scales of both operands' rows for one block of k, in LDS, A's first; 64 to a wave instruction, of which a wavefront has one at most.
+template <int BM, int BN, int NW>
+struct Scales {
+  static constexpr int PARTS = (BM + BN) / 64;
+  static_assert(PARTS <= NW, "");
+  const float* at;  // of this wavefront's, block 0
+  int64_t ld;
+  uint32_t voff;
+  int wave;
+  __device__ __forceinline__ void init(const float* sa, int64_t ld_sa, int shift_a, int64_t row_a, int rows_a, const float* sb, int64_t ld_sb, int shift_b,
+                                       int row_b, int rows_b, int wave_) {
+    wave = wave_;
+    const bool of_a = wave < BM / 64;
+    const int r = 64 * (of_a ? wave : wave - BM / 64) + (int)(threadIdx.x & 63), shift = of_a ? shift_a : shift_b;
+    const int64_t row = of_a ? row_a : row_b;
+    at = (of_a ? sa : sb) + (row >> shift);
+    ld = of_a ? ld_sa : ld_sb;
+    voff = r < (of_a ? rows_a : rows_b) ? (uint32_t)(((row + r) >> shift) - (row >> shift)) * 4u : kOob;
+  }
+  __device__ __forceinline__ void request(float* lds, int block, bool there) const {
+    if (wave >= PARTS) return;
+    request_to_lds<4>(at + block * ld, there ? 4u * (BM > BN ? BM : BN) : 0u, lds + 64 * wave, voff);
+  }
+};
 
 // Which tile a work-group takes.
 struct Place {
   int batch, split, m0, n0, rows, first;  // rows of the tile; first row of the expert's range
 };
-__device__ __forceinline__ bool place(const Gemm8Args& g, int64_t id, int BM, int BN, Place& p) {
-  // work-groups go round the eight dies; each gets a contiguous run of tiles
-  const int64_t run = g.groups / 8, rest = g.groups % 8, die = id % 8;
-  int64_t t = die * run + min(die, rest) + id / 8;
-  p.n0 = (int)(t % g.tiles_n) * BN;
-  t /= g.tiles_n;
+__device__ __forceinline__ bool place(const Gemm8Args& g, uint32_t id, int BM, int BN, Place& p) {
+  // work-groups go round the eight dies; each gets a contiguous run of tiles, row by row
+  const uint32_t die = id & 7;
+  uint32_t t = die * g.run + min(die, g.rest) + (id >> 3), col, row, split;
+  t = div_mod(t, g.by_n, col);
+  p.n0 = (int)col * BN;
   p.first = 0;
   if (!g.ranges) {
-    p.m0 = (int)(t % g.tiles_m) * BM;
-    t /= g.tiles_m;
-    p.split = (int)(t % g.splits);
-    p.batch = (int)(t / g.splits);
+    t = div_mod(t, g.by_m, row);
+    p.m0 = (int)row * BM;
+    p.batch = (int)div_mod(t, g.by_splits, split);
+    p.split = (int)split;
     p.rows = min(g.M - p.m0, BM);
     return true;
   }
@@ -114,18 +157,18 @@ __device__ __forceinline__ bool place(const Gemm8Args& g, int64_t id, int BM, in
     first = max(0, min(g.ranges[2 * e], g.M));
     count = max(0, min(g.ranges[2 * e + 1], g.M - first));
   };
-  int64_t mine = 0;
+  uint32_t mine = 0;
   int first, count;
   for (int i = 0; i < per; ++i) {
     const int e = lane * per + i;
     if (e < g.batch) {
       range(e, first, count);
-      mine += (count + BM - 1) / BM;
+      mine += (uint32_t)(count + BM - 1) / BM;
     }
   }
-  int64_t sum = mine;
+  uint32_t sum = mine;
   for (int step = 1; step < 64; step *= 2) {
-    const int64_t up = __shfl_up(sum, step);
+    const uint32_t up = __shfl_up(sum, step);
     sum += lane >= step ? up : 0;
   }
   const uint64_t behind = __ballot(sum > t);
@@ -134,7 +177,7 @@ __device__ __forceinline__ bool place(const Gemm8Args& g, int64_t id, int BM, in
   t -= __shfl(sum - mine, at);
   for (int e = at * per;; ++e) {
     range(e, first, count);
-    const int tiles = (count + BM - 1) / BM;
+    const uint32_t tiles = (uint32_t)(count + BM - 1) / BM;
     if (t < tiles) {
       p.batch = e;
       p.m0 = (int)t * BM;
@@ -190,18 +233,7 @@ __device__ __forceinline__ bf16x8_t widen(int lo, int hi) {
   u.two[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
   return u.all;
 }
-template <bool EXACT>
-struct Codes;
-template <>
-struct Codes<false> {  // as they are
-  frag_t f;
-  __device__ __forceinline__ void set(const frag_t& v) { f = v; }
-  __device__ __forceinline__ floatx4 times(const Codes& o) const {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f, o.f, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-  }
-};
-template <>
-struct Codes<true> {
+struct Codes {
   bf16x8_t f[4];
   __device__ __forceinline__ void set(const frag_t& v) {
 #pragma unroll
@@ -215,71 +247,188 @@ struct Codes<true> {
   }
 };
 
-// BM x BN of C by NW wavefronts, two of them along m.  Results lie transposed in the registers: lane L has row L & 15 of a 16 x 16 tile, columns 4 (L >> 4) to + 3.
-template <int BM, int BN, int NW, bool EXACT>
-__global__ void __launch_bounds__(64 * NW) gemm8_kernel(const Gemm8Args g) {
-  constexpr int WM = BM / 2, WN = BN / (NW / 2), TM = WM / 16, TN = WN / 16;
+// What a work-group needs of its product.
+template <int BM, int BN, int NW>
+struct Product {
+  static constexpr int WM = BM / 2, WN = BN / (NW / 2), TM = WM / 16, TN = WN / 16, STAGE = (BM + BN) * BK;
   using OpA = Operand<BM, NW>;
   using OpB = Operand<BN, NW>;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-  constexpr int STAGE = OpA::BYTES + OpB::BYTES;
-  auto stage = [&](int i) { return lds + i * STAGE; };
-  auto scales = [&](int i) { return reinterpret_cast<float*>(lds + 2 * STAGE) + i * (BM + BN); };
-  touch(g);
-  const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-  Place p;
-  if (id >= g.groups || !place(g, id, BM, BN, p)) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave % 2 * WM, wn = wave / 2 * WN;
-  const int k_begin = p.split * g.k_chunk, k_end = min(g.K, k_begin + g.k_chunk);
-  const int cols = min(g.N - p.n0, BN);
-  const int64_t row0 = (int64_t)p.first + p.m0;
   OpA a;
   OpB b;
-  a.init(g.a + (g.ranges ? 0 : p.batch * g.stride_a) + row0 * g.lda, g.lda, p.rows, k_end);
-  b.init(g.b + p.batch * g.stride_b + p.n0 * g.ldb, g.ldb, cols, k_end);
-  const float *sa = g.sa + (g.ranges ? 0 : p.batch * g.stride_sa), *sb = g.sb + p.batch * g.stride_sb;
-  auto request = [&](int s, int k) {
+  Scales<BM, BN, NW> s;
+  int wave, lane, wm, wn, k_begin, k_end;
+  int64_t row0;
+  __device__ __forceinline__ void init(const Gemm8Args& g, const Place& p) {
+    lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    wm = wave % 2 * WM, wn = wave / 2 * WN;
+    k_begin = p.split * g.k_chunk, k_end = min(g.K, k_begin + g.k_chunk);
+    row0 = (int64_t)p.first + p.m0;
+    const int64_t own = g.ranges ? 0 : p.batch;
+    const int cols = min(g.N - p.n0, BN);
+    a.init(g.a + own * g.stride_a + row0 * g.lda, g.lda, p.rows, wave);
+    b.init(g.b + p.batch * g.stride_b + p.n0 * g.ldb, g.ldb, cols, wave);
+    s.init(g.sa + own * g.stride_sa, g.ld_sa, g.shift_a, row0, p.rows, g.sb + p.batch * g.stride_sb, g.ld_sb, g.shift_b, p.n0, cols, wave);
+  }
+  static constexpr int REQUESTS = OpA::NV + OpB::NV + 1;
+  __device__ __forceinline__ void request(unsigned char* stage, float* scales, int k, int q) const {
+    const int left = k_end - k;
+    if (q < OpA::NV) a.request(stage, k, left, q);
+    else if (q < OpA::NV + OpB::NV) b.request(stage + OpA::BYTES, k, left, q - OpA::NV);
+    else s.request(scales, k / BK, left > 0);
+  }
+  __device__ __forceinline__ void request_all(unsigned char* stage, float* scales, int k) const {
 #pragma unroll
-    for (int it = 0; it < OpA::NV; ++it) a.request(stage(s), k, it);
-#pragma unroll
-    for (int it = 0; it < OpB::NV; ++it) b.request(stage(s) + OpA::BYTES, k, it);
-    for (int part = wave; part < (BM + BN) / 64; part += NW) {
-      if (part < BM / 64) request_scales<BM>(sa, g.ld_sa, g.shift_a, (int)row0, p.rows, k / BK, k < k_end, scales(s), part);
-      else request_scales<BN>(sb, g.ld_sb, g.shift_b, p.n0, cols, k / BK, k < k_end, scales(s) + BM, part - BM / 64);
-    }
-  };
-  auto arrived = [&](int s, int k) {
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (k_end - k < BK && k_end - k > 0 && (k_end & 15)) {
-      OpA::clear_tail(stage(s), k_end - k);
-      OpB::clear_tail(stage(s) + OpA::BYTES, k_end - k);
+    for (int q = 0; q < REQUESTS; ++q) request(stage, scales, k, q);
+  }
+  // Behind the barrier that publishes a stage.
+  __device__ __forceinline__ void tail(unsigned char* stage, int k) const {
+    const int left = k_end - k;
+    if (left > 0 && left < BK && (left & 15)) {
+      OpA::clear_tail(stage, left);
+      OpB::clear_tail(stage + OpA::BYTES, left);
       __syncthreads();
     }
-  };
+  }
+};
+
+// Codes as they are.  Results lie transposed in the registers: lane L has row L & 15 of a 16 x 16 tile, columns 4 (L >> 4) to + 3.
+//
+// A wavefront has TM strips of 16 rows and TN columns of tiles.  B's fragments of a block of k stay in registers, A's pass through G of them.  The first strips are multiplied one after the
+// other; then comes the barrier behind which the stage is free and the next one is there, and the last G strips are multiplied column by column, so that one of B's fragments after the other is done
+// with and can be fetched for the next block long before it is needed.  What a matrix instruction leaves is multiplied by its scales and added up LAG instructions later, which is the
+// vector units' work beside the matrix units'.  The requests for the block after next are spread over the last strips.
+// BFINE: B's rows have a scale each; else the wavefront's columns share one.
+template <int BM, int BN, int NW, bool BFINE>
+struct Strips : Product<BM, BN, NW> {
+  using P = Product<BM, BN, NW>;
+  using typename P::OpA;
+  using typename P::OpB;
+  static constexpr int TM = P::TM, TN = P::TN, G = TM < 3 ? TM : 3, ROWS = TM - G, SLOTS = TM * TN, LAG = 3, RING = 4;
+  static_assert(SLOTS % RING == 0, "");
+  static_assert(P::WN <= BK, "a wavefront's columns share a scale");
+  float acc[TM][TN][4];  // (apart, so that each is added to where it is)
+  floatx4 t[RING];
+  frag_t fa[G], fb[TN];
+  float sm[G], sn[BFINE ? 1 : 2];
+  float4 sn4[BFINE ? TN : 1];
+  floatx4 by4[BFINE ? RING : 1];
+  float by[BFINE ? 1 : RING];
+  int at_a, at_b, at_sm, at_sn;
+
+  static constexpr int strip_of(int g) {  // of the last strips the one in register g
+    for (int i = ROWS; i < TM; ++i)
+      if (i % G == g) return i;
+    return 0;
+  }
+  static constexpr int slot_i(int q) { return q < ROWS * TN ? q / TN : strip_of((q - ROWS * TN) % G); }
+  static constexpr int slot_j(int q) { return q < ROWS * TN ? q % TN : (q - ROWS * TN) / G; }
+
+  __device__ __forceinline__ void start() {
+    at_a = OpA::fragment_at(this->wm, this->lane), at_b = OpA::BYTES + OpB::fragment_at(this->wn, this->lane);
+    at_sm = this->wm + (this->lane & 15), at_sn = BM + this->wn + 4 * (this->lane >> 4);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.f;
+#pragma unroll
+    for (int r = 0; r < RING; ++r) {
+      t[r] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (BFINE) by4[r] = t[r];
+      else by[r] = 0.f;
+    }
+  }
+  __device__ __forceinline__ void fetch_a(const unsigned char* stage, const float* scales, int i) {
+    fa[i % G] = OpA::fragment(stage, at_a, i);
+    sm[i % G] = scales[at_sm + 16 * i];
+  }
+  __device__ __forceinline__ void fetch_b(const unsigned char* stage, const float* scales, int j) {
+    fb[j] = OpB::fragment(stage, at_b, j);
+    if constexpr (BFINE) sn4[j] = *reinterpret_cast<const float4*>(scales + at_sn + 16 * j);
+  }
+  __device__ __forceinline__ void first(const unsigned char* stage, const float* scales) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fetch_b(stage, scales, j);
+    if constexpr (!BFINE) sn[0] = scales[BM + this->wn];
+#pragma unroll
+    for (int i = 0; i < G; ++i) fetch_a(stage, scales, i);
+  }
+  __device__ __forceinline__ void add(int q) {  // the sums of slot q, of this block or (q < 0) the one before
+    const int slot = (q + SLOTS) % SLOTS, r = (q + SLOTS) % RING;
+    float(&c)[4] = acc[slot_i(slot)][slot_j(slot)];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = __builtin_fmaf(t[r][e], BFINE ? by4[BFINE ? r : 0][e] : by[BFINE ? 0 : r], c[e]);
+    asm volatile("" : "+v"(c[0]), "+v"(c[1]), "+v"(c[2]), "+v"(c[3]));  // (here and not behind a branch)
+  }
+  // One block of k from stage `from`; the next is in or on its way to `to`, the one after goes to `from`.
+  __device__ __forceinline__ void block(unsigned char* from, float* scales_from, unsigned char* to, float* scales_to, int k) {
+#pragma unroll
+    for (int q = 0; q < SLOTS; ++q) {
+      if (q == ROWS * TN) {
+        arrived();  // (the next stage's requests, this one's fragments)
+        this->tail(to, k + BK);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!BFINE) sn[1] = scales_to[BM + this->wn];
+      }
+      const int i = slot_i(q), j = slot_j(q), r = q % RING;
+      t[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i % G], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+      if constexpr (BFINE) by4[r] = floatx4{sn4[j].x * sm[i % G], sn4[j].y * sm[i % G], sn4[j].z * sm[i % G], sn4[j].w * sm[i % G]};
+      else by[r] = sm[i % G] * sn[0];
+      add(q - LAG);
+      __builtin_amdgcn_sched_barrier(0);
+      if (q < ROWS * TN) {
+        if (j == TN - 1) fetch_a(from, scales_from, i + G);
+      } else {
+        const int c = q - ROWS * TN, n = G * TN;
+        if (j == TN - 1) fetch_a(to, scales_to, c % G);
+        if (c % G == G - 1) fetch_b(to, scales_to, j);
+#pragma unroll
+        for (int x = c * P::REQUESTS / n; x < (c + 1) * P::REQUESTS / n; ++x) this->request(from, scales_from, k + 2 * BK, x);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (!BFINE) sn[0] = sn[1];
+  }
+  __device__ __forceinline__ void run(unsigned char* stages, float* scales) {
+    start();
+    this->request_all(stages, scales, this->k_begin);
+    __builtin_amdgcn_sched_barrier(0);
+    this->request_all(stages + P::STAGE, scales + BM + BN, this->k_begin + BK);
+    arrived();
+    this->tail(stages, this->k_begin);
+    first(stages, scales);
+    int s = 0;
+    for (int k = this->k_begin; k < this->k_end; k += BK, s ^= 1)
+      block(stages + s * P::STAGE, scales + s * (BM + BN), stages + (s ^ 1) * P::STAGE, scales + (s ^ 1) * (BM + BN), k);
+#pragma unroll
+    for (int q = -LAG; q < 0; ++q) add(q);
+    arrived();  // (requests past the end, of nothing, which write zeros)
+  }
+};
+
+// Codes as bf16, for results in fp32.
+template <int BM, int BN, int NW, bool BFINE>
+struct Wide : Product<BM, BN, NW> {
+  using P = Product<BM, BN, NW>;
+  using typename P::OpA;
+  using typename P::OpB;
+  static constexpr int TM = P::TM, TN = P::TN;
   floatx4 acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  request(0, k_begin);
-  arrived(0, k_begin);
-  int s = 0;
-  for (int k = k_begin; k < k_end; k += BK, s ^= 1) {
-    if (k + BK < k_end) request(s ^ 1, k + BK);
-    Codes<EXACT> fb[TN];
+  __device__ __forceinline__ void block(const unsigned char* stage, const float* scales) {
+    const int at_a = OpA::fragment_at(this->wm, this->lane), at_b = OpA::BYTES + OpB::fragment_at(this->wn, this->lane);
+    Codes fb[TN];
     float4 sn[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      fb[j].set(OpB::fragment(stage(s) + OpA::BYTES, wn + 16 * j, lane));
-      sn[j] = *reinterpret_cast<const float4*>(scales(s) + BM + wn + 16 * j + 4 * (lane >> 4));
+      fb[j].set(OpB::fragment(stage, at_b, j));
+      sn[j] = *reinterpret_cast<const float4*>(scales + BM + this->wn + 16 * j + 4 * (this->lane >> 4));
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      Codes<EXACT> fa;
-      fa.set(OpA::fragment(stage(s), wm + 16 * i, lane));
-      const float sm = scales(s)[wm + 16 * i + (lane & 15)];
+      Codes fa;
+      fa.set(OpA::fragment(stage, at_a, i));
+      const float sm = scales[this->wm + 16 * i + (this->lane & 15)];
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         const floatx4 t = fb[j].times(fa);
@@ -289,35 +438,152 @@ __global__ void __launch_bounds__(64 * NW) gemm8_kernel(const Gemm8Args g) {
         acc[i][j][3] = __builtin_fmaf(t[3], sn[j].w * sm, acc[i][j][3]);
       }
     }
-    arrived(s ^ 1, k + BK);
   }
+  __device__ __forceinline__ void run(unsigned char* stages, float* scales) {
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int m = wm + 16 * i + (lane & 15);
-    if (m >= p.rows) continue;
-    const int64_t row = row0 + m;
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int n = p.n0 + wn + 16 * j + 4 * (lane >> 4);
-      if (n >= g.N) continue;
-      if (g.partial) {
-        float* to = g.partial + (((int64_t)p.batch * g.splits + p.split) * g.M + row) * g.N + n;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < g.N) to[e] = acc[i][j][e];
-        continue;
-      }
-      auto out = [&](auto type) {
-        using T = decltype(type);
-        const int64_t own = g.ranges ? 0 : p.batch;
-        store4<T>(g, static_cast<T*>(g.c) + own * g.stride_c, g.bias ? static_cast<const T*>(g.bias) + p.batch * g.stride_bias : nullptr,
-                  g.add ? static_cast<const T*>(g.add) + own * g.stride_add : nullptr, row, n, acc[i][j]);
-      };
-      if (g.type == NMT_F16) out(half_t());
-      else if (g.type == NMT_BF16) out(bf16_t());
-      else out(float());
+      for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    this->request_all(stages, scales, this->k_begin);
+    arrived();
+    this->tail(stages, this->k_begin);
+    int s = 0;
+    for (int k = this->k_begin; k < this->k_end; k += BK, s ^= 1) {
+      this->request_all(stages + (s ^ 1) * P::STAGE, scales + (s ^ 1) * (BM + BN), k + BK);
+      __builtin_amdgcn_sched_barrier(0);
+      block(stages + s * P::STAGE, scales + s * (BM + BN));
+      arrived();
+      this->tail(stages + (s ^ 1) * P::STAGE, k + BK);
     }
   }
+};
+
+// A wavefront's share of C: strips of 16 rows turn round in LDS, so that lanes write 16 bytes each and a row's lie side by side.
+template <typename Loop, typename T>
+struct Result {
+  static constexpr int TM = Loop::TM, TN = Loop::TN, WN = Loop::WN, E = 16 / sizeof(T), LANES = WN / E, ROWS = 64 / LANES, N = 16 / ROWS, PITCH = WN + 4;
+  static constexpr int FLOATS = 16 * PITCH;
+  static_assert(N >= 1 && FLOATS * 4 * (Loop::STAGE == 512 * BK ? 8 : 4) <= 2 * Loop::STAGE, "");
+  typedef T vec __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+  typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  T* c;
+  const T* add;
+  int64_t ldc, ld_add;
+  int left, rows, row;  // columns from this lane's on; rows of the strips from the first on; this lane's of them
+  float bias[TN][4];
+  vec next[N];
+  __device__ __forceinline__ Result(const Loop& l, T* c_, int64_t ldc_, const T* bias_, const T* add_, int64_t ld_add_, const Place& p, int cols) {
+    const int n0 = p.n0 + l.wn, col = l.lane % LANES * E;
+    row = l.lane / LANES;
+    left = cols - n0 - col;
+    rows = p.rows - l.wm;
+    ldc = ldc_, ld_add = ld_add_;
+    const int64_t first = l.row0 + l.wm + row;
+    c = c_ + first * ldc + n0 + col;
+    add = add_ ? add_ + first * ld_add + n0 + col : nullptr;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int n = n0 + 16 * j + 4 * (l.lane >> 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bias[j][e] = 0.f;
+      if (bias_) {
+        if (cols >= 4) {  // (columns behind the last go nowhere: the last four's are as good)
+          const int at = min(n, cols - 4);
+          const four b = *reinterpret_cast<const four*>(bias_ + at);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int o = 0; o < 4; ++o) bias[j][e] = n + e == at + o ? (float)b[o] : bias[j][e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) bias[j][e] = (float)bias_[min(n + e, cols - 1)];
+        }
+      }
+    }
+    if (add) ask(0);
+  }
+  __device__ __forceinline__ void ask(int i) {
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      const T* from = add + (16 * i + ROWS * x) * ld_add;
+      if (16 * i + ROWS * x + row >= rows) continue;
+      if (left >= E) {
+        next[x] = *reinterpret_cast<const vec*>(from);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (e < left) next[x][e] = from[e];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(const Loop& l, float* turn) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      vec plus[N];
+#pragma unroll
+      for (int x = 0; x < N; ++x) plus[x] = next[x];
+      if (add && i + 1 < TM) ask(i + 1);
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        *reinterpret_cast<float4*>(turn + (l.lane & 15) * PITCH + 16 * j + 4 * (l.lane >> 4)) =
+            float4{l.acc[i][j][0] + bias[j][0], l.acc[i][j][1] + bias[j][1], l.acc[i][j][2] + bias[j][2], l.acc[i][j][3] + bias[j][3]};
+      wave_sync();
+#pragma unroll
+      for (int x = 0; x < N; ++x) {
+        float v[E];
+        const float* from = turn + (ROWS * x + row) * PITCH + l.lane % LANES * E;
+#pragma unroll
+        for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(v + e) = *reinterpret_cast<const float4*>(from + e);
+        vec o;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = (T)(add ? v[e] + (float)plus[x][e] : v[e]);
+        if (16 * i + ROWS * x + row >= rows) continue;
+        T* to = c + (16 * i + ROWS * x) * ldc;
+        if (left >= E) {
+          *reinterpret_cast<vec*>(to) = o;
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (e < left) to[e] = o[e];
+        }
+      }
+      wave_sync();
+    }
+  }
+};
+
+// BM x BN of C by NW wavefronts, two of them along m.
+template <int BM, int BN, int NW, bool BFINE, bool WIDE>
+__global__ void __launch_bounds__(64 * NW, 2) gemm8_kernel(const Gemm8Args g) {
+  using Loop = std::conditional_t<WIDE, Wide<BM, BN, NW, BFINE>, Strips<BM, BN, NW, BFINE>>;
+  constexpr int TM = Loop::TM, TN = Loop::TN;
+  __shared__ __attribute__((aligned(1024))) unsigned char stages[2 * Loop::STAGE];
+  __shared__ __attribute__((aligned(16))) float scales[2 * (BM + BN)];
+  touch(g);
+  const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
+  Place p;
+  if (id >= g.groups || !place(g, id, BM, BN, p)) return;
+  // (the same for all lanes, which the compiler does not see)
+  for (int* v : {&p.batch, &p.split, &p.m0, &p.n0, &p.rows, &p.first}) *v = __builtin_amdgcn_readfirstlane(*v);
+  Loop l;
+  l.init(g, p);
+  l.run(stages, scales);
+  float* turn = reinterpret_cast<float*>(stages) + l.wave * Result<Loop, float>::FLOATS;
+  const int64_t own = g.ranges ? 0 : p.batch;
+  if (g.partial) {
+    Result<Loop, float> r(l, g.partial + ((int64_t)p.batch * g.splits + p.split) * g.M * g.N, g.N, nullptr, nullptr, 0, p, g.N);
+    r.store(l, turn);
+    return;
+  }
+  auto out = [&](auto type) {
+    using T = decltype(type);
+    Result<Loop, T> r(l, static_cast<T*>(g.c) + own * g.stride_c, g.ldc, g.bias ? static_cast<const T*>(g.bias) + p.batch * g.stride_bias : nullptr,
+                      g.add ? static_cast<const T*>(g.add) + own * g.stride_add : nullptr, g.ld_add, p, g.N);
+    r.store(l, turn);
+  };
+  if constexpr (WIDE) out(float());
+  else if (g.type == NMT_F16) out(half_t());
+  else out(bf16_t());
 }
 
 // The pieces' sums in increasing k, and what comes behind a product.
@@ -339,14 +605,12 @@ __global__ void __launch_bounds__(256) gemm8_sums_kernel(const Gemm8Args g) {
 }
 
 struct Plan {
-  int tile, splits;  // tile: 256, 128 or 64
+  int tile, splits;  // tile: 128 or 64
 };
 Plan plan(int M, int N, int K, int batch, bool ranges) {
   auto tiles = [&](int t) { return ((int64_t)ceil_div(M, t) + (ranges ? batch : 0)) * ceil_div(N, t) * (ranges ? 1 : batch); };
   const int cus = 256;
-  Plan p = {64, 1};
-  if (tiles(256) >= cus) p.tile = 256;
-  else if (tiles(128) >= cus) p.tile = 128;
+  Plan p = {tiles(128) >= cus ? 128 : 64, 1};
   if (!ranges && tiles(p.tile) < cus) {
     const int blocks = ceil_div(K, BK);
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(blocks / 8, 2 * cus / std::max<int64_t>(1, tiles(p.tile))));
@@ -354,15 +618,15 @@ Plan plan(int M, int N, int K, int batch, bool ranges) {
   return p;
 }
 
-template <int BM, int BN, int NW, bool EXACT>
+template <int BM, int BN, int NW, bool WIDE>
 int launch_tiles(Gemm8Args g, hipStream_t stream) {
-  g.tiles_m = ceil_div(g.M, BM), g.tiles_n = ceil_div(g.N, BN);
-  g.groups = g.ranges ? ((int64_t)g.tiles_m + g.batch) * g.tiles_n : (int64_t)g.tiles_m * g.tiles_n * g.splits * g.batch;
-  const dim3 grid((uint32_t)std::min<int64_t>(g.groups, kGridX), (uint32_t)((g.groups + kGridX - 1) / kGridX));
-  constexpr size_t kLds = 2 * (BM + BN) * (BK + 4);
-  if (kLds > (64 << 10))
-    if (const int rc = allow_lds(reinterpret_cast<const void*>(gemm8_kernel<BM, BN, NW, EXACT>), kLds)) return rc;
-  hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, EXACT>), grid, dim3(64 * NW), kLds, stream, g);
+  const int64_t tiles_m = ceil_div(g.M, BM), tiles_n = ceil_div(g.N, BN);
+  const int64_t groups = g.ranges ? (tiles_m + g.batch) * tiles_n : tiles_m * tiles_n * g.splits * g.batch;
+  g.groups = (uint32_t)groups, g.run = g.groups / 8, g.rest = g.groups % 8;
+  g.by_n = divisor((uint32_t)tiles_n), g.by_m = divisor((uint32_t)tiles_m), g.by_splits = divisor((uint32_t)g.splits);
+  const dim3 grid((uint32_t)std::min<int64_t>(groups, kGridX), (uint32_t)((groups + kGridX - 1) / kGridX));
+  if (!WIDE && g.shift_b) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, WIDE>), grid, dim3(64 * NW), 0, stream, g);
+  else if constexpr (BM < 256) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, true, WIDE>), grid, dim3(64 * NW), 0, stream, g);
   NMT_LAUNCH_CHECK();
   return NMT_OK;
 }
@@ -370,7 +634,7 @@ int launch_tiles(Gemm8Args g, hipStream_t stream) {
 int check_sizes(const char* who, int M, int N, int K, int batch) {
   NMT_REQUIRE(M >= 0 && M <= kMaxSize && N >= 0 && N <= kMaxSize && K >= 0 && K <= kMaxSize, "%s: a product of %d x %d x %d", who, M, N, K);
   NMT_REQUIRE(batch >= 0 && batch <= kMaxBatch, "%s: %d products, at most %d", who, batch, kMaxBatch);
-  NMT_REQUIRE(((int64_t)ceil_div(M, 64) + batch) * ceil_div(N, 64) <= (1ll << 40), "%s: a product of %d x %d is too large", who, M, N);
+  NMT_REQUIRE((double)(ceil_div(M, 64) + 1) * ceil_div(N, 64) * std::max(batch, 1) < 1e9, "%s: %d products of %d x %d are too large", who, batch, M, N);
   return NMT_OK;
 }
 
@@ -422,8 +686,9 @@ extern "C" int nmt_op_gemm8(const nmt_gemm8* p, void* stream_) {
   g.splits = how.splits, g.k_chunk = ceil_div(ceil_div(p->K, BK), how.splits) * BK;
   g.partial = how.splits > 1 ? p->d_scratch : nullptr;
   int rc;
+  const int64_t large = ((int64_t)ceil_div(g.M, 256) + (g.ranges ? g.batch : 0)) * ceil_div(g.N, 256) * (g.ranges ? 1 : g.batch);
   if (g.type == NMT_F32) rc = how.tile >= 128 ? launch_tiles<128, 128, 4, true>(g, stream) : launch_tiles<64, 64, 4, true>(g, stream);
-  else rc = how.tile == 256 ? launch_tiles<256, 256, 8, false>(g, stream) : how.tile == 128 ? launch_tiles<128, 128, 4, false>(g, stream) : launch_tiles<64, 64, 4, false>(g, stream);
+  else rc = large >= 256 && g.shift_b ? launch_tiles<256, 256, 8, false>(g, stream) : how.tile == 128 ? launch_tiles<128, 128, 4, false>(g, stream) : launch_tiles<64, 64, 4, false>(g, stream);
   if (rc != NMT_OK || !g.partial) return rc;
   const int64_t groups = ((int64_t)g.batch * g.M * ((g.N + 3) / 4) + 255) / 256;
   const dim3 grid((uint32_t)std::min<int64_t>(groups, kGridX), (uint32_t)((groups + kGridX - 1) / kGridX));
