@@ -525,7 +525,7 @@ int nmt_op_norm8(const nmt_norm8* a /*host*/, void* stream);
  * d_ranges NULL: `batch` products of M x N x K each.  Otherwise d_ranges [batch, 2] (nmt_op_expert_dispatch): expert e's rows are the ranges[e, 1] rows of A, of the scales and of C from ranges[e, 0] on, M is
  * the number of rows of A and C in all, its B, scales of B and bias lie e strides on, the other strides are not used, and a_square is 0.  Rows that no expert has are left as they
  * were; ranges do not overlap, and what of them lies outside [0, M) is cut off.
- * Rows of A and B begin at multiples of 16 bytes; C, bias and add have any address that their type allows and any distance.  K = 0: bias + add.  batch <= 1024; lda, ldb <= 2^27.
+ * Rows of A and B begin at multiples of 16 bytes; C, bias and add have any address that their type allows and any distance.  K = 0: bias + add.  batch <= 1024; lda, ldb <= 2^22.
  * d_scratch: 16-byte aligned, scratch_floats >= nmt_op_gemm8_scratch(M, N, K, batch, ranges != NULL), which may be 0. */
 typedef struct nmt_gemm8 {
   int32_t M, N, K, batch, type, a_square, b_square;

@@ -11,11 +11,12 @@
 namespace {
 
 constexpr int kMaxSize = 0x7FFFFFFF - 65536;
-constexpr int64_t kMaxLd = 1 << 27;      // bytes from row to row: eight rows within 32-bit offsets
+constexpr int64_t kMaxLd = 1 << 22;      // bytes from row to row: a tile's rows within 31-bit offsets
 constexpr int kMaxBatch = 1024;
 constexpr uint32_t kOob = 0x80000000u;   // a byte offset that no operand reaches: such loads return 0
 constexpr int BK = kBlock8;              // bytes of a row of a stage
 constexpr int kGridX = 1 << 21;
+constexpr int kPatch = 4;                // rows of tiles that are swept together, column by column
 
 typedef int frag_t __attribute__((ext_vector_type(8)));  // 32 codes of a lane
 typedef __attribute__((address_space(3))) void* lds_void_ptr;
@@ -31,19 +32,28 @@ struct Gemm8Args {
   int M, N, K, batch, type, shift_a, shift_b;  // shift: 7 where 128 rows share a scale
   int k_chunk, splits;
   uint32_t groups, run, rest;  // work-groups; a die's of them (rest: how many dies have one more)
-  Divisor by_n, by_m, by_splits;
+  int tiles_m;
+  Divisor by_n, by_tiles, by_splits, by_patch, by_rows, by_last;  // columns of tiles; tiles; ...; tiles of kPatch rows; kPatch, and what is left of rows behind the last whole patch
 };
 
-// One wave instruction: lane L's SIZE bytes at byte offset `at` of the `bytes` from p on land at lds + SIZE L; what lies behind them arrives as zero.  Written as an
-// instruction because the compiler holds every read of LDS up until all such requests have arrived; whoever reads what this brings waits for it (arrived()).
+// A stretch of memory that wave instructions read from; what lies behind it arrives as zero.
+struct Stretch {
+  uint64_t base;  // (no address has more than 48 bits)
+  uint32_t bytes;
+};
+__device__ __forceinline__ Stretch stretch(const void* p, uint32_t bytes) {
+  auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+  return Stretch{(uint64_t)scalar((uint32_t)((uint64_t)p >> 32)) << 32 | scalar((uint32_t)(uint64_t)p), scalar(bytes)};
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_void_ptr)p; }
+// One wave instruction: lane L's SIZE bytes at byte offset `at` land at lds + SIZE L.  Written as an instruction because the compiler holds every read of LDS up until all such
+// requests have arrived; whoever reads what this brings waits for it (arrived()).
 template <int SIZE>
-__device__ __forceinline__ void request_to_lds(const void* p, uint32_t bytes, const void* lds, uint32_t at) {
+__device__ __forceinline__ void request_to_lds(const Stretch& from, uint32_t lds, uint32_t at) {
   typedef uint32_t rsrc_t __attribute__((ext_vector_type(4)));
-  const uint64_t base = (uint64_t)p;
-  const rsrc_t rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, bytes, 0x00020000u};
-  const uint32_t to = (uint32_t)(uintptr_t)(lds_void_ptr)lds;
-  if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(rsrc), "s"(to) : "memory");
-  else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(at), "s"(rsrc), "s"(to) : "memory");
+  const rsrc_t s = {(uint32_t)from.base, (uint32_t)(from.base >> 32), from.bytes, 0x00020000u};
+  if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(s), "s"(lds) : "memory");
+  else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(at), "s"(s), "s"(lds) : "memory");
 }
 // All of a wavefront's requests and reads of LDS have arrived; with the barrier behind it, all wavefronts'.
 __device__ __forceinline__ void arrived() {
@@ -53,36 +63,31 @@ __device__ __forceinline__ void arrived() {
 }
 
 // An operand's tile: R rows of 128 bytes in LDS, chunk p of 16 bytes of row r at p ^ (r >> 1 & 7), so that the 16 rows that a read touches lie on all banks.
-// One wave instruction brings eight rows; its descriptor starts where it reads and ends with the rows, so what lies behind them arrives as zero.
+// One wave instruction brings eight rows.  The stretch that it reads from begins with the tile's first row at the block of k at hand and ends with the last code of its last row
+// (with the 16 bytes in which that lies).
 template <int R, int NW>
 struct Operand {
   static constexpr int BYTES = R * BK, NV = R / (8 * NW);  // wave instructions of a wavefront and stage
   static_assert(NV >= 1, "");
-  const uint8_t* at;  // of this wavefront's first row, k = 0
-  int64_t step;       // bytes from one wave instruction's rows to the next's
-  int extent[NV];     // bytes from an instruction's first row to the end of 128 bytes of its last; 0: there is none
-  int wave;
-  uint32_t voff, chunk;
-  __device__ __forceinline__ void init(const uint8_t* first, int64_t ld, int rows, int wave_) {
-    wave = wave_;
-    const int lane = threadIdx.x & 63, row = lane >> 3;
-    chunk = ((lane & 7) ^ (((8 * wave + row) >> 1) & 7)) * 16;
-    voff = (uint32_t)(row * ld) + chunk;
-    at = first + 8 * wave * ld;
-    step = 8 * NW * ld;
+  Stretch at;
+  uint32_t voff[NV];
+  int chunk;
+  __device__ __forceinline__ void init(const uint8_t* first, int64_t ld, int rows, int k_left, int wave) {
+    const int lane = threadIdx.x & 63, row = 8 * wave + (lane >> 3);
+    chunk = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
+    at = stretch(first, (uint32_t)((rows - 1) * ld) + (uint32_t)((max(k_left, 0) + 15) & ~15));
 #pragma unroll
-    for (int it = 0; it < NV; ++it) {
-      const int left = min(rows - 8 * (wave + NW * it), 8);
-      extent[it] = left > 0 ? (left - 1) * (int)ld + BK : 0;
-    }
+    for (int it = 0; it < NV; ++it) voff[it] = row + 8 * NW * it < rows ? (uint32_t)((row + 8 * NW * it) * ld) + (uint32_t)chunk : kOob;
   }
-  // k_left: of the whole contraction from k on
-  __device__ __forceinline__ void request(unsigned char* stage, int k, int k_left, int it) const {
-    // (to the end of the 16 bytes in which the last row's last code lies)
-    const int cut = BK - min(max((k_left + 15) & ~15, 0), BK), bytes = k_left > 0 ? max(extent[it] - cut, 0) : 0;
-    int w = wave;
-    asm volatile("" : "+s"(w));  // (all of these addresses ahead of the loop would fill the scalar registers)
-    request_to_lds<16>(at + it * step + k, (uint32_t)bytes, stage + (w + NW * it) * 1024, (int)chunk < k_left ? voff : kOob);
+  // k_left: codes of a row from the block at hand on
+  __device__ __forceinline__ void request(uint32_t stage, int k_left, int wave, int it) const {
+    request_to_lds<16>(at, stage + (uint32_t)(wave + NW * it) * 1024u, chunk < k_left ? voff[it] : kOob);
+  }
+  __device__ __forceinline__ void next() {
+    at.base += BK;
+    uint32_t less = min(at.bytes, (uint32_t)BK);
+    asm volatile("" : "+s"(less));  // (or the compiler makes the two one operation, which the vector unit alone has)
+    at.bytes -= less;
   }
   // Where a lane reads its part of the fragment of 16 rows; rows 16 on lie 16 * BK on.
   __device__ __forceinline__ static int fragment_at(int row0, int lane) {
@@ -112,24 +117,22 @@ template <int BM, int BN, int NW>
 struct Scales {
   static constexpr int PARTS = (BM + BN) / 64;
   static_assert(PARTS <= NW, "");
-  const float* at;  // of this wavefront's, block 0
-  int64_t ld;
+  Stretch at;
+  int64_t step;
   uint32_t voff;
-  int wave;
   __device__ __forceinline__ void init(const float* sa, int64_t ld_sa, int shift_a, int64_t row_a, int rows_a, const float* sb, int64_t ld_sb, int shift_b,
-                                       int row_b, int rows_b, int wave_) {
-    wave = wave_;
+                                       int row_b, int rows_b, int wave) {
     const bool of_a = wave < BM / 64;
     const int r = 64 * (of_a ? wave : wave - BM / 64) + (int)(threadIdx.x & 63), shift = of_a ? shift_a : shift_b;
     const int64_t row = of_a ? row_a : row_b;
-    at = (of_a ? sa : sb) + (row >> shift);
-    ld = of_a ? ld_sa : ld_sb;
+    at = stretch((of_a ? sa : sb) + (row >> shift), 4u * (BM > BN ? BM : BN));
+    step = (of_a ? ld_sa : ld_sb) * 4;
     voff = r < (of_a ? rows_a : rows_b) ? (uint32_t)(((row + r) >> shift) - (row >> shift)) * 4u : kOob;
   }
-  __device__ __forceinline__ void request(float* lds, int block, bool there) const {
-    if (wave >= PARTS) return;
-    request_to_lds<4>(at + block * ld, there ? 4u * (BM > BN ? BM : BN) : 0u, lds + 64 * wave, voff);
+  __device__ __forceinline__ void request(uint32_t lds, int k_left, int wave) const {
+    if (wave < PARTS) request_to_lds<4>(at, lds + 256u * wave, k_left > 0 ? voff : kOob);
   }
+  __device__ __forceinline__ void next() { at.base += step; }
 };
 
 // Which tile a work-group takes.
@@ -137,20 +140,23 @@ struct Place {
   int batch, split, m0, n0, rows, first;  // rows of the tile; first row of the expert's range
 };
 __device__ __forceinline__ bool place(const Gemm8Args& g, uint32_t id, int BM, int BN, Place& p) {
-  // work-groups go round the eight dies; each gets a contiguous run of tiles, row by row
+  // work-groups go round the eight dies; each gets a contiguous run of tiles
   const uint32_t die = id & 7;
   uint32_t t = die * g.run + min(die, g.rest) + (id >> 3), col, row, split;
-  t = div_mod(t, g.by_n, col);
-  p.n0 = (int)col * BN;
   p.first = 0;
   if (!g.ranges) {
-    t = div_mod(t, g.by_m, row);
-    p.m0 = (int)row * BM;
+    // splits of a product apart, and its tiles in patches: what the compute units of a die work on at a time are a few rows and columns of tiles, whose operands its cache holds
+    t = div_mod(t, g.by_tiles, row);
     p.batch = (int)div_mod(t, g.by_splits, split);
     p.split = (int)split;
+    const int first = (int)div_mod(row, g.by_patch, col) * kPatch;
+    p.n0 = (int)div_mod(col, first + kPatch <= g.tiles_m ? g.by_rows : g.by_last, row) * BN;
+    p.m0 = (first + (int)row) * BM;
     p.rows = min(g.M - p.m0, BM);
     return true;
   }
+  t = div_mod(t, g.by_n, col);
+  p.n0 = (int)col * BN;
   p.split = 0;
   const int lane = threadIdx.x & 63, per = (g.batch + 63) / 64;
   auto range = [&](int e, int& first, int& count) {
@@ -256,7 +262,7 @@ struct Product {
   OpA a;
   OpB b;
   Scales<BM, BN, NW> s;
-  int wave, lane, wm, wn, k_begin, k_end;
+  int wave, lane, wm, wn, k_begin, k_end, left;  // left: codes of a row from the block that is asked for next on
   int64_t row0;
   __device__ __forceinline__ void init(const Gemm8Args& g, const Place& p) {
     lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -265,20 +271,25 @@ struct Product {
     row0 = (int64_t)p.first + p.m0;
     const int64_t own = g.ranges ? 0 : p.batch;
     const int cols = min(g.N - p.n0, BN);
-    a.init(g.a + own * g.stride_a + row0 * g.lda, g.lda, p.rows, wave);
-    b.init(g.b + p.batch * g.stride_b + p.n0 * g.ldb, g.ldb, cols, wave);
-    s.init(g.sa + own * g.stride_sa, g.ld_sa, g.shift_a, row0, p.rows, g.sb + p.batch * g.stride_sb, g.ld_sb, g.shift_b, p.n0, cols, wave);
+    const int block = k_begin / BK;
+    a.init(g.a + own * g.stride_a + row0 * g.lda + k_begin, g.lda, p.rows, k_end - k_begin, wave);
+    b.init(g.b + p.batch * g.stride_b + p.n0 * g.ldb + k_begin, g.ldb, cols, k_end - k_begin, wave);
+    s.init(g.sa + own * g.stride_sa + block * g.ld_sa, g.ld_sa, g.shift_a, row0, p.rows, g.sb + p.batch * g.stride_sb + block * g.ld_sb, g.ld_sb, g.shift_b, p.n0, cols, wave);
+    left = k_end - k_begin;
   }
   static constexpr int REQUESTS = OpA::NV + OpB::NV + 1;
-  __device__ __forceinline__ void request(unsigned char* stage, float* scales, int k, int q) const {
-    const int left = k_end - k;
-    if (q < OpA::NV) a.request(stage, k, left, q);
-    else if (q < OpA::NV + OpB::NV) b.request(stage + OpA::BYTES, k, left, q - OpA::NV);
-    else s.request(scales, k / BK, left > 0);
+  // The q-th of the requests of a block of k; behind the last, the next block's are at hand.
+  __device__ __forceinline__ void request(uint32_t stage, uint32_t scales, int q) {
+    if (q < OpA::NV) a.request(stage, left, wave, q);
+    else if (q < OpA::NV + OpB::NV) b.request(stage + OpA::BYTES, left, wave, q - OpA::NV);
+    else s.request(scales, left, wave);
+    if (q < REQUESTS - 1) return;
+    a.next(), b.next(), s.next();
+    left -= BK;
   }
-  __device__ __forceinline__ void request_all(unsigned char* stage, float* scales, int k) const {
+  __device__ __forceinline__ void request_all(uint32_t stage, uint32_t scales) {
 #pragma unroll
-    for (int q = 0; q < REQUESTS; ++q) request(stage, scales, k, q);
+    for (int q = 0; q < REQUESTS; ++q) request(stage, scales, q);
   }
   // Behind the barrier that publishes a stage.
   __device__ __forceinline__ void tail(unsigned char* stage, int k) const {
@@ -304,6 +315,7 @@ struct Strips : Product<BM, BN, NW> {
   using typename P::OpA;
   using typename P::OpB;
   static constexpr int TM = P::TM, TN = P::TN, G = TM < 3 ? TM : 3, ROWS = TM - G, SLOTS = TM * TN, LAG = 3, RING = 4;
+  static constexpr bool PER_STRIP = !BFINE && TM % 4 == 0;  // (of the strips in work at a time no two are the same modulo 4)
   static_assert(SLOTS % RING == 0, "");
   static_assert(P::WN <= BK, "a wavefront's columns share a scale");
   float acc[TM][TN][4];  // (apart, so that each is added to where it is)
@@ -312,7 +324,7 @@ struct Strips : Product<BM, BN, NW> {
   float sm[G], sn[BFINE ? 1 : 2];
   float4 sn4[BFINE ? TN : 1];
   floatx4 by4[BFINE ? RING : 1];
-  float by[BFINE ? 1 : RING];
+  float by[BFINE ? 1 : RING];    // of a slot, or (PER_STRIP) of a strip
   int at_a, at_b, at_sm, at_sn;
 
   static constexpr int strip_of(int g) {  // of the last strips the one in register g
@@ -358,11 +370,12 @@ struct Strips : Product<BM, BN, NW> {
     const int slot = (q + SLOTS) % SLOTS, r = (q + SLOTS) % RING;
     float(&c)[4] = acc[slot_i(slot)][slot_j(slot)];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c[e] = __builtin_fmaf(t[r][e], BFINE ? by4[BFINE ? r : 0][e] : by[BFINE ? 0 : r], c[e]);
+    for (int e = 0; e < 4; ++e) c[e] = __builtin_fmaf(t[r][e], BFINE ? by4[BFINE ? r : 0][e] : by[BFINE ? 0 : PER_STRIP ? slot_i(slot) % 4 : r], c[e]);
     asm volatile("" : "+v"(c[0]), "+v"(c[1]), "+v"(c[2]), "+v"(c[3]));  // (here and not behind a branch)
   }
   // One block of k from stage `from`; the next is in or on its way to `to`, the one after goes to `from`.
   __device__ __forceinline__ void block(unsigned char* from, float* scales_from, unsigned char* to, float* scales_to, int k) {
+    const uint32_t to_stage = lds_address(from), to_scales = lds_address(scales_from);
 #pragma unroll
     for (int q = 0; q < SLOTS; ++q) {
       if (q == ROWS * TN) {
@@ -374,8 +387,9 @@ struct Strips : Product<BM, BN, NW> {
       const int i = slot_i(q), j = slot_j(q), r = q % RING;
       t[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i % G], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
       if constexpr (BFINE) by4[r] = floatx4{sn4[j].x * sm[i % G], sn4[j].y * sm[i % G], sn4[j].z * sm[i % G], sn4[j].w * sm[i % G]};
-      else by[r] = sm[i % G] * sn[0];
+      else if (!PER_STRIP) by[r] = sm[i % G] * sn[0];
       add(q - LAG);
+      if (PER_STRIP && j == 0) by[i % 4] = sm[i % G] * sn[0];
       __builtin_amdgcn_sched_barrier(0);
       if (q < ROWS * TN) {
         if (j == TN - 1) fetch_a(from, scales_from, i + G);
@@ -384,7 +398,7 @@ struct Strips : Product<BM, BN, NW> {
         if (j == TN - 1) fetch_a(to, scales_to, c % G);
         if (c % G == G - 1) fetch_b(to, scales_to, j);
 #pragma unroll
-        for (int x = c * P::REQUESTS / n; x < (c + 1) * P::REQUESTS / n; ++x) this->request(from, scales_from, k + 2 * BK, x);
+        for (int x = c * P::REQUESTS / n; x < (c + 1) * P::REQUESTS / n; ++x) this->request(to_stage, to_scales, x);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -392,10 +406,12 @@ struct Strips : Product<BM, BN, NW> {
   }
   __device__ __forceinline__ void run(unsigned char* stages, float* scales) {
     start();
-    this->request_all(stages, scales, this->k_begin);
+    this->request_all(lds_address(stages), lds_address(scales));
     __builtin_amdgcn_sched_barrier(0);
-    this->request_all(stages + P::STAGE, scales + BM + BN, this->k_begin + BK);
-    arrived();
+    this->request_all(lds_address(stages + P::STAGE), lds_address(scales + BM + BN));
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(P::REQUESTS - 1) : "memory");  // (the first stage's; a wavefront may have no scales to bring)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     this->tail(stages, this->k_begin);
     first(stages, scales);
     int s = 0;
@@ -444,12 +460,12 @@ struct Wide : Product<BM, BN, NW> {
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    this->request_all(stages, scales, this->k_begin);
+    this->request_all(lds_address(stages), lds_address(scales));
     arrived();
     this->tail(stages, this->k_begin);
     int s = 0;
     for (int k = this->k_begin; k < this->k_end; k += BK, s ^= 1) {
-      this->request_all(stages + (s ^ 1) * P::STAGE, scales + (s ^ 1) * (BM + BN), k + BK);
+      this->request_all(lds_address(stages + (s ^ 1) * P::STAGE), lds_address(scales + (s ^ 1) * (BM + BN)));
       __builtin_amdgcn_sched_barrier(0);
       block(stages + s * P::STAGE, scales + s * (BM + BN));
       arrived();
@@ -623,7 +639,8 @@ int launch_tiles(Gemm8Args g, hipStream_t stream) {
   const int64_t tiles_m = ceil_div(g.M, BM), tiles_n = ceil_div(g.N, BN);
   const int64_t groups = g.ranges ? (tiles_m + g.batch) * tiles_n : tiles_m * tiles_n * g.splits * g.batch;
   g.groups = (uint32_t)groups, g.run = g.groups / 8, g.rest = g.groups % 8;
-  g.by_n = divisor((uint32_t)tiles_n), g.by_m = divisor((uint32_t)tiles_m), g.by_splits = divisor((uint32_t)g.splits);
+  g.tiles_m = (int)tiles_m, g.by_n = divisor((uint32_t)tiles_n), g.by_tiles = divisor((uint32_t)(tiles_m * tiles_n)), g.by_splits = divisor((uint32_t)g.splits);
+  g.by_patch = divisor((uint32_t)(kPatch * tiles_n)), g.by_rows = divisor(kPatch), g.by_last = divisor((uint32_t)std::max<int64_t>(1, tiles_m % kPatch));
   const dim3 grid((uint32_t)std::min<int64_t>(groups, kGridX), (uint32_t)((groups + kGridX - 1) / kGridX));
   if (!WIDE && g.shift_b) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, WIDE>), grid, dim3(64 * NW), 0, stream, g);
   else if constexpr (BM < 256) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, true, WIDE>), grid, dim3(64 * NW), 0, stream, g);

@@ -52,7 +52,7 @@ def gemm(**kw):
 
 
 @pytest.mark.parametrize("bad", [dict(M=-1), dict(N=-1), dict(K=-1), dict(M=2 ** 31 - 1), dict(batch=-1), dict(batch=1025), dict(type=3), dict(lda=399), dict(lda=408), dict(lda=384),
-                                 dict(ldb=384), dict(lda=2 ** 27 + 16), dict(ldb=2 ** 27 + 16), dict(ldc=299), dict(ld_add=299), dict(ld_sa=199), dict(ld_sb=2),
+                                 dict(ldb=384), dict(lda=2 ** 22 + 16), dict(ldb=2 ** 22 + 16), dict(ldc=299), dict(ld_add=299), dict(ld_sa=199), dict(ld_sb=2),
                                  dict(a_square=1, ld_sa=1), dict(b_square=0), dict(d_a=None), dict(d_b=None), dict(d_sa=None), dict(d_sb=None), dict(d_c=None),
                                  dict(d_a=P + 8), dict(d_b=P + 8), dict(stride_a=8), dict(stride_b=-16), dict(stride_c=0), dict(stride_c=-1), dict(stride_bias=-1),
                                  dict(stride_sa=-1), dict(ldc=301), dict(stride_add=0), dict(d_ranges=P, a_square=1), dict(d_scratch=P + 4)])
