@@ -46,3 +46,61 @@ __device__ __forceinline__ uint32_t codes8(float a, float b, float c, float d, f
   const int w = __builtin_amdgcn_cvt_pk_fp8_f32(q(a), q(b), 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q(c), q(d), w, true);
 }
+
+// Eight elements from column c of a row of d on, which may end before them (what is behind it is 0) or before c.  No access hangs on a branch that lanes take differently: of a row of
+// at least 8 columns the last 8 are loaded, and moved up.
+template <typename T, bool RAGGED>
+struct Eight {
+  typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+  vec v;
+  __device__ __forceinline__ void load(const T* row, int c, int d) {
+    if (!RAGGED) {
+      v = *reinterpret_cast<const vec*>(row + c);
+    } else if (d >= 8) {
+      v = *reinterpret_cast<const vec*>(row + min(c, d - 8));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = row[min(e, d - 1)];
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[8], int c, int d) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+    if (RAGGED) {
+      const int up = d >= 8 ? c - min(c, d - 8) : 0;
+#pragma unroll
+      for (int by = 4; by >= 1; by /= 2)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (up & by) && e + by < 8 ? x[(e + by) & 7] : x[e];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = c + e < d ? x[e] : 0.f;
+    }
+  }
+  static __device__ __forceinline__ void store(T* row, const float (&x)[8], int c, int d) {
+    vec t;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = (T)x[e];
+    if (!RAGGED || c + 8 <= d) {
+      *reinterpret_cast<vec*>(row + c) = t;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < d) row[c + e] = t[e];
+    }
+  }
+};
+
+// Eight codes times a power of two as bf16, which holds them exactly.
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi, float by = 1.f) {
+  union {
+    bf16x2_t two[4];
+    bf16x8_t all;
+  } u;
+  u.two[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, false);
+  u.two[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, true);
+  u.two[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, false);
+  u.two[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, true);
+  return u.all;
+}

@@ -10,10 +10,11 @@
 namespace {
 
 constexpr int kMaxTokens = 64, kMaxChoices = 64, kMaxExperts = 1024, kMaxWidth = 1 << 20;
-constexpr int kThreads = 256, kWaves = 4;
-constexpr int kMost = 16;  // choices of a matrix instruction
-
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+constexpr int kThreads = 512, kWaves = 8;
+constexpr int kMost = 16;      // choices of a matrix instruction
+// Codes go into the products 2^17 times smaller, and scales as much larger: so the sum of a block's 128 products, each of up to 448 times an input, is finite where the inputs are.
+constexpr float kDown = 0x1p17f;
+constexpr int kStretch = 512;  // of the width, in LDS at a time
 
 struct LayerArgs {
   const void* x;         // [tokens, d] rows of the layer's type, or hidden [choices, width] in fp32
@@ -22,15 +23,16 @@ struct LayerArgs {
   const int32_t* ids;
   float* out;            // [choices, rows of the result]
   int64_t ld_x, ld, stride, ld_scales, stride_scales;
-  int n, k, experts, by_expert;  // choices; of a token; by_expert: a work-group's first index is an expert, not a choice
-  int rows, width, act;          // rows: of the result; width: of x
+  int n, experts, by_expert;  // choices; by_expert: a work-group's first index is an expert, not a choice
+  int rows, width;            // rows: of the result; width: of x
+  Divisor by_k;               // choices of a token
 };
 
 template <int PARTS>
 struct Input {  // eight elements of a row as bf16 parts that add up to them
   bf16x8_t part[PARTS];
 };
-template <typename T, int PARTS>
+template <int PARTS>
 __device__ __forceinline__ void split8(const float (&x)[8], Input<PARTS>& in) {
 #pragma clang fp contract(off)
   float rest[8];
@@ -40,127 +42,219 @@ __device__ __forceinline__ void split8(const float (&x)[8], Input<PARTS>& in) {
   for (int p = 0; p < PARTS; ++p)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      in.part[p][e] = (__bf16)rest[e];
-      rest[e] -= (float)in.part[p][e];
+      float high = (float)(__bf16)rest[e];
+      if (p + 1 < PARTS) {
+        // (what is too large for bf16 keeps the rest of itself, an infinity or NaN has none)
+        constexpr float kMax = 0x1.FEp127f;
+        const bool number = fabsf(rest[e]) < __builtin_inff();
+        if (number) high = fminf(fmaxf(high, -kMax), kMax);
+        in.part[p][e] = (__bf16)high;
+        rest[e] = number ? rest[e] - high : 0.f;
+      } else {
+        in.part[p][e] = (__bf16)high;
+      }
     }
 }
 
-// out[c] = W x for the choices c of an expert.  UP: c's row of x is its token's, GATED: rows r and rows + r of W together, silu(g) * u; ReLU otherwise.  Not UP: c's row is
-// its own, nothing is done to the result.  KS: the wavefronts of a work-group share 16 rows, each a part of the width; else each has 16 of its own.
-template <typename T, int PARTS, bool UP, bool GATED, bool KS>
-__global__ void __launch_bounds__(kThreads) layer8_product_kernel(const LayerArgs a) {
-  __shared__ int32_t list[kMaxTokens];
-  __shared__ int32_t found;
-  __shared__ float join[KS ? kWaves : 1][GATED ? 2 : 1][4][64];
-  touch(a);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int index = blockIdx.y;
-  const int expert = a.by_expert ? index : a.ids[index];
-  if ((uint32_t)expert >= (uint32_t)a.experts) return;
-  // the expert's choices, in their order; a token that chose it twice has one row
-  if (wave == 0) {
+// The choices of an expert, in their order, in `list`; returns how many.  A token that chose it twice has one row, that of its first choice.
+__device__ __forceinline__ int choices_of(const LayerArgs& a, int expert, int32_t* list, int32_t* found) {
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
     int count = 0;
     for (int c0 = 0; c0 < a.n; c0 += 64) {
       const int c = c0 + lane;
-      bool hit = c < a.n && a.ids[min(c, a.n - 1)] == expert;
-      for (int j = c - c % a.k; hit && j < c; ++j) hit = a.ids[j] != expert;
+      uint32_t j;
+      div_mod((uint32_t)c, a.by_k, j);
+      bool hit = a.ids[min(c, a.n - 1)] == expert && c < a.n;
+      for (int back = (int)j; hit && back > 0; --back) hit = a.ids[c - back] != expert;
       const uint64_t hits = __ballot(hit);
       if (hit) list[count + __popcll(hits & ((1ull << lane) - 1))] = c;
       count += __popcll(hits);
     }
-    if (lane == 0) found = count;
+    if (lane == 0) *found = count;
   }
   __syncthreads();
-  const int count = found;
+  return *found;
+}
+
+// The matrix instruction's sums of 16 rows of W times 16 columns of inputs over the blocks of 128 that are at hand.
+template <int PARTS, int HALVES>
+struct Block {
+  code4_t w[HALVES][2];  // a lane's codes: 16 from column 16 (L >> 4) of the block, and 64 further on
+  float scale[HALVES][4];
+  __device__ __forceinline__ void ask(const LayerArgs& a, const uint8_t* codes, const float* scales, int row0, int b) {
+    const int lane = threadIdx.x & 63, group = lane >> 4;
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      const uint8_t* row = codes + (int64_t)(min(row0 + (lane & 15), a.rows - 1) + h * a.rows) * a.ld;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int k = b * kBlock8 + 64 * half + 16 * group;
+        w[h][half] = __builtin_nontemporal_load(reinterpret_cast<const code4_t*>(row + (k < a.width ? k : 0)));  // (16 bytes with a code of the row in them)
+      }
+      // 16 rows from a multiple of 16 on share a scale, other 16 may have two
+      const float* at = scales + b * a.ld_scales;
+      if (h * a.rows % 16 == 0) {
+        const float s = at[(row0 + h * a.rows) >> 7];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) scale[h][e] = s;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) scale[h][e] = at[(min(row0 + 4 * group + e, a.rows - 1) + h * a.rows) >> 7];
+      }
+    }
+  }
+  // Codes behind a row's end belong to nobody.
+  __device__ __forceinline__ void cut(const LayerArgs& a, int b) {
+    if ((b + 1) * kBlock8 <= a.width) return;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int keep = a.width - (b * kBlock8 + 64 * half + 16 * (int)((threadIdx.x & 63) >> 4));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t mask = keep >= 4 * i + 4 ? 0xFFFFFFFFu : keep <= 4 * i ? 0u : (1u << 8 * (keep - 4 * i)) - 1;
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) w[h][half][i] &= mask;
+      }
+    }
+  }
+  // in(half, q): the inputs of eight codes from 64 half + 16 (L >> 4) + 8 q on.
+  template <typename F>
+  __device__ __forceinline__ void add(floatx4 (&acc)[HALVES], F in) const {
+    floatx4 t[HALVES];
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) t[h] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const Input<PARTS> x = in(half, q);
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+          const bf16x8_t m = widen8(w[h][half][2 * q], w[h][half][2 * q + 1], 1.f / kDown);
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p) t[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(m, x.part[p], t[h], 0, 0, 0);
+        }
+      }
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[h][e] = __builtin_fmaf(t[h][e], scale[h][e] * kDown, acc[h][e]);
+  }
+};
+
+// out[c] = W x for the choices c of an expert.  UP: c's row of x is its token's, GATED: rows r and rows + r of W together, silu(g) * u; ReLU otherwise.  Not UP: c's row is
+// its own, nothing is done to the result.
+// ROWS: a wavefront of a work-group has 16 rows of its own, and inputs are split once for all of them, a stretch of kStretch at a time, in LDS.  Otherwise the work-group has 16 rows, each wavefront every
+// kWaves-th block of them, and splits its own inputs: for layers that leave compute units idle.
+template <typename T, int PARTS, bool UP, bool GATED, bool ROWS>
+__global__ void __launch_bounds__(kThreads) layer8_product_kernel(const LayerArgs a) {
+  constexpr int HALVES = GATED ? 2 : 1, PITCH = kStretch + 8, BLOCKS = kStretch / kBlock8;
+  __shared__ int32_t list[kMaxTokens], found;
+  __shared__ __attribute__((aligned(16))) __bf16 xs[ROWS ? PARTS : 1][ROWS ? kMost : 1][ROWS ? PITCH : 8];
+  __shared__ float join[ROWS ? 1 : kWaves][HALVES][4][64];
+  touch(a);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4;
+  const int index = blockIdx.y;
+  const int expert = a.by_expert ? index : a.ids[index];
+  if ((uint32_t)expert >= (uint32_t)a.experts) return;
+  const int count = choices_of(a, expert, list, &found);
   if (count == 0 || (!a.by_expert && list[0] != index)) return;  // (the expert's first choice has its work-groups)
-  const int row0 = (KS ? blockIdx.x : blockIdx.x * kWaves + wave) * 16;
-  if (!KS && row0 >= a.rows) return;
-  const int group = lane >> 4;
+  const int row0 = (ROWS ? blockIdx.x * kWaves + wave : blockIdx.x) * 16;
   const uint8_t* codes = a.codes + expert * a.stride;
   const float* scales = a.scales + expert * a.stride_scales;
   const int blocks = (a.width + kBlock8 - 1) / kBlock8;
+  auto input = [&](int choice) {
+    uint32_t j;
+    return static_cast<const T*>(a.x) + (int64_t)(UP ? div_mod((uint32_t)choice, a.by_k, j) : (uint32_t)choice) * a.ld_x;
+  };
   for (int c0 = 0; c0 < count; c0 += kMost) {
-    const int col = c0 + (lane & 15), choice = list[min(col, count - 1)];
-    const bool there = col < count;
-    const T* x = static_cast<const T*>(a.x) + (UP ? choice / a.k : choice) * a.ld_x;
-    floatx4 acc[GATED ? 2 : 1];
+    const int cols = min(count - c0, kMost), col = lane & 15, choice = list[min(c0 + col, count - 1)];
+    floatx4 acc[HALVES];
 #pragma unroll
-    for (int h = 0; h < (GATED ? 2 : 1); ++h) acc[h] = floatx4{0.f, 0.f, 0.f, 0.f};
-    for (int b = KS ? wave : 0; b < blocks; b += KS ? kWaves : 1) {
-      const int k0 = b * kBlock8;
-      floatx4 t[GATED ? 2 : 1];
+    for (int h = 0; h < HALVES; ++h) acc[h] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (ROWS) {
+      for (int b0 = 0; b0 < blocks; b0 += BLOCKS) {
+        Block<PARTS, HALVES> w[BLOCKS];
 #pragma unroll
-      for (int h = 0; h < (GATED ? 2 : 1); ++h) t[h] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int k = k0 + 64 * half + 16 * group;  // this lane's 16 columns
-        // 16 of the inputs
-        Input<PARTS> in[2];
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int i = 0; i < BLOCKS; ++i) w[i].ask(a, codes, scales, min(row0, a.rows - 1) & ~15, min(b0 + i, blocks - 1));
+        __syncthreads();  // (the last stretch is done with)
+        for (int i = threadIdx.x; i < cols * (kStretch / 8); i += kThreads) {
+          const int c = i / (kStretch / 8), k = i % (kStretch / 8) * 8, at = b0 * kBlock8 + k;
+          Eight<T, true> e;
           float v[8];
+          e.load(input(list[c0 + c]), min(at, a.width - 1), a.width);
+          e.get(v, min(at, a.width - 1), a.width);
+          if (at >= a.width)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int at = k + 8 * q + e;
-            const float w = (float)x[min(at, a.width - 1)];
-            v[e] = there && at < a.width ? w : 0.f;
-          }
-          split8<T, PARTS>(v, in[q]);
+            for (int u = 0; u < 8; ++u) v[u] = 0.f;
+          Input<PARTS> in;
+          split8(v, in);
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) *reinterpret_cast<bf16x8_t*>(&xs[p][c][k]) = in.part[p];
         }
+        __syncthreads();
 #pragma unroll
-        for (int h = 0; h < (GATED ? 2 : 1); ++h) {
-          const int row = min(row0 + (lane & 15), a.rows - 1) + h * a.rows;
-          // (16 bytes with a code of the row in them, or the row's first; codes behind the row's end belong to nobody)
-          code4_t w = *reinterpret_cast<const code4_t*>(codes + row * a.ld + (k < a.width ? k : 0));
-          const int keep = a.width - k;
-          if (keep < 16)
+        for (int i = 0; i < BLOCKS; ++i) {
+          if (b0 + i >= blocks) break;
+          w[i].cut(a, b0 + i);
+          w[i].add(acc, [&](int half, int q) {
+            Input<PARTS> in;  // (columns without a choice hold whatever was there: nothing of theirs is written)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] &= keep >= 4 * i + 4 ? 0xFFFFFFFFu : keep <= 4 * i ? 0u : (1u << 8 * (keep - 4 * i)) - 1;
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            bf16x8_t m;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int word = (int)w[2 * q + i];
-              m[4 * i + 0] = (__bf16)__builtin_amdgcn_cvt_f32_fp8(word, 0);
-              m[4 * i + 1] = (__bf16)__builtin_amdgcn_cvt_f32_fp8(word, 1);
-              m[4 * i + 2] = (__bf16)__builtin_amdgcn_cvt_f32_fp8(word, 2);
-              m[4 * i + 3] = (__bf16)__builtin_amdgcn_cvt_f32_fp8(word, 3);
-            }
-#pragma unroll
-            for (int p = PARTS - 1; p >= 0; --p) t[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(m, in[q].part[p], t[h], 0, 0, 0);
-          }
+            for (int p = 0; p < PARTS; ++p) in.part[p] = *reinterpret_cast<const bf16x8_t*>(&xs[p][col][i * kBlock8 + 64 * half + 16 * group + 8 * q]);
+            return in;
+          });
         }
       }
+      if (row0 >= a.rows) continue;
+    } else {
+      const T* x = input(choice);
+      for (int b = wave; b < blocks; b += kWaves) {
+        Block<PARTS, HALVES> w;
+        w.ask(a, codes, scales, row0, b);
+        Eight<T, true> e[2][2];
 #pragma unroll
-      for (int h = 0; h < (GATED ? 2 : 1); ++h)
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = min(row0 + 4 * group + e, a.rows - 1) + h * a.rows;
-          acc[h][e] = __builtin_fmaf(t[h][e], scales[b * a.ld_scales + (row >> 7)], acc[h][e]);
-        }
-    }
-    if (KS) {
-      __syncthreads();
+          for (int q = 0; q < 2; ++q) e[half][q].load(x, min(b * kBlock8 + 64 * half + 16 * group + 8 * q, a.width - 1), a.width);
+        w.cut(a, b);
+        w.add(acc, [&](int half, int q) {
+          const int at = b * kBlock8 + 64 * half + 16 * group + 8 * q;
+          float v[8];
+          e[half][q].get(v, min(at, a.width - 1), a.width);
+          if (at >= a.width)
 #pragma unroll
-      for (int h = 0; h < (GATED ? 2 : 1); ++h)
+            for (int u = 0; u < 8; ++u) v[u] = 0.f;
+          Input<PARTS> in;
+          split8(v, in);
+          return in;
+        });
+      }
+      __syncthreads();  // (the last choices' sums are read)
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e) join[wave][h][e][lane] = acc[h][e];
       __syncthreads();
-      if (wave == 0)
+      if (wave > 0) continue;
 #pragma unroll
-        for (int h = 0; h < (GATED ? 2 : 1); ++h)
+      for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[h][e] = (join[0][h][e][lane] + join[1][h][e][lane]) + (join[KS ? 2 : 0][h][e][lane] + join[KS ? 3 : 0][h][e][lane]);
+        for (int e = 0; e < 4; ++e) {
+          float v = join[0][h][e][lane];
+#pragma unroll
+          for (int w = 1; w < kWaves; ++w) v += join[ROWS ? 0 : w][h][e][lane];
+          acc[h][e] = v;
+        }
     }
-    if (there && (!KS || wave == 0))
+    if (col >= cols) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = row0 + 4 * group + e;
-        float v = acc[0][e];
-        if (UP) v = GATED ? v / (1.f + expf(-v)) * acc[GATED ? 1 : 0][e] : v < 0.f ? 0.f : v;
-        if (row < a.rows) a.out[(int64_t)choice * a.rows + row] = v;
-      }
+    for (int e = 0; e < 4; ++e) {
+      const int row = row0 + 4 * group + e;
+      float v = acc[0][e];
+      if (UP) v = GATED ? v / (1.f + expf(-v)) * acc[HALVES - 1][e] : v < 0.f ? 0.f : v;
+      if (row < a.rows) a.out[(int64_t)choice * a.rows + row] = v;
+    }
   }
 }
 
@@ -191,8 +285,8 @@ template <typename T, int PARTS, bool UP, bool GATED>
 int launch_product(LayerArgs a, hipStream_t stream) {
   const int tiles = ceil_div(a.rows, 16), experts = std::min(a.n, a.experts);
   a.by_expert = a.n > a.experts;
-  if ((int64_t)tiles * experts < 8192) hipLaunchKernelGGL((layer8_product_kernel<T, PARTS, UP, GATED, true>), dim3(tiles, experts), dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((layer8_product_kernel<T, PARTS, UP, GATED, false>), dim3(ceil_div(tiles, kWaves), experts), dim3(kThreads), 0, stream, a);
+  if ((int64_t)tiles * experts >= 256 * kWaves) hipLaunchKernelGGL((layer8_product_kernel<T, PARTS, UP, GATED, true>), dim3(ceil_div(tiles, kWaves), experts), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((layer8_product_kernel<T, PARTS, UP, GATED, false>), dim3(tiles, experts), dim3(kThreads), 0, stream, a);
   NMT_LAUNCH_CHECK();
   return NMT_OK;
 }
@@ -201,7 +295,7 @@ int launch_layer(const nmt_expert_layer8* p, hipStream_t stream) {
   const int n = p->tokens * p->k;
   float *hidden = p->d_scratch, *y = p->d_scratch + (int64_t)n * p->ff;
   LayerArgs a = {};
-  a.ids = p->d_expert, a.n = n, a.k = p->k, a.experts = p->experts, a.act = p->act;
+  a.ids = p->d_expert, a.n = n, a.by_k = divisor((uint32_t)p->k), a.experts = p->experts;
   a.x = p->d_x, a.ld_x = p->ld_x, a.codes = static_cast<const uint8_t*>(p->d_up), a.ld = p->ld_up, a.stride = p->stride_up;
   a.scales = p->d_up_scales, a.ld_scales = p->ld_up_scales, a.stride_scales = p->stride_up_scales, a.out = hidden, a.rows = p->ff, a.width = p->d;
   const int rc = p->act == NMT_ACT_SILU_GATE ? launch_product<T, PARTS, true, true>(a, stream) : launch_product<T, PARTS, true, false>(a, stream);

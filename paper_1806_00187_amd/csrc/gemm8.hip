@@ -225,25 +225,12 @@ __device__ __forceinline__ void store4(const Gemm8Args& g, T* c, const T* bias, 
   }
 }
 
-// Sixteen codes of one wavefront's rows as bf16, which holds them exactly.
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ bf16x8_t widen(int lo, int hi) {
-  union {
-    bf16x2_t two[4];
-    bf16x8_t all;
-  } u;
-  u.two[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
-  u.two[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
-  u.two[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
-  u.two[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
-  return u.all;
-}
+// A fragment as bf16.
 struct Codes {
   bf16x8_t f[4];
   __device__ __forceinline__ void set(const frag_t& v) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) f[q] = widen(v[2 * q], v[2 * q + 1]);
+    for (int q = 0; q < 4; ++q) f[q] = widen8((uint32_t)v[2 * q], (uint32_t)v[2 * q + 1]);
   }
   __device__ __forceinline__ floatx4 times(const Codes& o) const {
     floatx4 t = {0.f, 0.f, 0.f, 0.f};
@@ -556,7 +543,7 @@ struct Result {
         if (16 * i + ROWS * x + row >= rows) continue;
         T* to = c + (16 * i + ROWS * x) * ldc;
         if (left >= E) {
-          *reinterpret_cast<vec*>(to) = o;
+          __builtin_nontemporal_store(o, reinterpret_cast<vec*>(to));
         } else {
 #pragma unroll
           for (int e = 0; e < E; ++e)

@@ -10,49 +10,6 @@ constexpr int kMaxRows = 0x7FFFFFFF - 65536, kMaxCols = 16384;
 constexpr int kThreads = 256;
 constexpr int kGridX = 1 << 22;  // work-groups in a row of the grid: one has less than 2^32 threads
 
-// Eight elements from column c of a row of d on, which may end before them (what is behind it is 0) or before c.  No access hangs on a branch that lanes take differently: of a row of
-// at least 8 columns the last 8 are loaded, and moved up.
-template <typename T, bool RAGGED>
-struct Eight {
-  typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-  vec v;
-  __device__ __forceinline__ void load(const T* row, int c, int d) {
-    if (!RAGGED) {
-      v = *reinterpret_cast<const vec*>(row + c);
-    } else if (d >= 8) {
-      v = *reinterpret_cast<const vec*>(row + min(c, d - 8));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = row[min(e, d - 1)];
-    }
-  }
-  __device__ __forceinline__ void get(float (&x)[8], int c, int d) const {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
-    if (RAGGED) {
-      const int up = d >= 8 ? c - min(c, d - 8) : 0;
-#pragma unroll
-      for (int by = 4; by >= 1; by /= 2)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (up & by) && e + by < 8 ? x[(e + by) & 7] : x[e];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = c + e < d ? x[e] : 0.f;
-    }
-  }
-  static __device__ __forceinline__ void store(T* row, const float (&x)[8], int c, int d) {
-    vec t;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = (T)x[e];
-    if (!RAGGED || c + 8 <= d) {
-      *reinterpret_cast<vec*>(row + c) = t;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (c + e < d) row[c + e] = t[e];
-    }
-  }
-};
-
 // ---- a matrix into 8 bits --------------------------------------------------------------------------
 struct QuantArgs {
   const void* x;

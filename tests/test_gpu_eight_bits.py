@@ -453,6 +453,28 @@ def test_layer_of_many_work_groups(tokens, k, E, d, ff):
     check_layer(tokens, k, E, d, ff, F16, "silu_gate")
 
 
+def test_layer_of_infinities_and_huge_inputs():
+    """An infinity, a NaN and inputs near the end of fp32's range reach the tokens that have them as the formula says, and no other."""
+    x, ids, weights, (up, su), (down, sd) = layer_inputs(6, 2, 3, 200, 160, F32, "relu", 31)
+    scratch = torch.empty(A.nmt_op_expert_layer8_scratch(6, 2, 3, 200, 160), device=DEV)
+    want, out = torch.empty_like(x), torch.empty_like(x)
+    A.nmt_op_expert_layer8(x, ids, weights, up, su, down, sd, want, scratch)
+    z = x.clone()
+    z[1, 7], z[2, 9] = float("inf"), float("nan")
+    z[4] = 0
+    z[4, 11] = 3.4028e38       # (beyond the largest bf16)
+    small, tiny = su / 2.0 ** 20, z.clone()
+    A.nmt_op_expert_layer8(z, ids, weights, up, su, down, sd, out, scratch)
+    assert not torch.isfinite(out[1]).any() and torch.isnan(out[2]).all()
+    for t in (0, 3, 5):
+        assert torch.equal(out[t], want[t])
+    tiny[4, 11] = 3.4028e38 / 2.0 ** 40
+    huge, ref = torch.empty_like(x), torch.empty_like(x)
+    A.nmt_op_expert_layer8(z[4:5], ids[4:5], weights[4:5], up, small / 2.0 ** 20, down, sd, huge[:1], scratch)      # the same hidden values from weights 2^40 smaller
+    A.nmt_op_expert_layer8(tiny[4:5], ids[4:5], weights[4:5], up, su, down, sd, ref[:1], scratch)
+    assert torch.isfinite(huge[0]).all() and float((huge[0] - ref[0]).norm() / ref[0].norm()) < 1e-5
+
+
 # ---- as they are used ------------------------------------------------------------------------------
 def test_graphs_streams_and_the_same_bits_again():
     """Every operator captured, and replayed with eager calls and other inputs between: each replay gives the eager call's bits."""
