@@ -17,12 +17,13 @@ constexpr float kDown = 0x1p17f;
 constexpr int kStretch = 512;  // of the width, in LDS at a time
 
 struct LayerArgs {
-  const void* x;         // [tokens, d] rows of the layer's type, or hidden [choices, width] in fp32
+  const void* x;         // [tokens, d] rows of the layer's type, or hidden [parts, choices, width rounded up to 16] in bf16
   const uint8_t* codes;  // of the experts' weights
   const float* scales;
   const int32_t* ids;
-  float* out;            // [choices, rows of the result]
-  int64_t ld_x, ld, stride, ld_scales, stride_scales;
+  float* out;            // [choices, rows of the result] ...
+  __bf16* hidden;        // ... or hidden, ld_hidden
+  int64_t ld_hidden, ld_x, ld, stride, ld_scales, stride_scales;
   int n, experts, by_expert;  // choices; by_expert: a work-group's first index is an expert, not a choice
   int rows, width;            // rows: of the result; width: of x
   Divisor by_k;               // choices of a token
@@ -32,29 +33,77 @@ template <int PARTS>
 struct Input {  // eight elements of a row as bf16 parts that add up to them
   bf16x8_t part[PARTS];
 };
-template <int PARTS>
-__device__ __forceinline__ void split8(const float (&x)[8], Input<PARTS>& in) {
+// T: the type that the elements had.
+template <typename T, int PARTS, int N>
+__device__ __forceinline__ void split(const float (&x)[N], __bf16 (&part)[PARTS][N]) {
 #pragma clang fp contract(off)
-  float rest[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) rest[e] = x[e];
+  for (int e = 0; e < N; ++e) {
+    float rest = x[e];
 #pragma unroll
-  for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float high = (float)(__bf16)rest[e];
+    for (int p = 0; p < PARTS; ++p) {
+      float high = (float)(__bf16)rest;
       if (p + 1 < PARTS) {
         // (what is too large for bf16 keeps the rest of itself, an infinity or NaN has none)
         constexpr float kMax = 0x1.FEp127f;
-        const bool number = fabsf(rest[e]) < __builtin_inff();
-        if (number) high = fminf(fmaxf(high, -kMax), kMax);
-        in.part[p][e] = (__bf16)high;
-        rest[e] = number ? rest[e] - high : 0.f;
+        const bool number = fabsf(rest) < __builtin_inff();
+        if (sizeof(T) == 4 && number) high = fminf(fmaxf(high, -kMax), kMax);
+        part[p][e] = (__bf16)high;
+        rest = number ? rest - high : 0.f;
       } else {
-        in.part[p][e] = (__bf16)high;
+        part[p][e] = (__bf16)high;
       }
     }
+  }
 }
+
+// Where a product's inputs come from.  Rows of T, which are split when they are loaded, RAGGED: of a width that is no multiple of 8; or parts that were split before.
+template <typename T, int PARTS, bool RAGGED>
+struct Rows {
+  static constexpr bool SPLIT = false;
+  static constexpr int kParts = PARTS;
+  Eight<T, RAGGED> e;
+  const T* row;
+  __device__ __forceinline__ void set(const LayerArgs& a, int choice, bool up) {
+    uint32_t j;
+    row = static_cast<const T*>(a.x) + (int64_t)(up ? div_mod((uint32_t)choice, a.by_k, j) : (uint32_t)choice) * a.ld_x;
+  }
+  __device__ __forceinline__ void ask(const LayerArgs& a, int at) { e.load(row, min(at, RAGGED ? a.width - 1 : a.width - 8), a.width); }
+  __device__ __forceinline__ Input<PARTS> get(const LayerArgs& a, int at) const {
+    float v[8];
+    __bf16 part[PARTS][8];
+    e.get(v, min(at, a.width - 1), a.width);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = at < a.width ? v[u] : 0.f;
+    split<T, PARTS, 8>(v, part);
+    Input<PARTS> in;
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) in.part[p][u] = part[p][u];
+    return in;
+  }
+};
+template <int PARTS>
+struct Parts {
+  static constexpr bool SPLIT = true;
+  static constexpr int kParts = PARTS;
+  Input<PARTS> in;
+  const __bf16* row;
+  __device__ __forceinline__ void set(const LayerArgs& a, int choice, bool) { row = static_cast<const __bf16*>(a.x) + (int64_t)choice * a.ld_x; }
+  __device__ __forceinline__ void ask(const LayerArgs& a, int at) {
+    const int64_t plane = (int64_t)a.n * a.ld_x;
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) in.part[p] = *reinterpret_cast<const bf16x8_t*>(row + p * plane + min(at, (int)a.ld_x - 8));
+  }
+  __device__ __forceinline__ Input<PARTS> get(const LayerArgs& a, int at) const {
+    Input<PARTS> x = in;
+    if (at >= a.width)
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) x.part[p] = bf16x8_t{};
+    return x;
+  }
+};
 
 // The choices of an expert, in their order, in `list`; returns how many.  A token that chose it twice has one row, that of its first choice.
 __device__ __forceinline__ int choices_of(const LayerArgs& a, int expert, int32_t* list, int32_t* found) {
@@ -143,31 +192,28 @@ struct Block {
   }
 };
 
-// out[c] = W x for the choices c of an expert.  UP: c's row of x is its token's, GATED: rows r and rows + r of W together, silu(g) * u; ReLU otherwise.  Not UP: c's row is
-// its own, nothing is done to the result.
+// out[c] = W x for the choices c of an expert.  UP: c's row of x is its token's, and what comes of it is hidden, in HIDDEN bf16 parts for the next product, GATED: of rows r and
+// rows + r of W together, silu(g) * u; ReLU otherwise.  Not UP: c's row is its own, and the result is left in fp32.
 // ROWS: a wavefront of a work-group has 16 rows of its own, and inputs are split once for all of them, a stretch of kStretch at a time, in LDS.  Otherwise the work-group has 16 rows, each wavefront every
 // kWaves-th block of them, and splits its own inputs: for layers that leave compute units idle.
-template <typename T, int PARTS, bool UP, bool GATED, bool ROWS>
+template <typename Source, int HIDDEN, bool GATED, bool ROWS>
 __global__ void __launch_bounds__(kThreads) layer8_product_kernel(const LayerArgs a) {
-  constexpr int HALVES = GATED ? 2 : 1, PITCH = kStretch + 8, BLOCKS = kStretch / kBlock8;
+  constexpr bool UP = HIDDEN > 0;
+  constexpr int PARTS = Source::kParts, HALVES = GATED ? 2 : 1, PITCH = kStretch + 8, BLOCKS = kStretch / kBlock8;
   __shared__ int32_t list[kMaxTokens], found;
   __shared__ __attribute__((aligned(16))) __bf16 xs[ROWS ? PARTS : 1][ROWS ? kMost : 1][ROWS ? PITCH : 8];
   __shared__ float join[ROWS ? 1 : kWaves][HALVES][4][64];
   touch(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4;
   const int index = blockIdx.y;
-  const int expert = a.by_expert ? index : a.ids[index];
+  const int expert = a.by_expert ? index : __builtin_amdgcn_readfirstlane(a.ids[index]);
   if ((uint32_t)expert >= (uint32_t)a.experts) return;
-  const int count = choices_of(a, expert, list, &found);
-  if (count == 0 || (!a.by_expert && list[0] != index)) return;  // (the expert's first choice has its work-groups)
+  const int count = __builtin_amdgcn_readfirstlane(choices_of(a, expert, list, &found));
+  if (count == 0 || (!a.by_expert && __builtin_amdgcn_readfirstlane(list[0]) != index)) return;  // (the expert's first choice has its work-groups)
   const int row0 = (ROWS ? blockIdx.x * kWaves + wave : blockIdx.x) * 16;
   const uint8_t* codes = a.codes + expert * a.stride;
   const float* scales = a.scales + expert * a.stride_scales;
   const int blocks = (a.width + kBlock8 - 1) / kBlock8;
-  auto input = [&](int choice) {
-    uint32_t j;
-    return static_cast<const T*>(a.x) + (int64_t)(UP ? div_mod((uint32_t)choice, a.by_k, j) : (uint32_t)choice) * a.ld_x;
-  };
   for (int c0 = 0; c0 < count; c0 += kMost) {
     const int cols = min(count - c0, kMost), col = lane & 15, choice = list[min(c0 + col, count - 1)];
     floatx4 acc[HALVES];
@@ -181,15 +227,10 @@ __global__ void __launch_bounds__(kThreads) layer8_product_kernel(const LayerArg
         __syncthreads();  // (the last stretch is done with)
         for (int i = threadIdx.x; i < cols * (kStretch / 8); i += kThreads) {
           const int c = i / (kStretch / 8), k = i % (kStretch / 8) * 8, at = b0 * kBlock8 + k;
-          Eight<T, true> e;
-          float v[8];
-          e.load(input(list[c0 + c]), min(at, a.width - 1), a.width);
-          e.get(v, min(at, a.width - 1), a.width);
-          if (at >= a.width)
-#pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = 0.f;
-          Input<PARTS> in;
-          split8(v, in);
+          Source x;
+          x.set(a, list[c0 + c], UP);
+          x.ask(a, at);
+          const Input<PARTS> in = x.get(a, at);
 #pragma unroll
           for (int p = 0; p < PARTS; ++p) *reinterpret_cast<bf16x8_t*>(&xs[p][c][k]) = in.part[p];
         }
@@ -208,27 +249,20 @@ __global__ void __launch_bounds__(kThreads) layer8_product_kernel(const LayerArg
       }
       if (row0 >= a.rows) continue;
     } else {
-      const T* x = input(choice);
       for (int b = wave; b < blocks; b += kWaves) {
+        const int at = b * kBlock8 + 16 * group;
         Block<PARTS, HALVES> w;
         w.ask(a, codes, scales, row0, b);
-        Eight<T, true> e[2][2];
+        Source x[2][2];
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) e[half][q].load(x, min(b * kBlock8 + 64 * half + 16 * group + 8 * q, a.width - 1), a.width);
+          for (int q = 0; q < 2; ++q) {
+            x[half][q].set(a, choice, UP);
+            x[half][q].ask(a, at + 64 * half + 8 * q);
+          }
         w.cut(a, b);
-        w.add(acc, [&](int half, int q) {
-          const int at = b * kBlock8 + 64 * half + 16 * group + 8 * q;
-          float v[8];
-          e[half][q].get(v, min(at, a.width - 1), a.width);
-          if (at >= a.width)
-#pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = 0.f;
-          Input<PARTS> in;
-          split8(v, in);
-          return in;
-        });
+        w.add(acc, [&](int half, int q) { return x[half][q].get(a, at + 64 * half + 8 * q); });
       }
       __syncthreads();  // (the last choices' sums are read)
 #pragma unroll
@@ -248,12 +282,26 @@ __global__ void __launch_bounds__(kThreads) layer8_product_kernel(const LayerArg
         }
     }
     if (col >= cols) continue;
+    const int row = row0 + 4 * group;
+    if constexpr (UP) {
+      float v[4];
+      __bf16 part[HIDDEN][4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int row = row0 + 4 * group + e;
-      float v = acc[0][e];
-      if (UP) v = GATED ? v / (1.f + expf(-v)) * acc[HALVES - 1][e] : v < 0.f ? 0.f : v;
-      if (row < a.rows) a.out[(int64_t)choice * a.rows + row] = v;
+      for (int e = 0; e < 4; ++e) {
+        const float g = acc[0][e];
+        v[e] = GATED ? g / (1.f + expf(-g)) * acc[HALVES - 1][e] : g < 0.f ? 0.f : g;
+        if (row + e >= a.rows) v[e] = 0.f;  // (hidden rows are whole 16s)
+      }
+      split<float, HIDDEN, 4>(v, part);
+#pragma unroll
+      for (int p = 0; p < HIDDEN; ++p) {
+        typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<bf16x4_t*>(a.hidden + ((int64_t)p * a.n + choice) * a.ld_hidden + row) = bf16x4_t{part[p][0], part[p][1], part[p][2], part[p][3]};
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (row + e < a.rows) a.out[(int64_t)choice * a.rows + row + e] = acc[0][e];
     }
   }
 }
@@ -281,28 +329,35 @@ __global__ void __launch_bounds__(kThreads) layer8_sum_kernel(const SumArgs a) {
   static_cast<T*>(a.out)[t * a.ld_out + c] = (T)v;
 }
 
-template <typename T, int PARTS, bool UP, bool GATED>
+template <typename Source, int HIDDEN, bool GATED>
 int launch_product(LayerArgs a, hipStream_t stream) {
   const int tiles = ceil_div(a.rows, 16), experts = std::min(a.n, a.experts);
   a.by_expert = a.n > a.experts;
-  if ((int64_t)tiles * experts >= 256 * kWaves) hipLaunchKernelGGL((layer8_product_kernel<T, PARTS, UP, GATED, true>), dim3(ceil_div(tiles, kWaves), experts), dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((layer8_product_kernel<T, PARTS, UP, GATED, false>), dim3(tiles, experts), dim3(kThreads), 0, stream, a);
+  if ((int64_t)tiles * experts >= 256 * kWaves) hipLaunchKernelGGL((layer8_product_kernel<Source, HIDDEN, GATED, true>), dim3(ceil_div(tiles, kWaves), experts), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((layer8_product_kernel<Source, HIDDEN, GATED, false>), dim3(tiles, experts), dim3(kThreads), 0, stream, a);
   NMT_LAUNCH_CHECK();
   return NMT_OK;
 }
-template <typename T, int PARTS, int HIDDEN_PARTS>
+// Floats of hidden, in three parts at most.
+int64_t hidden_floats(int n, int ff) { return (int64_t)n * round_up(ff, 16) / 2 * 3; }
+
+template <typename T, int PARTS, int HIDDEN>
 int launch_layer(const nmt_expert_layer8* p, hipStream_t stream) {
   const int n = p->tokens * p->k;
-  float *hidden = p->d_scratch, *y = p->d_scratch + (int64_t)n * p->ff;
+  __bf16* hidden = reinterpret_cast<__bf16*>(p->d_scratch);
+  float* y = p->d_scratch + hidden_floats(n, p->ff);
   LayerArgs a = {};
-  a.ids = p->d_expert, a.n = n, a.by_k = divisor((uint32_t)p->k), a.experts = p->experts;
+  a.ids = p->d_expert, a.n = n, a.by_k = divisor((uint32_t)p->k), a.experts = p->experts, a.hidden = hidden, a.ld_hidden = round_up(p->ff, 16);
   a.x = p->d_x, a.ld_x = p->ld_x, a.codes = static_cast<const uint8_t*>(p->d_up), a.ld = p->ld_up, a.stride = p->stride_up;
-  a.scales = p->d_up_scales, a.ld_scales = p->ld_up_scales, a.stride_scales = p->stride_up_scales, a.out = hidden, a.rows = p->ff, a.width = p->d;
-  const int rc = p->act == NMT_ACT_SILU_GATE ? launch_product<T, PARTS, true, true>(a, stream) : launch_product<T, PARTS, true, false>(a, stream);
+  a.scales = p->d_up_scales, a.ld_scales = p->ld_up_scales, a.stride_scales = p->stride_up_scales, a.rows = p->ff, a.width = p->d;
+  const bool gate = p->act == NMT_ACT_SILU_GATE;
+  int rc;
+  if (p->d % 8) rc = gate ? launch_product<Rows<T, PARTS, true>, HIDDEN, true>(a, stream) : launch_product<Rows<T, PARTS, true>, HIDDEN, false>(a, stream);
+  else rc = gate ? launch_product<Rows<T, PARTS, false>, HIDDEN, true>(a, stream) : launch_product<Rows<T, PARTS, false>, HIDDEN, false>(a, stream);
   if (rc != NMT_OK) return rc;
-  a.x = hidden, a.ld_x = p->ff, a.codes = static_cast<const uint8_t*>(p->d_down), a.ld = p->ld_down, a.stride = p->stride_down;
+  a.x = hidden, a.ld_x = a.ld_hidden, a.codes = static_cast<const uint8_t*>(p->d_down), a.ld = p->ld_down, a.stride = p->stride_down;
   a.scales = p->d_down_scales, a.ld_scales = p->ld_down_scales, a.stride_scales = p->stride_down_scales, a.out = y, a.rows = p->d, a.width = p->ff;
-  if (const int rc2 = launch_product<float, HIDDEN_PARTS, false, false>(a, stream); rc2 != NMT_OK) return rc2;
+  if (const int rc2 = launch_product<Parts<HIDDEN>, 0, false>(a, stream); rc2 != NMT_OK) return rc2;
   SumArgs s = {};
   s.y = y, s.weights = p->d_weights, s.ids = p->d_expert, s.add = p->d_add, s.out = p->d_out, s.ld_add = p->ld_add, s.ld_out = p->ld_out;
   s.tokens = p->tokens, s.k = p->k, s.experts = p->experts, s.d = p->d;
@@ -323,7 +378,7 @@ int check_layer(const char* who, int tokens, int k, int experts, int d, int ff) 
 
 extern "C" int64_t nmt_op_expert_layer8_scratch(int32_t tokens, int32_t k, int32_t experts, int32_t d, int32_t ff) {
   if (const int rc = check_layer("nmt_op_expert_layer8_scratch", tokens, k, experts, d, ff); rc != NMT_OK) return rc;
-  return (int64_t)tokens * k * ((int64_t)ff + d);
+  return hidden_floats(tokens * k, ff) + (int64_t)tokens * k * d;
 }
 
 extern "C" int nmt_op_expert_layer8(const nmt_expert_layer8* p, void* stream_) {
