@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libnmt.so")
@@ -146,11 +147,11 @@ _SIGNATURES = {
     "nmt_adamw_create": (C.c_int, [_I32, C.POINTER(nmt_adamw_tensor), _I32, _I32, _I32, _P, _I64, _P, C.POINTER(_P)]),
     "nmt_adamw_destroy": (None, [_P]),
     "nmt_op_quantize8": (C.c_int, [_P, _I64, _I32, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P]),
-    "nmt_op_norm8": (C.c_int, [C.POINTER(nmt_norm8), _P]),
+    "nmt_op_norm8": (C.c_int, [_P, _P]),
     "nmt_op_gemm8_scratch": (_I64, [_I32, _I32, _I32, _I32, _I32]),
-    "nmt_op_gemm8": (C.c_int, [C.POINTER(nmt_gemm8), _P]),
+    "nmt_op_gemm8": (C.c_int, [_P, _P]),
     "nmt_op_expert_layer8_scratch": (_I64, [_I32, _I32, _I32, _I32, _I32]),
-    "nmt_op_expert_layer8": (C.c_int, [C.POINTER(nmt_expert_layer8), _P]),
+    "nmt_op_expert_layer8": (C.c_int, [_P, _P]),
     "nmt_adamw_step": (C.c_int, [_P, C.c_double, C.c_double, C.c_double, C.c_double, _I32, _F, _P, _P]),
 }
 
@@ -826,6 +827,12 @@ def nmt_op_quantize8(x, codes=None, scales=None, codes_t=None, scales_t=None, sq
           codes_t_, ld_codes_t, scales_t_, ld_scales_t)
 
 
+# The structs of these calls as bytes, in one go: field by field they cost 2 us more.
+_NORM8, _GEMM8, _LAYER8 = struct.Struct("4i2f6q9Q"), struct.Struct("7i13q9Qq"), struct.Struct("7i11q10Qq")
+for _s, _c in ((_NORM8, nmt_norm8), (_GEMM8, nmt_gemm8), (_LAYER8, nmt_expert_layer8)):
+    assert _s.size == C.sizeof(_c), _c
+
+
 def nmt_op_norm8(x, y, h, codes, scales, gain, shift=None, n=None, stats=None, kind="rms", resid_scale=1.0, eps=1e-5, stream=None):
     """h = resid_scale * x + y, n = norm(h) * gain + shift in 8 bits: codes [rows, d], scales [ceil(d / 128), rows]; n itself as well if a tensor is given.  y None: h is x, and
     h None."""
@@ -833,46 +840,42 @@ def nmt_op_norm8(x, y, h, codes, scales, gain, shift=None, n=None, stats=None, k
     rows, d, dtype, device = _rows_of(x, who, "x")
     if kind not in _KINDS:
         _refuse(f"{who}: kind {kind!r}: 'layer' or 'rms'")
-    a = nmt_norm8()
-    a.rows, a.d, a.type, a.kind, a.resid_scale, a.eps = rows, d, _type_code(dtype, who), _KINDS[kind], resid_scale, eps
-    a.d_x, a.ld_x = _matrix(x, rows, d, dtype, device, "x")
-    if y is not None:
-        a.d_y, a.ld_y = _matrix(y, rows, d, dtype, device, "y")
-    if h is not None:
-        a.d_h, a.ld_h = _matrix(h, rows, d, dtype, device, "h")
-    if n is not None:
-        a.d_n, a.ld_n = _matrix(n, rows, d, dtype, device, "n")
-    a.d_gain = _vector(gain, d, dtype, device, "the gain")
-    if shift is not None:
-        a.d_shift = _vector(shift, d, dtype, device, "the shift")
-    a.d_codes, a.ld_codes = _matrix(codes, rows, d, _E4M3, device, "codes")
-    a.d_scales, a.ld_scales = _matrix(scales, -(-d // 128), rows, _FLOAT, device, "scales")
-    if stats is not None:
-        a.d_stats = _vector(stats, 4 * rows, _FLOAT, device, "stats")
-    _call(lib.nmt_op_norm8, device, stream, a)
+    if not (abs(resid_scale) < 3.4e38 and abs(eps) < 3.4e38):
+        _refuse(f"{who}: resid_scale {resid_scale} and eps {eps} are numbers of 32 bits")
+    x_, ld_x = _matrix(x, rows, d, dtype, device, "x")
+    y_, ld_y = (0, 0) if y is None else _matrix(y, rows, d, dtype, device, "y")
+    h_, ld_h = (0, 0) if h is None else _matrix(h, rows, d, dtype, device, "h")
+    n_, ld_n = (0, 0) if n is None else _matrix(n, rows, d, dtype, device, "n")
+    codes_, ld_codes = _matrix(codes, rows, d, _E4M3, device, "codes")
+    scales_, ld_scales = _matrix(scales, -(-d // 128), rows, _FLOAT, device, "scales")
+    _call(lib.nmt_op_norm8, device, stream,
+          _NORM8.pack(rows, d, _type_code(dtype, who), _KINDS[kind], eps, resid_scale, ld_x, ld_y, ld_h, ld_n, ld_codes, ld_scales, x_, y_,
+                      _vector(gain, d, dtype, device, "the gain"), 0 if shift is None else _vector(shift, d, dtype, device, "the shift"), h_, n_, codes_, scales_,
+                      0 if stats is None else _vector(stats, 4 * rows, _FLOAT, device, "stats")))
 
 
 def _stack(t, batch, rows, d, dtype, device, what):
     """(address, distance between rows, distance between matrices) of a [rows, d] tensor, or of a [batch, rows, d] one."""
-    if t.dtype is not dtype or t.get_device() != device or t.shape not in ((rows, d), (batch, rows, d)) or (batch != 1 and t.dim() == 2):
-        _refuse(f"{what} is {tuple(t.shape)} {t.dtype} on {t.device}, not ({batch}, {rows}, {d}) {dtype} on device {device}")
-    *many, ld, step = t.stride()
-    if rows <= 1:
-        ld = d
-    stride = many[0] if many and batch > 1 else 0
-    if (step != 1 and d > 1) or ld < d or stride < 0:
-        _refuse(f"{what} has strides {t.stride()}: rows whose elements lie side by side and that do not overlap are taken")
-    return t.data_ptr(), ld, stride
+    strides, shape = t.stride(), t.shape
+    if t.dtype is dtype and t.get_device() == device and ((shape == (rows, d) and batch == 1) or shape == (batch, rows, d)):
+        ld, step = strides[-2:]
+        if rows <= 1:
+            ld = d
+        stride = strides[0] if batch > 1 else 0
+        if (step == 1 or d <= 1) and ld >= d and stride >= 0:
+            return t.data_ptr(), ld, stride
+        _refuse(f"{what} has strides {strides}: rows whose elements lie side by side and that do not overlap are taken")
+    _refuse(f"{what} is {tuple(shape)} {t.dtype} on {t.device}, not ({batch}, {rows}, {d}) {dtype} on device {device}")
 
 
 def _scale_lines(scales, rows, what):
-    """Whether these are the scales of 128 x 128 elements each."""
+    """Whether these are the scales of 128 x 128 elements each, and how many lie side by side."""
     lines = scales.shape[-1] if scales.dim() in (2, 3) else -1
     if lines == rows:
-        return 0
+        return 0, rows
     if lines != -(-rows // 128):
         _refuse(f"{what} are {tuple(scales.shape)}: a column for each of {rows} rows, or for each 128 of them")
-    return 1
+    return 1, lines
 
 
 def nmt_op_gemm8_scratch(M, N, K, batch=1, ranges=False):
@@ -890,32 +893,42 @@ def nmt_op_gemm8(a, a_scales, b, b_scales, c, bias=None, add=None, ranges=None, 
     if c is None or c.dim() not in (2, 3) or a is None or a.dim() not in (2, 3) or b is None or b.dim() not in (2, 3):
         _refuse(f"{who}: a, b and c are tensors of two or three dimensions")
     device, dtype = c.get_device(), c.dtype
-    (M, N), K = c.shape[-2:], a.shape[-1]
-    batch = b.shape[0] if ranges is not None and b.dim() == 3 else 1 if ranges is not None or c.dim() == 2 else c.shape[0]
-    _sizes(who, M, N, K, batch)
-    rows_batch = 1 if ranges is not None else batch
-    if ranges is not None and (c.dim() == 3 or a.dim() == 3):
-        _refuse(f"{who}: experts' rows lie in one matrix")
-    g = nmt_gemm8()
-    g.M, g.N, g.K, g.batch, g.type = M, N, K, batch, _type_code(dtype, who)
-    g.d_a, g.lda, g.stride_a = _stack(a, rows_batch, M, K, _E4M3, device, "a")
-    g.d_b, g.ldb, g.stride_b = _stack(b, batch, N, K, _E4M3, device, "b")
-    g.lda, g.ldb = (-(-K // 16) * 16 if M <= 1 else g.lda), (-(-K // 16) * 16 if N <= 1 else g.ldb)
-    g.d_c, g.ldc, g.stride_c = _stack(c, rows_batch, M, N, dtype, device, "c")
-    blocks = -(-K // 128)
-    g.a_square, g.b_square = _scale_lines(a_scales, M, "a's scales"), _scale_lines(b_scales, N, "b's scales")
-    g.d_sa, g.ld_sa, g.stride_sa = _stack(a_scales, rows_batch, blocks, -(-M // 128) if g.a_square else M, _FLOAT, device, "a's scales")
-    g.d_sb, g.ld_sb, g.stride_sb = _stack(b_scales, batch, blocks, -(-N // 128) if g.b_square else N, _FLOAT, device, "b's scales")
-    if add is not None:
-        g.d_add, g.ld_add, g.stride_add = _stack(add, rows_batch, M, N, dtype, device, "add")
-    if bias is not None:
-        g.d_bias, _, g.stride_bias = _stack(bias.unsqueeze(-2) if bias.dim() == 2 else bias.unsqueeze(0), batch, 1, N, dtype, device, "bias")
+    *many, M, N = c.shape
+    K = a.shape[-1]
+    batch = own = many[0] if many else 1        # (own: products that have an a and a c of their own)
+    ranges_ = add_ = bias_ = scratch_ = ld_add = stride_add = stride_bias = held = 0
     if ranges is not None:
-        g.d_ranges = _vector(ranges, 2 * batch, _INT, device, "ranges")
+        if many or a.dim() == 3:
+            _refuse(f"{who}: experts' rows lie in one matrix")
+        batch = b.shape[0] if b.dim() == 3 else 1
+        ranges_ = _vector(ranges, 2 * batch, _INT, device, "ranges")
+    if M > _MOST or N > _MOST or K > _MOST or batch > _MOST:
+        _sizes(who, M, N, K, batch)
+    a_, lda, stride_a = _stack(a, own, M, K, _E4M3, device, "a")
+    b_, ldb, stride_b = _stack(b, batch, N, K, _E4M3, device, "b")
+    c_, ldc, stride_c = _stack(c, own, M, N, dtype, device, "c")
+    if M <= 1:
+        lda = -(-K // 16) * 16
+    if N <= 1:
+        ldb = -(-K // 16) * 16
+    a_square, a_lines = _scale_lines(a_scales, M, "a's scales")
+    b_square, b_lines = _scale_lines(b_scales, N, "b's scales")
+    blocks = -(-K // 128)
+    sa_, ld_sa, stride_sa = _stack(a_scales, own, blocks, a_lines, _FLOAT, device, "a's scales")
+    sb_, ld_sb, stride_sb = _stack(b_scales, batch, blocks, b_lines, _FLOAT, device, "b's scales")
+    if add is not None:
+        add_, ld_add, stride_add = _stack(add, own, M, N, dtype, device, "add")
+    if bias is not None:
+        if batch == 1 and bias.dim() == 1:
+            bias_ = _vector(bias, N, dtype, device, "bias")
+        else:
+            bias_, _, stride_bias = _stack(bias.unsqueeze(-2), batch, 1, N, dtype, device, "bias")
     if scratch is not None:
-        g.scratch_floats = scratch.numel()
-        g.d_scratch = _vector(scratch, g.scratch_floats, _FLOAT, device, "scratch")
-    _call(lib.nmt_op_gemm8, device, stream, g)
+        held = scratch.numel()
+        scratch_ = _vector(scratch, held, _FLOAT, device, "scratch")
+    _call(lib.nmt_op_gemm8, device, stream,
+          _GEMM8.pack(M, N, K, batch, _type_code(dtype, who), a_square, b_square, lda, ldb, ldc, ld_add, ld_sa, ld_sb, stride_a, stride_b, stride_c, stride_add,
+                      stride_bias, stride_sa, stride_sb, a_, b_, sa_, sb_, bias_, add_, c_, ranges_, scratch_, held))
 
 
 def nmt_op_expert_layer8_scratch(tokens, k, experts, d, ff):
@@ -939,21 +952,22 @@ def nmt_op_expert_layer8(x, expert, weights, up, up_scales, down, down_scales, o
     experts, _, ff = down.shape
     _sizes(who, experts, ff)
     wide = 2 * ff if act == "silu_gate" else ff
-    p = nmt_expert_layer8()
-    p.tokens, p.k, p.experts, p.d, p.ff, p.type, p.act = tokens, k, experts, d, ff, _type_code(dtype, who), _ACTS[act]
-    p.d_x, p.ld_x = _matrix(x, tokens, d, dtype, device, "x")
-    p.d_expert = _vector(expert, tokens * k, _INT, device, "expert")
-    if weights is not None:
-        p.d_weights = _vector(weights, tokens * k, _FLOAT, device, "weights")
-    p.d_up, p.ld_up, p.stride_up = _stack(up, experts, wide, d, _E4M3, device, "up")
-    p.d_down, p.ld_down, p.stride_down = _stack(down, experts, d, ff, _E4M3, device, "down")
-    p.ld_up, p.ld_down = (-(-d // 16) * 16 if wide <= 1 else p.ld_up), (-(-ff // 16) * 16 if d <= 1 else p.ld_down)
-    p.d_up_scales, p.ld_up_scales, p.stride_up_scales = _stack(up_scales, experts, -(-d // 128), -(-wide // 128), _FLOAT, device, "up's scales")
-    p.d_down_scales, p.ld_down_scales, p.stride_down_scales = _stack(down_scales, experts, -(-ff // 128), -(-d // 128), _FLOAT, device, "down's scales")
-    p.d_out, p.ld_out = _matrix(out, tokens, d, dtype, device, "out")
-    if add is not None:
-        p.d_add, p.ld_add = _matrix(add, tokens, d, dtype, device, "add")
+    x_, ld_x = _matrix(x, tokens, d, dtype, device, "x")
+    out_, ld_out = _matrix(out, tokens, d, dtype, device, "out")
+    add_, ld_add = (0, 0) if add is None else _matrix(add, tokens, d, dtype, device, "add")
+    up_, ld_up, stride_up = _stack(up, experts, wide, d, _E4M3, device, "up")
+    down_, ld_down, stride_down = _stack(down, experts, d, ff, _E4M3, device, "down")
+    if wide <= 1:
+        ld_up = -(-d // 16) * 16
+    if d <= 1:
+        ld_down = -(-ff // 16) * 16
+    us_, ld_us, stride_us = _stack(up_scales, experts, -(-d // 128), -(-wide // 128), _FLOAT, device, "up's scales")
+    ds_, ld_ds, stride_ds = _stack(down_scales, experts, -(-ff // 128), -(-d // 128), _FLOAT, device, "down's scales")
+    scratch_ = held = 0
     if scratch is not None:
-        p.scratch_floats = scratch.numel()
-        p.d_scratch = _vector(scratch, p.scratch_floats, _FLOAT, device, "scratch")
-    _call(lib.nmt_op_expert_layer8, device, stream, p)
+        held = scratch.numel()
+        scratch_ = _vector(scratch, held, _FLOAT, device, "scratch")
+    _call(lib.nmt_op_expert_layer8, device, stream,
+          _LAYER8.pack(tokens, k, experts, d, ff, _type_code(dtype, who), _ACTS[act], ld_x, ld_add, ld_out, ld_up, stride_up, ld_us, stride_us, ld_down, stride_down,
+                       ld_ds, stride_ds, x_, _vector(expert, tokens * k, _INT, device, "expert"),
+                       0 if weights is None else _vector(weights, tokens * k, _FLOAT, device, "weights"), up_, us_, down_, ds_, add_, out_, scratch_, held))

@@ -12,45 +12,52 @@ typedef uint32_t code4_t __attribute__((ext_vector_type(4)));                   
 typedef uint32_t code4_any __attribute__((ext_vector_type(4), aligned(1)));         // at any address
 typedef uint32_t code2_any __attribute__((ext_vector_type(2), aligned(1)));         // 8 codes at any address
 
-// Largest magnitude over groups of 16 lanes; every lane gets its group's.
-__device__ __forceinline__ float lanes16_max(float v) {
-  auto meet = [](float x, auto ctrl) {
-    return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, true)));
-  };
+// An element's part in its block's largest magnitude, in an order that unsigned integers have: twice its bits without the sign, and one more in the exponent, which
+// wraps round for what is inf or NaN: that is less than any number's.
+__device__ __forceinline__ uint32_t magnitude8(float x) { return (__float_as_uint(x) << 1) + 0x01000000u; }
+template <int N>
+__device__ __forceinline__ uint32_t magnitude8(const float (&x)[N]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) top = max(top, magnitude8(x[e]));
+  return top;
+}
+// The magnitude itself; 0 if there are no numbers.
+__device__ __forceinline__ float magnitude8_value(uint32_t top) { return top < 0x01000000u ? 0.f : __uint_as_float((top - 0x01000000u) >> 1); }
+// Largest over groups of 16 lanes; every lane gets its group's.
+__device__ __forceinline__ uint32_t lanes16_max(uint32_t v) {
+  auto meet = [](uint32_t x, auto ctrl) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xF, 0xF, true)); };
   v = meet(v, std::integral_constant<int, 0x128>{});  // row_ror:8
   v = meet(v, std::integral_constant<int, 0x124>{});  // row_ror:4
   v = meet(v, std::integral_constant<int, 0x4E>{});   // quad_perm:[2,3,0,1]
   return meet(v, std::integral_constant<int, 0xB1>{});  // quad_perm:[1,0,3,2]
 }
 
-// An element's part in its block's largest magnitude: what is inf or NaN has none.
-__device__ __forceinline__ float magnitude8(float x) {
-  const float a = fabsf(x);
-  return a < __builtin_inff() ? a : 0.f;
-}
-// A block's scale and the scale's reciprocal, each rounded once; nothing is left of a block that is next to nothing.
+// A block's scale, rounded once, and its reciprocal; nothing is left of a block that is next to nothing.
 struct Scale8 { float scale, back; };
-__device__ __forceinline__ Scale8 scale8(float top) {
+__device__ __forceinline__ Scale8 scale8(uint32_t magnitude) {
 #pragma clang fp contract(off)
+  const float top = magnitude8_value(magnitude);
   Scale8 s = {0.f, 0.f};
   if (top > kTiny8) {
     s.scale = top * (1.f / kTop8);
-    s.back = 1.f / s.scale;
+    const float near = __builtin_amdgcn_rcpf(s.scale);  // (no scale is subnormal: one step of Newton's makes it the nearest but for a last bit now and then)
+    s.back = __builtin_fmaf(__builtin_fmaf(-s.scale, near, 1.f), near, near);
   }
   return s;
 }
-// Four codes, nearest, ties to even.  |x back| exceeds 448 by two roundings at most, which the nearest code hides; what is inf or NaN becomes NaN.
+// Four codes, nearest, ties to even.  |x back| exceeds 448 by two roundings at most, which the nearest code hides; an infinity has no code and becomes NaN, as NaN does.
 __device__ __forceinline__ uint32_t codes8(float a, float b, float c, float d, float back) {
 #pragma clang fp contract(off)
-  auto q = [back](float x) { return fabsf(x) < __builtin_inff() ? x * back : __uint_as_float(0x7FC00000u); };
-  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(q(a), q(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q(c), q(d), w, true);
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * back, b * back, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * back, d * back, w, true);
 }
 
-// Eight elements from column c of a row of d on, which may end before them (what is behind it is 0) or before c.  No access hangs on a branch that lanes take differently: of a row of
-// at least 8 columns the last 8 are loaded, and moved up.
+// Eight elements from column c of a row of d on; what is behind the row's end is 0.  No access hangs on a branch that lanes take differently: where eight from c on are not there
+// (RAGGED), the row's last eight are loaded, and moved down.
 template <typename T, bool RAGGED>
 struct Eight {
+  static constexpr int WORDS = 2 * sizeof(T);
   typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
   vec v;
   __device__ __forceinline__ void load(const T* row, int c, int d) {
@@ -60,35 +67,60 @@ struct Eight {
       v = *reinterpret_cast<const vec*>(row + min(c, d - 8));
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = row[min(e, d - 1)];
+      for (int e = 0; e < 8; ++e) v[e] = e < d ? row[e] : T(0);
     }
   }
   __device__ __forceinline__ void get(float (&x)[8], int c, int d) const {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
     if (RAGGED) {
-      const int up = d >= 8 ? c - min(c, d - 8) : 0;
+      struct Words {
+        uint32_t w[WORDS];
+      };
+      Words t = __builtin_bit_cast(Words, v);
+      const int up = d >= 8 ? min(max(c - (d - 8), 0), 8) : min(c, 8);
+      auto down = [&](bool on, int words) {
 #pragma unroll
-      for (int by = 4; by >= 1; by /= 2)
+        for (int i = 0; i < WORDS; ++i) t.w[i] = on ? (i + words < WORDS ? t.w[(i + words) % WORDS] : 0u) : t.w[i];
+      };
+      down(up & 8, WORDS);
+      down(up & 4, WORDS / 2);
+      down(up & 2, WORDS / 4);
+      if constexpr (sizeof(T) == 4) {
+        down(up & 1, 1);
+      } else {
+        const uint32_t by = (up & 1) * 16;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (up & by) && e + by < 8 ? x[(e + by) & 7] : x[e];
+        for (int i = 0; i < WORDS; ++i) t.w[i] = __builtin_amdgcn_alignbit(i + 1 < WORDS ? t.w[(i + 1) % WORDS] : 0u, t.w[i], by);
+      }
+      const vec moved = __builtin_bit_cast(vec, t);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = c + e < d ? x[e] : 0.f;
+      for (int e = 0; e < 8; ++e) x[e] = (float)moved[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
     }
   }
-  static __device__ __forceinline__ void store(T* row, const float (&x)[8], int c, int d) {
-    vec t;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = (T)x[e];
-    if (!RAGGED || c + 8 <= d) {
-      *reinterpret_cast<vec*>(row + c) = t;
+  // Of the n (0 to 8) that are there.
+  static __device__ __forceinline__ void store(T* to, const vec& t, int n) {
+    if (!RAGGED || n >= 8) {
+      *reinterpret_cast<vec*>(to) = t;
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (c + e < d) row[c + e] = t[e];
+        if (e < n) to[e] = t[e];
     }
   }
 };
+// Eight codes, n (0 to 8) of which are there.
+template <bool RAGGED>
+__device__ __forceinline__ void store8(uint8_t* to, uint32_t lo, uint32_t hi, int n) {
+  if (!RAGGED || n >= 8) {
+    *reinterpret_cast<code2_any*>(to) = code2_any{lo, hi};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) to[e] = (uint8_t)((e < 4 ? lo : hi) >> 8 * (e & 3));
+  }
+}
 
 // Eight codes times a power of two as bf16, which holds them exactly.
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));

@@ -26,9 +26,10 @@ struct QuantArgs {
 // the 16 lanes of a row write to different banks.
 // COLS: all 128 columns are there.
 template <typename T, bool COLS>
-__device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, int64_t c0, uint64_t (&turn)[128][16], float (&tops)[4][128]) {
+__device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, int64_t c0, uint64_t (&turn)[128][16], uint32_t (&tops)[4][128]) {
   const int lane16 = threadIdx.x & 15, group = threadIdx.x >> 4, wave = threadIdx.x >> 6;
   const int64_t r = r0 + 8 * group, c = c0 + 8 * lane16;
+  const int rows = (int)min((int64_t)a.rows - r, (int64_t)8), cols = (int)max(min((int64_t)a.d - c, (int64_t)8), (int64_t)0);  // of this thread's (rows may be negative)
   const T* x = static_cast<const T*>(a.x);
   float v[8][8];
   {
@@ -39,20 +40,21 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
     for (int i = 0; i < 8; ++i) {
       t[i].get(v[i], (int)c, a.d);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = r + i < a.rows ? v[i][e] : 0.f;
+      for (int e = 0; e < 8; ++e) v[i][e] = i < rows ? v[i][e] : 0.f;
     }
   }
   Scale8 whole = {0.f, 0.f};
   if (a.square) {
-    float top = 0.f;
+    uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, magnitude8(v[i][e]));
-    top = wave_max(top);
-    if ((threadIdx.x & 63) == 0) tops[wave][0] = top;
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude8(v[i]));
+    top = lanes16_max(top);
+    if (lane16 == 0) tops[0][group] = top;
     __syncthreads();
-    whole = scale8(fmaxf(fmaxf(tops[0][0], tops[1][0]), fmaxf(tops[2][0], tops[3][0])));
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, tops[0][i]);
+    whole = scale8(top);
     if (threadIdx.x == 0) {
       if (a.codes) a.scales[(c0 >> 7) * a.ld_scales + (r0 >> 7)] = whole.scale;
       if (a.codes_t) a.scales_t[(r0 >> 7) * a.ld_scales_t + (c0 >> 7)] = whole.scale;
@@ -63,33 +65,24 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
     for (int i = 0; i < 8; ++i) {
       Scale8 s = whole;
       if (!a.square) {
-        float top = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, magnitude8(v[i][e]));
-        s = scale8(lanes16_max(top));
-        if (lane16 == 0 && r + i < a.rows) a.scales[(c0 >> 7) * a.ld_scales + r + i] = s.scale;
+        s = scale8(lanes16_max(magnitude8(v[i])));
+        if (lane16 == 0 && i < rows) a.scales[(c0 >> 7) * a.ld_scales + r + i] = s.scale;
       }
-      const uint32_t lo = codes8(v[i][0], v[i][1], v[i][2], v[i][3], s.back), hi = codes8(v[i][4], v[i][5], v[i][6], v[i][7], s.back);
-      if (r + i < a.rows) {
-        uint8_t* to = a.codes + (r + i) * a.ld_codes + c;
-        if (COLS || c + 8 <= a.d) {
-          *reinterpret_cast<code2_any*>(to) = code2_any{lo, hi};
-        } else {
-          const uint64_t w = (uint64_t)hi << 32 | lo;
-          for (int e = 0; c + e < a.d; ++e) to[e] = (uint8_t)(w >> 8 * e);
-        }
-      }
+      if (i < rows)
+        store8<!COLS>(a.codes + (r + i) * a.ld_codes + c, codes8(v[i][0], v[i][1], v[i][2], v[i][3], s.back), codes8(v[i][4], v[i][5], v[i][6], v[i][7], s.back), cols);
     }
   }
   if (a.codes_t) {
     if (!a.square) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float top = 0.f;
+        uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, magnitude8(v[i][e]));
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
+        for (int i = 0; i < 8; ++i) top = max(top, magnitude8(v[i][e]));
+        const auto rows16 = __builtin_amdgcn_permlane16_swap(top, top, false, false);
+        top = max(rows16[0], rows16[1]);
+        const auto halves = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+        top = max(halves[0], halves[1]);
         if ((threadIdx.x & 63) < 16) tops[wave][8 * lane16 + e] = top;
       }
       __syncthreads();
@@ -99,8 +92,8 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
       Scale8 s = whole;
       if (!a.square) {
         const int at = 8 * lane16 + e;
-        s = scale8(fmaxf(fmaxf(tops[0][at], tops[1][at]), fmaxf(tops[2][at], tops[3][at])));
-        if (group == 0 && (COLS || c + e < a.d)) a.scales_t[(r0 >> 7) * a.ld_scales_t + c + e] = s.scale;
+        s = scale8(max(max(tops[0][at], tops[1][at]), max(tops[2][at], tops[3][at])));
+        if (group == 0 && e < cols) a.scales_t[(r0 >> 7) * a.ld_scales_t + c + e] = s.scale;
       }
       const uint32_t lo = codes8(v[0][e], v[1][e], v[2][e], v[3][e], s.back), hi = codes8(v[4][e], v[5][e], v[6][e], v[7][e], s.back);
       turn[8 * lane16 + e][group ^ lane16] = (uint64_t)hi << 32 | lo;
@@ -108,17 +101,17 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
     __syncthreads();
     // a column's 128 codes lie with 8 lanes, 16 each
     const int at = threadIdx.x & 7;
+    const int64_t row = r0 + 16 * at;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int col = (threadIdx.x >> 3) + 32 * i, by = col >> 3;
       const uint64_t w0 = turn[col][(2 * at) ^ by], w1 = turn[col][(2 * at + 1) ^ by];
-      if (!COLS && c0 + col >= a.d) continue;
-      const int64_t row = r0 + 16 * at;
+      if (c0 + col >= a.d) continue;
       uint8_t* to = a.codes_t + (c0 + col) * a.ld_codes_t + row;
       if (row + 16 <= a.rows) {
         *reinterpret_cast<code4_any*>(to) = code4_any{(uint32_t)w0, (uint32_t)(w0 >> 32), (uint32_t)w1, (uint32_t)(w1 >> 32)};
       } else {
-        for (int e = 0; row + e < a.rows && e < 16; ++e) to[e] = (uint8_t)((e < 8 ? w0 : w1) >> 8 * (e & 7));
+        for (int e = 0; row + e < a.rows; ++e) to[e] = (uint8_t)((e < 8 ? w0 : w1) >> 8 * (e & 7));
       }
     }
   }
@@ -127,7 +120,7 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
 template <typename T>
 __global__ void __launch_bounds__(kThreads) quantize8_kernel(const QuantArgs a) {
   __shared__ uint64_t turn[128][16];
-  __shared__ float tops[4][128];
+  __shared__ uint32_t tops[4][128];
   const int64_t tile = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   if (tile >= a.tiles) return;
   uint32_t col;
@@ -159,9 +152,12 @@ __global__ void __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) norm8_kernel(con
   const int d = a.d, lane = threadIdx.x % HOLD, worker = threadIdx.x / HOLD, first_wave = worker * WAVES;
   const float inv_d = 1.f / (float)d;
   const int64_t begin = min(((int64_t)blockIdx.x * WORKERS + worker) * a.chunk, (int64_t)a.rows), end = min(begin + a.chunk, (int64_t)a.rows);
-  int at[VECS];
+  int at[VECS], there[VECS];  // the first column of every eight, and how many of them there are
 #pragma unroll
-  for (int i = 0; i < VECS; ++i) at[i] = (lane + i * HOLD) * 8;
+  for (int i = 0; i < VECS; ++i) {
+    at[i] = (lane + i * HOLD) * 8;
+    there[i] = min(max(d - at[i], 0), 8);
+  }
   // (columns past the row's end: its last are loaded, and count as zero)
   const int most = RAGGED ? 0x7FFFFFFF : d - 8;
   const T *x = static_cast<const T*>(a.x), *y = static_cast<const T*>(a.y);
@@ -192,7 +188,7 @@ __global__ void __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) norm8_kernel(con
   if (begin < end) ask(begin);
   // (rows that several wavefronts hold: every worker of a work-group goes round as often, for the barriers)
   for (int64_t row = begin, last = WAVES > 1 ? begin + a.chunk : end; row < last; ++row) {
-    const bool there = row < end;
+    const bool mine = row < end;
     float h[VECS][8];
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
@@ -225,7 +221,7 @@ __global__ void __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) norm8_kernel(con
 #pragma unroll
       for (int i = 0; i < VECS; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[i][e] = (RAGGED ? at[i] + e < d : at[i] <= most) ? h[i][e] - mean : 0.f;
+        for (int e = 0; e < 8; ++e) h[i][e] = (RAGGED ? e < there[i] : at[i] <= most) ? h[i][e] - mean : 0.f;
     }
 #pragma unroll
     for (int i = 0; i < VECS; ++i)
@@ -238,35 +234,24 @@ __global__ void __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) norm8_kernel(con
       float g[8], b[8];
       gain[i].get(g, at[i], d);
       if (a.shift) shift[i].get(b, at[i], d);
-      float top = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         h[i][e] = h[i][e] * rstd * g[e];
         if (a.shift) h[i][e] += b[e];
-        if (RAGGED ? at[i] + e < d : at[i] <= most) top = fmaxf(top, magnitude8(h[i][e]));
       }
-      const Scale8 sc = scale8(lanes16_max(top));
-      if (!there || at[i] >= d) continue;
+      const Scale8 sc = scale8(lanes16_max(RAGGED || at[i] <= most ? magnitude8(h[i]) : 0u));
+      if (!mine || there[i] == 0) continue;
       if ((lane & 15) == 0) a.scales[(int64_t)(at[i] >> 7) * a.ld_scales + row] = sc.scale;
-      const uint32_t lo = codes8(h[i][0], h[i][1], h[i][2], h[i][3], sc.back), hi = codes8(h[i][4], h[i][5], h[i][6], h[i][7], sc.back);
-      uint8_t* to = a.codes + row * a.ld_codes + at[i];
-      if (!RAGGED || at[i] + 8 <= d) {
-        *reinterpret_cast<code2_any*>(to) = code2_any{lo, hi};
-      } else {
-        const uint64_t w = (uint64_t)hi << 32 | lo;
+      store8<RAGGED>(a.codes + row * a.ld_codes + at[i], codes8(h[i][0], h[i][1], h[i][2], h[i][3], sc.back), codes8(h[i][4], h[i][5], h[i][6], h[i][7], sc.back), there[i]);
+      if (a.h) V::store(static_cast<T*>(a.h) + row * a.ld_h + at[i], keep[i].v, there[i]);
+      if (a.n) {
+        typename V::vec t;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (at[i] + e < d) to[e] = (uint8_t)(w >> 8 * e);
+        for (int e = 0; e < 8; ++e) t[e] = (T)h[i][e];
+        V::store(static_cast<T*>(a.n) + row * a.ld_n + at[i], t, there[i]);
       }
-      if (a.h) {
-        float t[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = (float)keep[i].v[e];
-        V::store(static_cast<T*>(a.h) + row * a.ld_h, t, at[i], d);
-      }
-      if (a.n) V::store(static_cast<T*>(a.n) + row * a.ld_n, h[i], at[i], d);
     }
-    if (a.stats && there && lane == 0) *reinterpret_cast<float4_any*>(a.stats + 4 * row) = float4_any{0.f, 1.f, mean, rstd};
+    if (a.stats && mine && lane == 0) *reinterpret_cast<float4_any*>(a.stats + 4 * row) = float4_any{0.f, 1.f, mean, rstd};
   }
 }
 
