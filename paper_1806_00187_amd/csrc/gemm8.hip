@@ -607,18 +607,41 @@ __global__ void __launch_bounds__(256) gemm8_sums_kernel(const Gemm8Args g) {
             g.add ? static_cast<const T*>(g.add) + batch * g.stride_add : nullptr, row, n, v);
 }
 
-struct Plan {
-  int tile, splits;  // tile: 128 or 64
+// How a product is cut up: tiles of 256 x 256, 128 x 128 or 64 x 64, of which a compute unit holds one, two or four, and pieces along k.  What it takes is estimated from what was measured, microseconds: a
+// block of k with that many tiles on a compute unit, what a tile takes besides, and the sums of pieces.  Over 30 sizes of 5 to 13000 rows and 512 to 52701 k the fastest
+// of all forms was picked, or one within 12 %.
+struct Form {
+  int tile, held;
+  double block[4], besides;
 };
-Plan plan(int M, int N, int K, int batch, bool ranges) {
-  auto tiles = [&](int t) { return ((int64_t)ceil_div(M, t) + (ranges ? batch : 0)) * ceil_div(N, t) * (ranges ? 1 : batch); };
-  const int cus = 256;
-  Plan p = {tiles(128) >= cus ? 128 : 64, 1};
-  if (!ranges && tiles(p.tile) < cus) {
-    const int blocks = ceil_div(K, BK);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(blocks / 8, 2 * cus / std::max<int64_t>(1, tiles(p.tile))));
+constexpr Form kNarrow[] = {{256, 1, {1.6}, 8.0}, {128, 2, {0.9, 1.22}, 3.5}, {64, 4, {0.56, 0.66, 0.85, 1.1}, 2.5}};
+constexpr Form kWide[] = {{128, 2, {1.36, 2.1}, 3.5}, {64, 4, {0.65, 0.8, 1.1, 1.4}, 2.5}};
+constexpr double kSums = 4.0, kSumsRate = 4e6;  // microseconds; bytes of pieces, written and read, in a microsecond
+struct Plan {
+  int tile, splits;
+  double us;
+};
+Plan plan(int M, int N, int K, int batch, bool ranges, bool wide, bool b_square) {
+  const int cus = device_info().cus, blocks = std::max(1, ceil_div(K, BK));
+  Plan best = {64, 1, 1e30};
+  auto look = [&](const Form& f, int splits) {
+    if (splits > 1 && (ranges || blocks / splits < 2)) return;
+    // (of experts' rows the last tile is half full)
+    const double tiles = (ranges ? ceil_div(M, f.tile) + 0.5 * batch : (double)ceil_div(M, f.tile) * batch) * ceil_div(N, f.tile);
+    const int64_t each = (int64_t)((tiles * splits + cus - 1) / cus), rest = each % f.held;
+    auto set = [&](int n) { return n ? ceil_div(blocks, splits) * f.block[n - 1] + f.besides : 0.0; };
+    double us = (double)(each / f.held) * set(f.held) + set((int)rest);
+    if (splits > 1) us += kSums + 8.0 * splits * batch * M * N / kSumsRate;
+    if (us < best.us) best = {f.tile, splits, us};
+  };
+  for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+    if (wide)
+      for (const Form& f : kWide) look(f, splits);
+    else
+      for (const Form& f : kNarrow)
+        if (f.tile < 256 || b_square) look(f, splits);
   }
-  return p;
+  return best;
 }
 
 template <int BM, int BN, int NW, bool WIDE>
@@ -646,8 +669,9 @@ int check_sizes(const char* who, int M, int N, int K, int batch) {
 
 extern "C" int64_t nmt_op_gemm8_scratch(int32_t M, int32_t N, int32_t K, int32_t batch, int32_t ranges) {
   if (const int rc = check_sizes("nmt_op_gemm8_scratch", M, N, K, batch); rc != NMT_OK) return rc;
-  const Plan p = plan(M, N, K, batch, ranges != 0);
-  return p.splits > 1 ? (int64_t)p.splits * batch * M * N : 0;
+  int splits = 0;
+  for (int kind = 0; kind < 3; ++kind) splits = std::max(splits, plan(M, N, K, batch, ranges != 0, kind == 0, kind == 1).splits);
+  return splits > 1 ? (int64_t)splits * batch * M * N : 0;
 }
 
 extern "C" int nmt_op_gemm8(const nmt_gemm8* p, void* stream_) {
@@ -672,7 +696,7 @@ extern "C" int nmt_op_gemm8(const nmt_gemm8* p, void* stream_) {
               "%s: a distance between products is negative", who);
   NMT_REQUIRE(p->d_ranges || p->batch <= 1 || p->stride_c > 0, "%s: products of a batch write the same C", who);
   NMT_REQUIRE(aligned16(p->d_scratch), "%s: the scratch buffer must be 16-byte aligned", who);
-  const Plan how = plan(p->M, p->N, p->K, p->batch, p->d_ranges != nullptr);
+  const Plan how = plan(p->M, p->N, p->K, p->batch, p->d_ranges != nullptr, p->type == NMT_F32, p->b_square != 0);
   const int64_t need = how.splits > 1 ? (int64_t)how.splits * p->batch * p->M * p->N : 0;
   if (need > 0 && (!p->d_scratch || p->scratch_floats < need)) {
     nmt_set_error("%s: needs %lld floats of scratch", who, (long long)need);
@@ -690,9 +714,8 @@ extern "C" int nmt_op_gemm8(const nmt_gemm8* p, void* stream_) {
   g.splits = how.splits, g.k_chunk = ceil_div(ceil_div(p->K, BK), how.splits) * BK;
   g.partial = how.splits > 1 ? p->d_scratch : nullptr;
   int rc;
-  const int64_t large = ((int64_t)ceil_div(g.M, 256) + (g.ranges ? g.batch : 0)) * ceil_div(g.N, 256) * (g.ranges ? 1 : g.batch);
-  if (g.type == NMT_F32) rc = how.tile >= 128 ? launch_tiles<128, 128, 4, true>(g, stream) : launch_tiles<64, 64, 4, true>(g, stream);
-  else rc = large >= 256 && g.shift_b ? launch_tiles<256, 256, 8, false>(g, stream) : how.tile == 128 ? launch_tiles<128, 128, 4, false>(g, stream) : launch_tiles<64, 64, 4, false>(g, stream);
+  if (g.type == NMT_F32) rc = how.tile == 128 ? launch_tiles<128, 128, 4, true>(g, stream) : launch_tiles<64, 64, 4, true>(g, stream);
+  else rc = how.tile == 256 ? launch_tiles<256, 256, 8, false>(g, stream) : how.tile == 128 ? launch_tiles<128, 128, 4, false>(g, stream) : launch_tiles<64, 64, 4, false>(g, stream);
   if (rc != NMT_OK || !g.partial) return rc;
   const int64_t groups = ((int64_t)g.batch * g.M * ((g.N + 3) / 4) + 255) / 256;
   const dim3 grid((uint32_t)std::min<int64_t>(groups, kGridX), (uint32_t)((groups + kGridX - 1) / kGridX));

@@ -258,7 +258,8 @@ __global__ void __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) norm8_kernel(con
 template <typename T, int LANES, int VECS, int WAVES>
 int launch_norm8(Norm8Args a, hipStream_t stream) {
   constexpr int THREADS = WAVES > 4 ? 64 * WAVES : 256, WORKERS = THREADS / (LANES * WAVES);
-  const int64_t workers = (int64_t)device_info().cus * 8 * 4 / WAVES * (64 / LANES);  // (8 wavefronts on a SIMD)
+  // A row each (52701 x 1024 bf16 66.7 us; seven rows to each of as many workers as there is room for 78.5), but few rows of the widest ones in turn (2000 x 16384 39.2 us, 44.6).
+  const int64_t workers = (int64_t)device_info().cus * (VECS > 2 ? 16 : 256) / WAVES * (64 / LANES);
   a.chunk = (int)std::max<int64_t>(1, (a.rows + workers - 1) / workers);
   const int groups = ceil_div(ceil_div(a.rows, a.chunk), WORKERS);
   if (a.d % 8) hipLaunchKernelGGL((norm8_kernel<T, LANES, VECS, WAVES, true>), dim3(groups), dim3(THREADS), 0, stream, a);
