@@ -31,51 +31,56 @@ struct Gemm8Args {
   int64_t lda, ldb, ldc, ld_add, ld_sa, ld_sb, stride_a, stride_b, stride_c, stride_add, stride_bias, stride_sa, stride_sb;
   int M, N, K, batch, type, shift_a, shift_b;  // shift: 7 where 128 rows share a scale
   int k_chunk, splits;
-  uint32_t groups, run, rest;  // work-groups; a die's of them (rest: how many dies have one more)
+  uint32_t groups, run, rest, launched;  // tiles; a die's of them (rest: how many dies have one more); work-groups, which take one after the other
   int tiles_m;
   Divisor by_n, by_tiles, by_splits, by_patch, by_rows, by_last;  // columns of tiles; tiles; ...; tiles of kPatch rows; kPatch, and what is left of rows behind the last whole patch
 };
 
-// A stretch of memory that wave instructions read from; what lies behind it arrives as zero.
-struct Stretch {
-  uint64_t base;  // (no address has more than 48 bits)
-  uint32_t bytes;
-};
-__device__ __forceinline__ Stretch stretch(const void* p, uint32_t bytes) {
-  auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
-  return Stretch{(uint64_t)scalar((uint32_t)((uint64_t)p >> 32)) << 32 | scalar((uint32_t)(uint64_t)p), scalar(bytes)};
-}
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_void_ptr)p; }
-// One wave instruction: lane L's SIZE bytes at byte offset `at` land at lds + SIZE L.  Written as an instruction because the compiler holds every read of LDS up until all such
-// requests have arrived; whoever reads what this brings waits for it (arrived()).
+// The kernel's arguments, fetched anew: kept from a tile to the next they would fill the scalar registers.
+__device__ __forceinline__ Gemm8Args arguments() {
+#ifdef __HIP_DEVICE_COMPILE__
+  auto* p = (const __attribute__((address_space(4))) Gemm8Args*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *p;
+#else
+  return {};
+#endif
+}
+// One wave instruction: lane L's SIZE bytes, `at` bytes from base on, land at lds + SIZE L; zeros where `at` is kOob.  Written as an instruction because the compiler holds every read of LDS up
+// until all such requests have arrived; whoever reads what this brings waits for it (arrived()).
 template <int SIZE>
-__device__ __forceinline__ void request_to_lds(const Stretch& from, uint32_t lds, uint32_t at) {
+__device__ __forceinline__ void request_to_lds(uint64_t base, uint32_t lds, uint32_t at) {
   typedef uint32_t rsrc_t __attribute__((ext_vector_type(4)));
-  const rsrc_t s = {(uint32_t)from.base, (uint32_t)(from.base >> 32), from.bytes, 0x00020000u};
+  const rsrc_t s = {(uint32_t)base, (uint32_t)(base >> 32), kOob, 0x00020000u};  // (no address has more than 48 bits)
   if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(s), "s"(lds) : "memory");
   else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(at), "s"(s), "s"(lds) : "memory");
 }
-// All of a wavefront's requests and reads of LDS have arrived; with the barrier behind it, all wavefronts'.
+__device__ __forceinline__ uint64_t scalar(const void* p) {
+  auto one = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+  return (uint64_t)one((uint32_t)((uint64_t)p >> 32)) << 32 | one((uint32_t)(uint64_t)p);
+}
+// All of a wavefront's requests and reads of LDS have arrived, but for the last BUT accesses; with the barrier behind it, all wavefronts'.
+template <int BUT = 0>
 __device__ __forceinline__ void arrived() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(BUT) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
 
 // An operand's tile: R rows of 128 bytes in LDS, chunk p of 16 bytes of row r at p ^ (r >> 1 & 7), so that the 16 rows that a read touches lie on all banks.
-// One wave instruction brings eight rows.  The stretch that it reads from begins with the tile's first row at the block of k at hand and ends with the last code of its last row
-// (with the 16 bytes in which that lies).
+// One wave instruction brings eight rows, from the block of k at hand on; rows that the tile does not have and 16 bytes without a code of their row arrive as zeros.
 template <int R, int NW>
 struct Operand {
   static constexpr int BYTES = R * BK, NV = R / (8 * NW);  // wave instructions of a wavefront and stage
   static_assert(NV >= 1, "");
-  Stretch at;
+  uint64_t at;  // the tile's first row at the block of k at hand
   uint32_t voff[NV];
   int chunk;
-  __device__ __forceinline__ void init(const uint8_t* first, int64_t ld, int rows, int k_left, int wave) {
+  __device__ __forceinline__ void init(const uint8_t* first, int64_t ld, int rows, int wave) {
     const int lane = threadIdx.x & 63, row = 8 * wave + (lane >> 3);
     chunk = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
-    at = stretch(first, (uint32_t)((rows - 1) * ld) + (uint32_t)((max(k_left, 0) + 15) & ~15));
+    at = scalar(first);
 #pragma unroll
     for (int it = 0; it < NV; ++it) voff[it] = row + 8 * NW * it < rows ? (uint32_t)((row + 8 * NW * it) * ld) + (uint32_t)chunk : kOob;
   }
@@ -83,12 +88,7 @@ struct Operand {
   __device__ __forceinline__ void request(uint32_t stage, int k_left, int wave, int it) const {
     request_to_lds<16>(at, stage + (uint32_t)(wave + NW * it) * 1024u, chunk < k_left ? voff[it] : kOob);
   }
-  __device__ __forceinline__ void next() {
-    at.base += BK;
-    uint32_t less = min(at.bytes, (uint32_t)BK);
-    asm volatile("" : "+s"(less));  // (or the compiler makes the two one operation, which the vector unit alone has)
-    at.bytes -= less;
-  }
+  __device__ __forceinline__ void next() { at += BK; }
   // Where a lane reads its part of the fragment of 16 rows; rows 16 on lie 16 * BK on.
   __device__ __forceinline__ static int fragment_at(int row0, int lane) {
     const int row = row0 + (lane & 15);
@@ -117,7 +117,7 @@ template <int BM, int BN, int NW>
 struct Scales {
   static constexpr int PARTS = (BM + BN) / 64;
   static_assert(PARTS <= NW, "");
-  Stretch at;
+  uint64_t at;
   int64_t step;
   uint32_t voff;
   __device__ __forceinline__ void init(const float* sa, int64_t ld_sa, int shift_a, int64_t row_a, int rows_a, const float* sb, int64_t ld_sb, int shift_b,
@@ -125,14 +125,14 @@ struct Scales {
     const bool of_a = wave < BM / 64;
     const int r = 64 * (of_a ? wave : wave - BM / 64) + (int)(threadIdx.x & 63), shift = of_a ? shift_a : shift_b;
     const int64_t row = of_a ? row_a : row_b;
-    at = stretch((of_a ? sa : sb) + (row >> shift), 4u * (BM > BN ? BM : BN));
+    at = scalar((of_a ? sa : sb) + (row >> shift));
     step = (of_a ? ld_sa : ld_sb) * 4;
     voff = r < (of_a ? rows_a : rows_b) ? (uint32_t)(((row + r) >> shift) - (row >> shift)) * 4u : kOob;
   }
   __device__ __forceinline__ void request(uint32_t lds, int k_left, int wave) const {
     if (wave < PARTS) request_to_lds<4>(at, lds + 256u * wave, k_left > 0 ? voff : kOob);
   }
-  __device__ __forceinline__ void next() { at.base += step; }
+  __device__ __forceinline__ void next() { at += step; }
 };
 
 // Which tile a work-group takes.
@@ -140,12 +140,13 @@ struct Place {
   int batch, split, m0, n0, rows, first;  // rows of the tile; first row of the expert's range
 };
 __device__ __forceinline__ bool place(const Gemm8Args& g, uint32_t id, int BM, int BN, Place& p) {
-  // work-groups go round the eight dies; each gets a contiguous run of tiles
-  const uint32_t die = id & 7;
-  uint32_t t = die * g.run + min(die, g.rest) + (id >> 3), col, row, split;
+  // work-groups go round the eight dies; each die gets a contiguous run of tiles
+  const uint32_t die = id & 7, turn = id >> 3;
   p.first = 0;
   if (!g.ranges) {
+    if (id >= g.groups) return false;
     // splits of a product apart, and its tiles in patches: what the compute units of a die work on at a time are a few rows and columns of tiles, whose operands its cache holds
+    uint32_t t = die * g.run + min(die, g.rest) + turn, col, row, split;
     t = div_mod(t, g.by_tiles, row);
     p.batch = (int)div_mod(t, g.by_splits, split);
     p.split = (int)split;
@@ -155,8 +156,6 @@ __device__ __forceinline__ bool place(const Gemm8Args& g, uint32_t id, int BM, i
     p.rows = min(g.M - p.m0, BM);
     return true;
   }
-  t = div_mod(t, g.by_n, col);
-  p.n0 = (int)col * BN;
   p.split = 0;
   const int lane = threadIdx.x & 63, per = (g.batch + 63) / 64;
   auto range = [&](int e, int& first, int& count) {
@@ -173,15 +172,20 @@ __device__ __forceinline__ bool place(const Gemm8Args& g, uint32_t id, int BM, i
     }
   }
   uint32_t sum = mine;
+#pragma unroll
   for (int step = 1; step < 64; step *= 2) {
     const uint32_t up = __shfl_up(sum, step);
     sum += lane >= step ? up : 0;
   }
+  const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)sum, 63) * g.by_n.d;
+  if (id >= all) return false;
+  uint32_t col, t = div_mod(die * (all >> 3) + min(die, all & 7) + turn, g.by_n, col);
+  p.n0 = (int)col * BN;
   const uint64_t behind = __ballot(sum > t);
   if (!behind) return false;
   const int at = __builtin_ctzll(behind);
-  t -= __shfl(sum - mine, at);
-  for (int e = at * per;; ++e) {
+  t -= (uint32_t)__builtin_amdgcn_readlane((int)(sum - mine), at);
+  for (int e = at * per; e < g.batch; ++e) {
     range(e, first, count);
     const uint32_t tiles = (uint32_t)(count + BM - 1) / BM;
     if (t < tiles) {
@@ -193,6 +197,13 @@ __device__ __forceinline__ bool place(const Gemm8Args& g, uint32_t id, int BM, i
     }
     t -= tiles;
   }
+  return false;
+}
+// The same for all lanes, which the compiler does not see.
+__device__ __forceinline__ bool place_scalar(const Gemm8Args& g, uint32_t id, int BM, int BN, Place& p) {
+  const int there = __builtin_amdgcn_readfirstlane(place(g, id, BM, BN, p));
+  for (int* v : {&p.batch, &p.split, &p.m0, &p.n0, &p.rows, &p.first}) *v = __builtin_amdgcn_readfirstlane(*v);
+  return there != 0;
 }
 
 template <typename T>
@@ -243,29 +254,30 @@ struct Codes {
 // What a work-group needs of its product.
 template <int BM, int BN, int NW>
 struct Product {
-  static constexpr int WM = BM / 2, WN = BN / (NW / 2), TM = WM / 16, TN = WN / 16, STAGE = (BM + BN) * BK;
+  static constexpr int WM = BM / 2, WN = BN / (NW / 2), TM = WM / 16, TN = WN / 16, STAGE = (BM + BN) * BK, ROWS_OF_TILE = BM, COLS_OF_TILE = BN, WAVES = NW;
   using OpA = Operand<BM, NW>;
   using OpB = Operand<BN, NW>;
   OpA a;
   OpB b;
   Scales<BM, BN, NW> s;
-  int wave, lane, wm, wn, k_begin, k_end, left;  // left: codes of a row from the block that is asked for next on
-  int64_t row0;
-  __device__ __forceinline__ void init(const Gemm8Args& g, const Place& p) {
+  int wave, lane, wm, wn;
+  int left, length;  // codes of a row from the block that is asked for next on, and in all
+  __device__ __forceinline__ void start() {
     lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     wm = wave % 2 * WM, wn = wave / 2 * WN;
-    k_begin = p.split * g.k_chunk, k_end = min(g.K, k_begin + g.k_chunk);
-    row0 = (int64_t)p.first + p.m0;
-    const int64_t own = g.ranges ? 0 : p.batch;
+  }
+  // The requests go to this tile's operands.
+  __device__ __forceinline__ void aim(const Gemm8Args& g, const Place& p) {
+    const int k_begin = p.split * g.k_chunk, k_end = min(g.K, k_begin + g.k_chunk), block = k_begin / BK;
+    const int64_t own = g.ranges ? 0 : p.batch, row0 = (int64_t)p.first + p.m0;
     const int cols = min(g.N - p.n0, BN);
-    const int block = k_begin / BK;
-    a.init(g.a + own * g.stride_a + row0 * g.lda + k_begin, g.lda, p.rows, k_end - k_begin, wave);
-    b.init(g.b + p.batch * g.stride_b + p.n0 * g.ldb + k_begin, g.ldb, cols, k_end - k_begin, wave);
+    left = length = max(k_end - k_begin, 0);
+    a.init(g.a + own * g.stride_a + row0 * g.lda + k_begin, g.lda, p.rows, wave);
+    b.init(g.b + p.batch * g.stride_b + p.n0 * g.ldb + k_begin, g.ldb, cols, wave);
     s.init(g.sa + own * g.stride_sa + block * g.ld_sa, g.ld_sa, g.shift_a, row0, p.rows, g.sb + p.batch * g.stride_sb + block * g.ld_sb, g.ld_sb, g.shift_b, p.n0, cols, wave);
-    left = k_end - k_begin;
   }
   static constexpr int REQUESTS = OpA::NV + OpB::NV + 1;
-  // The q-th of the requests of a block of k; behind the last, the next block's are at hand.
+  // The q-th of the requests of a block of k; behind the last, the next block's are at hand.  Behind the last block nothing is asked for.
   __device__ __forceinline__ void request(uint32_t stage, uint32_t scales, int q) {
     if (q < OpA::NV) a.request(stage, left, wave, q);
     else if (q < OpA::NV + OpB::NV) b.request(stage + OpA::BYTES, left, wave, q - OpA::NV);
@@ -278,12 +290,11 @@ struct Product {
 #pragma unroll
     for (int q = 0; q < REQUESTS; ++q) request(stage, scales, q);
   }
-  // Behind the barrier that publishes a stage.
-  __device__ __forceinline__ void tail(unsigned char* stage, int k) const {
-    const int left = k_end - k;
-    if (left > 0 && left < BK && (left & 15)) {
-      OpA::clear_tail(stage, left);
-      OpB::clear_tail(stage + OpA::BYTES, left);
+  // Behind the barrier that publishes a stage; codes: of a row from its block on.
+  __device__ __forceinline__ static void tail(unsigned char* stage, int codes) {
+    if (__builtin_expect(codes > 0 && codes < BK && (codes & 15), 0)) {
+      OpA::clear_tail(stage, codes);
+      OpB::clear_tail(stage + OpA::BYTES, codes);
       __syncthreads();
     }
   }
@@ -322,9 +333,12 @@ struct Strips : Product<BM, BN, NW> {
   static constexpr int slot_i(int q) { return q < ROWS * TN ? q / TN : strip_of((q - ROWS * TN) % G); }
   static constexpr int slot_j(int q) { return q < ROWS * TN ? q % TN : (q - ROWS * TN) / G; }
 
-  __device__ __forceinline__ void start() {
+  __device__ __forceinline__ void begin() {
     at_a = OpA::fragment_at(this->wm, this->lane), at_b = OpA::BYTES + OpB::fragment_at(this->wn, this->lane);
     at_sm = this->wm + (this->lane & 15), at_sn = BM + this->wn + 4 * (this->lane >> 4);
+    clear();
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -360,52 +374,99 @@ struct Strips : Product<BM, BN, NW> {
     for (int e = 0; e < 4; ++e) c[e] = __builtin_fmaf(t[r][e], BFINE ? by4[BFINE ? r : 0][e] : by[BFINE ? 0 : PER_STRIP ? slot_i(slot) % 4 : r], c[e]);
     asm volatile("" : "+v"(c[0]), "+v"(c[1]), "+v"(c[2]), "+v"(c[3]));  // (here and not behind a branch)
   }
-  // One block of k from stage `from`; the next is in or on its way to `to`, the one after goes to `from`.
-  __device__ __forceinline__ void block(unsigned char* from, float* scales_from, unsigned char* to, float* scales_to, int k) {
+  __device__ __forceinline__ void multiply(int q) {
+    const int i = slot_i(q), j = slot_j(q), r = q % RING;
+    t[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i % G], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+    if constexpr (BFINE) by4[r] = floatx4{sn4[j].x * sm[i % G], sn4[j].y * sm[i % G], sn4[j].z * sm[i % G], sn4[j].w * sm[i % G]};
+    else if (!PER_STRIP) by[r] = sm[i % G] * sn[0];
+    add(q - LAG);
+    if (PER_STRIP && j == 0) by[i % 4] = sm[i % G] * sn[0];
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // One block of k from stage `from`; the next is in or on its way to `to`, where a row has `codes` from there on; the one after goes to `from`.  aim(): the requests go on to the next tile's operands, if
+  // there is one.  The wavefront may have STORES stores behind those requests under way, which need not be waited for.
+  template <int STORES, typename Aim>
+  __device__ __forceinline__ void block(unsigned char* from, float* scales_from, unsigned char* to, float* scales_to, int codes, bool stores, Aim aim) {
     const uint32_t to_stage = lds_address(from), to_scales = lds_address(scales_from);
 #pragma unroll
-    for (int q = 0; q < SLOTS; ++q) {
-      if (q == ROWS * TN) {
-        arrived();  // (the next stage's requests, this one's fragments)
-        this->tail(to, k + BK);
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (!BFINE) sn[1] = scales_to[BM + this->wn];
-      }
-      const int i = slot_i(q), j = slot_j(q), r = q % RING;
-      t[r] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i % G], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-      if constexpr (BFINE) by4[r] = floatx4{sn4[j].x * sm[i % G], sn4[j].y * sm[i % G], sn4[j].z * sm[i % G], sn4[j].w * sm[i % G]};
-      else if (!PER_STRIP) by[r] = sm[i % G] * sn[0];
-      add(q - LAG);
-      if (PER_STRIP && j == 0) by[i % 4] = sm[i % G] * sn[0];
+    for (int q = 0; q < ROWS * TN; ++q) {
+      multiply(q);
+      if (slot_j(q) == TN - 1) fetch_a(from, scales_from, slot_i(q) + G);
       __builtin_amdgcn_sched_barrier(0);
-      if (q < ROWS * TN) {
-        if (j == TN - 1) fetch_a(from, scales_from, i + G);
-      } else {
-        const int c = q - ROWS * TN, n = G * TN;
-        if (j == TN - 1) fetch_a(to, scales_to, c % G);
-        if (c % G == G - 1) fetch_b(to, scales_to, j);
+    }
+    if (STORES > 0 && stores) arrived<STORES>();
+    else arrived();  // (the next stage's requests, this one's fragments)
+    this->tail(to, codes);
+    if (__builtin_expect(this->left <= 0, 0)) aim();
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (!BFINE) sn[1] = scales_to[BM + this->wn];
 #pragma unroll
-        for (int x = c * P::REQUESTS / n; x < (c + 1) * P::REQUESTS / n; ++x) this->request(to_stage, to_scales, x);
-      }
+    for (int c = 0; c < G * TN; ++c) {
+      const int q = ROWS * TN + c, j = slot_j(q);
+      multiply(q);
+      if (j == TN - 1) fetch_a(to, scales_to, c % G);
+      if (c % G == G - 1) fetch_b(to, scales_to, j);
+#pragma unroll
+      for (int x = c * P::REQUESTS / (G * TN); x < (c + 1) * P::REQUESTS / (G * TN); ++x) this->request(to_stage, to_scales, x);
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (!BFINE) sn[0] = sn[1];
   }
-  __device__ __forceinline__ void run(unsigned char* stages, float* scales) {
-    start();
+  // One tile after the other, from work-group to work-group of the grid: the requests of a tile's last blocks are the next one's first, which arrive while results are written.
+  // finish(place): writes acc; returns whether that took STORES stores.
+  template <int STORES, typename Finish>
+  __device__ __forceinline__ void run(const Gemm8Args& g, uint32_t id, Place& at, unsigned char* stages, float* scales, Finish finish) {
+    this->start();
+    this->aim(g, at);
+    begin();
     this->request_all(lds_address(stages), lds_address(scales));
     __builtin_amdgcn_sched_barrier(0);
+    int codes = this->length;
     this->request_all(lds_address(stages + P::STAGE), lds_address(scales + BM + BN));
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(P::REQUESTS - 1) : "memory");  // (the first stage's; a wavefront may have no scales to bring)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    this->tail(stages, this->k_begin);
+    this->tail(stages, codes);
     first(stages, scales);
+    Place next = at;
+    bool more = false, stores = false;
+    auto aim = [&] {
+      if constexpr (STORES > 0) {
+        const Gemm8Args g = arguments();
+        if (id + g.launched >= g.groups) return;
+        more = place_scalar(g, id + g.launched, BM, BN, next);
+        if (!more) return;
+        id += g.launched;
+        this->aim(g, next);
+      }
+    };
     int s = 0;
-    for (int k = this->k_begin; k < this->k_end; k += BK, s ^= 1)
-      block(stages + s * P::STAGE, scales + s * (BM + BN), stages + (s ^ 1) * P::STAGE, scales + (s ^ 1) * (BM + BN), k);
+    auto one = [&] {
+      const int behind = codes > BK ? codes - BK : more ? this->length : 0;
+      block<STORES>(stages + s * P::STAGE, scales + s * (BM + BN), stages + (s ^ 1) * P::STAGE, scales + (s ^ 1) * (BM + BN), behind, stores, aim);
+      codes -= BK, s ^= 1;
+    };
+    auto rest = [&] {
 #pragma unroll
-    for (int q = -LAG; q < 0; ++q) add(q);
+      for (int q = -LAG; q < 0; ++q) add(q);
+    };
+    if constexpr (STORES == 0) {
+      while (codes > 0) one();
+      rest();
+      finish(at);
+    } else {
+      for (;;) {  // (one loop: of one in another the compiler keeps two sets of sums)
+        if (__builtin_expect(codes > 0, 1)) one();
+        stores = false;
+        if (__builtin_expect(codes > 0, 1)) continue;
+        rest();
+        stores = finish(at);
+        if (!more) break;
+        clear();
+        first(stages + s * P::STAGE, scales + s * (BM + BN));  // (once more: registers do not hold them while results are written)
+        at = next, more = false, codes = this->length;
+      }
+    }
     arrived();  // (requests past the end, of nothing, which write zeros)
   }
 };
@@ -442,151 +503,161 @@ struct Wide : Product<BM, BN, NW> {
       }
     }
   }
-  __device__ __forceinline__ void run(unsigned char* stages, float* scales) {
+  template <int, typename Finish>
+  __device__ __forceinline__ void run(const Gemm8Args& g, uint32_t, Place& at, unsigned char* stages, float* scales, Finish finish) {
+    this->start();
+    this->aim(g, at);
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     this->request_all(lds_address(stages), lds_address(scales));
     arrived();
-    this->tail(stages, this->k_begin);
+    this->tail(stages, this->length);
     int s = 0;
-    for (int k = this->k_begin; k < this->k_end; k += BK, s ^= 1) {
+    for (int codes = this->length; codes > 0; codes -= BK, s ^= 1) {
       this->request_all(lds_address(stages + (s ^ 1) * P::STAGE), lds_address(scales + (s ^ 1) * (BM + BN)));
       __builtin_amdgcn_sched_barrier(0);
       block(stages + s * P::STAGE, scales + s * (BM + BN));
       arrived();
-      this->tail(stages + (s ^ 1) * P::STAGE, k + BK);
+      this->tail(stages + (s ^ 1) * P::STAGE, codes - BK);
     }
+    finish(at);
   }
 };
 
 // A wavefront's share of C: strips of 16 rows turn round in LDS, so that lanes write 16 bytes each and a row's lie side by side.
 template <typename Loop, typename T>
 struct Result {
-  static constexpr int TM = Loop::TM, TN = Loop::TN, WN = Loop::WN, E = 16 / sizeof(T), LANES = WN / E, ROWS = 64 / LANES, N = 16 / ROWS, PITCH = WN + 4;
-  static constexpr int FLOATS = 16 * PITCH;
-  static_assert(N >= 1 && FLOATS * 4 * (Loop::STAGE == 512 * BK ? 8 : 4) <= 2 * Loop::STAGE, "");
+  static constexpr int TM = Loop::TM, TN = Loop::TN, WN = Loop::WN, E = 16 / sizeof(T), LANES = WN / E, ROWS = 64 / LANES, N = 16 / ROWS, PITCH = WN + E;
+  static constexpr int BYTES = 16 * PITCH * sizeof(T), STORES = TM * N;
+  static_assert(N >= 1, "");
   typedef T vec __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+  typedef T lds_vec __attribute__((ext_vector_type(E)));
   typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-  T* c;
-  const T* add;
-  int64_t ldc, ld_add;
-  int left, rows, row;  // columns from this lane's on; rows of the strips from the first on; this lane's of them
-  float bias[TN][4];
-  vec next[N];
-  __device__ __forceinline__ Result(const Loop& l, T* c_, int64_t ldc_, const T* bias_, const T* add_, int64_t ld_add_, const Place& p, int cols) {
-    const int n0 = p.n0 + l.wn, col = l.lane % LANES * E;
-    row = l.lane / LANES;
-    left = cols - n0 - col;
-    rows = p.rows - l.wm;
-    ldc = ldc_, ld_add = ld_add_;
-    const int64_t first = l.row0 + l.wm + row;
-    c = c_ + first * ldc + n0 + col;
-    add = add_ ? add_ + first * ld_add + n0 + col : nullptr;
+  typedef T lds_four __attribute__((ext_vector_type(4)));
+  // Of n columns those that are there, from `from` on.
+  static __device__ __forceinline__ four ask(const T* from, int n) {
+    four v = {};
+    if (n >= 4) {
+      v = *reinterpret_cast<const four*>(from);
+    } else {
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int n = n0 + 16 * j + 4 * (l.lane >> 4);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) bias[j][e] = 0.f;
-      if (bias_) {
-        if (cols >= 4) {  // (columns behind the last go nowhere: the last four's are as good)
-          const int at = min(n, cols - 4);
-          const four b = *reinterpret_cast<const four*>(bias_ + at);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int o = 0; o < 4; ++o) bias[j][e] = n + e == at + o ? (float)b[o] : bias[j][e];
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) bias[j][e] = (float)bias_[min(n + e, cols - 1)];
-        }
-      }
+      for (int e = 0; e < 3; ++e)
+        if (e < n) v[e] = from[e];
     }
-    if (add) ask(0);
+    return v;
   }
-  __device__ __forceinline__ void ask(int i) {
+  // ALL: all of the share is there.  ADD: something may be added to it.
+  template <bool ALL, bool ADD>
+  static __device__ __forceinline__ void strips(const Loop& l, int rows, int cols, T* c, int64_t ldc, const T* add, int64_t ld_add, T* turn) {
+    // as results lie in registers ...
+    const int m = l.lane & 15, n = 4 * (l.lane >> 4);
+    four plus[TN], next[TN];
+    auto ask_strip = [&](int i) {
 #pragma unroll
-    for (int x = 0; x < N; ++x) {
-      const T* from = add + (16 * i + ROWS * x) * ld_add;
-      if (16 * i + ROWS * x + row >= rows) continue;
-      if (left >= E) {
-        next[x] = *reinterpret_cast<const vec*>(from);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (e < left) next[x][e] = from[e];
-      }
-    }
-  }
-  __device__ __forceinline__ void store(const Loop& l, float* turn) {
+      for (int j = 0; j < TN; ++j) next[j] = ask(add + (int64_t)(16 * i + m) * ld_add + n + 16 * j, 16 * i + m < rows ? cols - (n + 16 * j) : 0);
+    };
+    if (ADD && add) ask_strip(0);
+    // ... and as they are written
+    const int row = l.lane / LANES, col = l.lane % LANES * E;
+    T* to = c + (int64_t)row * ldc + col;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      vec plus[N];
+      if (ADD && add) {
 #pragma unroll
-      for (int x = 0; x < N; ++x) plus[x] = next[x];
-      if (add && i + 1 < TM) ask(i + 1);
+        for (int j = 0; j < TN; ++j) plus[j] = next[j];
+        if (i + 1 < TM) ask_strip(i + 1);
+      }
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
-        *reinterpret_cast<float4*>(turn + (l.lane & 15) * PITCH + 16 * j + 4 * (l.lane >> 4)) =
-            float4{l.acc[i][j][0] + bias[j][0], l.acc[i][j][1] + bias[j][1], l.acc[i][j][2] + bias[j][2], l.acc[i][j][3] + bias[j][3]};
+      for (int j = 0; j < TN; ++j) {
+        lds_four o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (T)(ADD && add ? l.acc[i][j][e] + (float)plus[j][e] : l.acc[i][j][e]);
+        *reinterpret_cast<lds_four*>(turn + m * PITCH + 16 * j + n) = o;
+      }
       wave_sync();
 #pragma unroll
       for (int x = 0; x < N; ++x) {
-        float v[E];
-        const float* from = turn + (ROWS * x + row) * PITCH + l.lane % LANES * E;
+        const lds_vec o = *reinterpret_cast<const lds_vec*>(turn + (ROWS * x + row) * PITCH + col);
+        if (ALL || (16 * i + ROWS * x + row < rows && col + E <= cols)) {
+          __builtin_nontemporal_store((vec)o, reinterpret_cast<vec*>(to));
+        } else if (16 * i + ROWS * x + row < rows) {
 #pragma unroll
-        for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(v + e) = *reinterpret_cast<const float4*>(from + e);
-        vec o;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = (T)(add ? v[e] + (float)plus[x][e] : v[e]);
-        if (16 * i + ROWS * x + row >= rows) continue;
-        T* to = c + (16 * i + ROWS * x) * ldc;
-        if (left >= E) {
-          __builtin_nontemporal_store(o, reinterpret_cast<vec*>(to));
-        } else {
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (e < left) to[e] = o[e];
+          for (int e = 0; e < E - 1; ++e)
+            if (col + e < cols) to[e] = o[e];
         }
+        to += ROWS * ldc;
       }
       wave_sync();
     }
   }
+  // c, add: of the product; bias: of its columns.  Returns whether all of the share was there, and written with STORES stores.
+  template <bool ADD = true>
+  static __device__ __forceinline__ bool store(Loop& l, const Place& p, int all_cols, T* c, int64_t ldc, const T* bias, const T* add, int64_t ld_add, unsigned char* turn_) {
+    T* turn = reinterpret_cast<T*>(turn_);
+    const int n0 = p.n0 + l.wn, rows = p.rows - l.wm, cols = all_cols - n0;  // of the share
+    const int64_t row0 = (int64_t)p.first + p.m0 + l.wm;
+    if (bias) {
+      const int n = 4 * (l.lane >> 4);
+      four b[TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) b[j] = ask(bias + n0 + n + 16 * j, cols - (n + 16 * j));
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) l.acc[i][j][e] += (float)b[j][e];
+    }
+    c += row0 * ldc + n0;
+    if (rows >= 16 * TM && cols >= WN && (!ADD || !add)) {
+      strips<true, false>(l, rows, cols, c, ldc, nullptr, 0, turn);
+      return true;
+    }
+    strips<false, ADD>(l, rows, cols, c, ldc, add ? add + row0 * ld_add + n0 : nullptr, ld_add, turn);
+    return false;
+  }
 };
 
-// BM x BN of C by NW wavefronts, two of them along m.
-template <int BM, int BN, int NW, bool BFINE, bool WIDE>
-__global__ void __launch_bounds__(64 * NW, 2) gemm8_kernel(const Gemm8Args g) {
+// BM x BN of C by NW wavefronts, two of them along m.  WIDE: codes as bf16, C in fp32.  TURNS, a type and not void: C is of that type, nothing is added to it, and a work-group takes one tile after the
+// other: the next one's first blocks arrive while results are written, which turn round in LDS of their own.
+template <int BM, int BN, int NW, bool BFINE, bool WIDE, typename TURNS>
+__global__ void __launch_bounds__(64 * NW, BM == 64 ? 4 : 2) gemm8_kernel(const Gemm8Args g) {
   using Loop = std::conditional_t<WIDE, Wide<BM, BN, NW, BFINE>, Strips<BM, BN, NW, BFINE>>;
-  constexpr int TM = Loop::TM, TN = Loop::TN;
   __shared__ __attribute__((aligned(1024))) unsigned char stages[2 * Loop::STAGE];
   __shared__ __attribute__((aligned(16))) float scales[2 * (BM + BN)];
   touch(g);
   const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
   Place p;
-  if (id >= g.groups || !place(g, id, BM, BN, p)) return;
-  // (the same for all lanes, which the compiler does not see)
-  for (int* v : {&p.batch, &p.split, &p.m0, &p.n0, &p.rows, &p.first}) *v = __builtin_amdgcn_readfirstlane(*v);
+  if (!place_scalar(g, id, BM, BN, p)) return;
   Loop l;
-  l.init(g, p);
-  l.run(stages, scales);
-  float* turn = reinterpret_cast<float*>(stages) + l.wave * Result<Loop, float>::FLOATS;
-  const int64_t own = g.ranges ? 0 : p.batch;
-  if (g.partial) {
-    Result<Loop, float> r(l, g.partial + ((int64_t)p.batch * g.splits + p.split) * g.M * g.N, g.N, nullptr, nullptr, 0, p, g.N);
-    r.store(l, turn);
-    return;
+  if constexpr (!std::is_same_v<TURNS, void>) {
+    using R = Result<Loop, TURNS>;
+    __shared__ __attribute__((aligned(16))) unsigned char turns[NW * R::BYTES];
+    l.template run<R::STORES>(g, id, p, stages, scales, [&](const Place& at) {
+      const Gemm8Args g = arguments();
+      const int64_t own = g.ranges ? 0 : at.batch;
+      return R::template store<false>(l, at, g.N, static_cast<TURNS*>(g.c) + own * g.stride_c, g.ldc, g.bias ? static_cast<const TURNS*>(g.bias) + at.batch * g.stride_bias : nullptr,
+                                      nullptr, 0, turns + l.wave * R::BYTES);
+    });
+  } else {
+    static_assert(NW * Result<Loop, float>::BYTES <= 2 * Loop::STAGE, "");
+    l.template run<0>(g, id, p, stages, scales, [&](const Place& at) {
+      const int64_t own = g.ranges ? 0 : at.batch;
+      arrived();  // (the stages are free)
+      auto out = [&](auto type, void* c, int64_t ldc, bool whole) {
+        using T = decltype(type);
+        using R = Result<Loop, T>;
+        R::store(l, at, g.N, static_cast<T*>(c), ldc, whole && g.bias ? static_cast<const T*>(g.bias) + at.batch * g.stride_bias : nullptr,
+                 whole && g.add ? static_cast<const T*>(g.add) + own * g.stride_add : nullptr, g.ld_add, stages + l.wave * R::BYTES);
+      };
+      if (g.partial) out(float(), g.partial + ((int64_t)at.batch * g.splits + at.split) * g.M * g.N, g.N, false);
+      else if constexpr (WIDE) out(float(), static_cast<float*>(g.c) + own * g.stride_c, g.ldc, true);
+      else if (g.type == NMT_F16) out(half_t(), static_cast<half_t*>(g.c) + own * g.stride_c, g.ldc, true);
+      else out(bf16_t(), static_cast<bf16_t*>(g.c) + own * g.stride_c, g.ldc, true);
+    });
   }
-  auto out = [&](auto type) {
-    using T = decltype(type);
-    Result<Loop, T> r(l, static_cast<T*>(g.c) + own * g.stride_c, g.ldc, g.bias ? static_cast<const T*>(g.bias) + p.batch * g.stride_bias : nullptr,
-                      g.add ? static_cast<const T*>(g.add) + own * g.stride_add : nullptr, g.ld_add, p, g.N);
-    r.store(l, turn);
-  };
-  if constexpr (WIDE) out(float());
-  else if (g.type == NMT_F16) out(half_t());
-  else out(bf16_t());
 }
 
 // The pieces' sums in increasing k, and what comes behind a product.
@@ -651,9 +722,20 @@ int launch_tiles(Gemm8Args g, hipStream_t stream) {
   g.groups = (uint32_t)groups, g.run = g.groups / 8, g.rest = g.groups % 8;
   g.tiles_m = (int)tiles_m, g.by_n = divisor((uint32_t)tiles_n), g.by_tiles = divisor((uint32_t)(tiles_m * tiles_n)), g.by_splits = divisor((uint32_t)g.splits);
   g.by_patch = divisor((uint32_t)(kPatch * tiles_n)), g.by_rows = divisor(kPatch), g.by_last = divisor((uint32_t)std::max<int64_t>(1, tiles_m % kPatch));
-  const dim3 grid((uint32_t)std::min<int64_t>(groups, kGridX), (uint32_t)((groups + kGridX - 1) / kGridX));
-  if (!WIDE && g.shift_b) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, WIDE>), grid, dim3(64 * NW), 0, stream, g);
-  else if constexpr (BM < 256) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, true, WIDE>), grid, dim3(64 * NW), 0, stream, g);
+  // Tiles of 256 x 256: a work-group on each compute unit takes one after the other, where the requests of two blocks are of one tile or of two.
+  const bool turns = BM == 256 && g.splits == 1 && g.K > BK && !g.add;
+  const int64_t launched = turns ? std::min<int64_t>(groups, device_info().cus / 8 * 8) : groups;
+  g.launched = (uint32_t)launched;
+  const dim3 grid((uint32_t)std::min<int64_t>(launched, kGridX), (uint32_t)((launched + kGridX - 1) / kGridX)), threads(64 * NW);
+  if constexpr (BM == 256) {
+    if (turns && g.type == NMT_F16) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, false, half_t>), grid, threads, 0, stream, g);
+    else if (turns) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, false, bf16_t>), grid, threads, 0, stream, g);
+    else hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, false, void>), grid, threads, 0, stream, g);
+  } else if (!WIDE && g.shift_b) {
+    hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, WIDE, void>), grid, threads, 0, stream, g);
+  } else {
+    hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, true, WIDE, void>), grid, threads, 0, stream, g);
+  }
   NMT_LAUNCH_CHECK();
   return NMT_OK;
 }
