@@ -685,7 +685,7 @@ struct Form {
   int tile, held;
   double block[4], besides;
 };
-constexpr Form kNarrow[] = {{256, 1, {1.6}, 8.0}, {128, 2, {0.9, 1.22}, 3.5}, {64, 4, {0.56, 0.66, 0.85, 1.1}, 2.5}};
+constexpr Form kNarrow[] = {{256, 1, {1.6}, 5.0}, {128, 2, {0.9, 1.22}, 3.5}, {64, 4, {0.56, 0.66, 0.85, 1.1}, 2.5}};
 constexpr Form kWide[] = {{128, 2, {1.36, 2.1}, 3.5}, {64, 4, {0.65, 0.8, 1.1, 1.4}, 2.5}};
 constexpr double kSums = 4.0, kSumsRate = 4e6;  // microseconds; bytes of pieces, written and read, in a microsecond
 struct Plan {
