@@ -243,12 +243,6 @@ struct Codes {
 #pragma unroll
     for (int q = 0; q < 4; ++q) f[q] = widen8((uint32_t)v[2 * q], (uint32_t)v[2 * q + 1]);
   }
-  __device__ __forceinline__ floatx4 times(const Codes& o) const {
-    floatx4 t = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int q = 0; q < 4; ++q) t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[q], o.f[q], t, 0, 0, 0);
-    return t;
-  }
 };
 
 // What a work-group needs of its product.
@@ -471,46 +465,63 @@ struct Strips : Product<BM, BN, NW> {
   }
 };
 
-// Codes as bf16, for results in fp32.
+// Codes as bf16, for results in fp32.  B's fragments of a block of k are widened once, A's strip by strip; a strip's sums are multiplied by their scales while the next strip's are formed.
 template <int BM, int BN, int NW, bool BFINE>
 struct Wide : Product<BM, BN, NW> {
   using P = Product<BM, BN, NW>;
   using typename P::OpA;
   using typename P::OpB;
   static constexpr int TM = P::TM, TN = P::TN;
-  floatx4 acc[TM][TN];
+  float acc[TM][TN][4];
+  int at_a, at_b, at_sm, at_sn;
   __device__ __forceinline__ void block(const unsigned char* stage, const float* scales) {
-    const int at_a = OpA::fragment_at(this->wm, this->lane), at_b = OpA::BYTES + OpB::fragment_at(this->wn, this->lane);
     Codes fb[TN];
     float4 sn[TN];
+    floatx4 t[2][TN];
+    frag_t raw = OpA::fragment(stage, at_a, 0);
+    float sm[2];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       fb[j].set(OpB::fragment(stage, at_b, j));
-      sn[j] = *reinterpret_cast<const float4*>(scales + BM + this->wn + 16 * j + 4 * (this->lane >> 4));
+      sn[j] = *reinterpret_cast<const float4*>(scales + at_sn + 16 * j);
     }
+    auto add = [&](int i) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const floatx4& v = t[i % 2][j];
+        acc[i][j][0] = __builtin_fmaf(v[0], sn[j].x * sm[i % 2], acc[i][j][0]);
+        acc[i][j][1] = __builtin_fmaf(v[1], sn[j].y * sm[i % 2], acc[i][j][1]);
+        acc[i][j][2] = __builtin_fmaf(v[2], sn[j].z * sm[i % 2], acc[i][j][2]);
+        acc[i][j][3] = __builtin_fmaf(v[3], sn[j].w * sm[i % 2], acc[i][j][3]);
+      }
+    };
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       Codes fa;
-      fa.set(OpA::fragment(stage, at_a, i));
-      const float sm = scales[this->wm + 16 * i + (this->lane & 15)];
+      fa.set(raw);
+      sm[i % 2] = scales[at_sm + 16 * i];
+      if (i + 1 < TM) raw = OpA::fragment(stage, at_a, i + 1);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const floatx4 t = fb[j].times(fa);
-        acc[i][j][0] = __builtin_fmaf(t[0], sn[j].x * sm, acc[i][j][0]);
-        acc[i][j][1] = __builtin_fmaf(t[1], sn[j].y * sm, acc[i][j][1]);
-        acc[i][j][2] = __builtin_fmaf(t[2], sn[j].z * sm, acc[i][j][2]);
-        acc[i][j][3] = __builtin_fmaf(t[3], sn[j].w * sm, acc[i][j][3]);
-      }
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) t[i % 2][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j].f[q], fa.f[q], q ? t[i % 2][j] : floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      if (i > 0) add(i - 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    add(TM - 1);
   }
   template <int, typename Finish>
   __device__ __forceinline__ void run(const Gemm8Args& g, uint32_t, Place& at, unsigned char* stages, float* scales, Finish finish) {
     this->start();
     this->aim(g, at);
+    at_a = OpA::fragment_at(this->wm, this->lane), at_b = OpA::BYTES + OpB::fragment_at(this->wn, this->lane);
+    at_sm = this->wm + (this->lane & 15), at_sn = BM + this->wn + 4 * (this->lane >> 4);
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.f;
     this->request_all(lds_address(stages), lds_address(scales));
     arrived();
     this->tail(stages, this->length);
