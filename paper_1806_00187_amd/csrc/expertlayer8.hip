@@ -25,7 +25,7 @@ struct LayerArgs {
   __bf16* hidden;        // ... or hidden, ld_hidden
   int64_t ld_hidden, ld_x, ld, stride, ld_scales, stride_scales;
   int n, experts, by_expert;  // choices; by_expert: a work-group's first index is an expert, not a choice
-  int rows, width;            // rows: of the result; width: of x
+  int rows, width, piece;     // rows: of the result; width: of x; piece: blocks of it that a work-group of the second product takes
   Divisor by_k;               // choices of a token
 };
 
@@ -197,7 +197,7 @@ struct Block {
 // ROWS: a wavefront of a work-group has 16 rows of its own, and inputs are split once for all of them, a stretch of kStretch at a time, in LDS.  Otherwise the work-group has 16 rows, each wavefront every
 // kWaves-th block of them, and splits its own inputs: for layers that leave compute units idle.
 template <typename Source, int HIDDEN, bool GATED, bool ROWS>
-__global__ void __launch_bounds__(kThreads) layer8_product_kernel(const LayerArgs a) {
+__global__ void __launch_bounds__(kThreads, ROWS ? 4 : 2) layer8_product_kernel(const LayerArgs a) {
   constexpr bool UP = HIDDEN > 0;
   constexpr int PARTS = Source::kParts, HALVES = GATED ? 2 : 1, PITCH = kStretch + 8, BLOCKS = kStretch / kBlock8;
   __shared__ int32_t list[kMaxTokens], found;
@@ -213,14 +213,14 @@ __global__ void __launch_bounds__(kThreads) layer8_product_kernel(const LayerArg
   const int row0 = (ROWS ? blockIdx.x * kWaves + wave : blockIdx.x) * 16;
   const uint8_t* codes = a.codes + expert * a.stride;
   const float* scales = a.scales + expert * a.stride_scales;
-  const int blocks = (a.width + kBlock8 - 1) / kBlock8;
+  const int all = (a.width + kBlock8 - 1) / kBlock8, first = UP ? 0 : (int)blockIdx.z * a.piece, blocks = UP ? all : min(all, first + a.piece);
   for (int c0 = 0; c0 < count; c0 += kMost) {
     const int cols = min(count - c0, kMost), col = lane & 15, choice = list[min(c0 + col, count - 1)];
     floatx4 acc[HALVES];
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) acc[h] = floatx4{0.f, 0.f, 0.f, 0.f};
     if constexpr (ROWS) {
-      for (int b0 = 0; b0 < blocks; b0 += BLOCKS) {
+      for (int b0 = first; b0 < blocks; b0 += BLOCKS) {
         Block<PARTS, HALVES> w[BLOCKS];
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) w[i].ask(a, codes, scales, min(row0, a.rows - 1) & ~15, min(b0 + i, blocks - 1));
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(kThreads) layer8_product_kernel(const LayerArg
       }
       if (row0 >= a.rows) continue;
     } else {
-      for (int b = wave; b < blocks; b += kWaves) {
+      for (int b = first + wave; b < blocks; b += kWaves) {
         const int at = b * kBlock8 + 16 * group;
         Block<PARTS, HALVES> w;
         w.ask(a, codes, scales, row0, b);
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kThreads) layer8_product_kernel(const LayerArg
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (row + e < a.rows) a.out[(int64_t)choice * a.rows + row + e] = acc[0][e];
+        if (row + e < a.rows) a.out[((int64_t)blockIdx.z * a.n + choice) * a.rows + row + e] = acc[0][e];
     }
   }
 }
@@ -312,7 +312,7 @@ struct SumArgs {
   const void* add;
   void* out;
   int64_t ld_add, ld_out;
-  int tokens, k, experts, d;
+  int tokens, k, experts, d, pieces;
 };
 template <typename T>
 __global__ void __launch_bounds__(kThreads) layer8_sum_kernel(const SumArgs a) {
@@ -324,17 +324,29 @@ __global__ void __launch_bounds__(kThreads) layer8_sum_kernel(const SumArgs a) {
     if ((uint32_t)e >= (uint32_t)a.experts) continue;
     int first = 0;  // (where a token chose an expert twice, the first choice has the row)
     while (a.ids[t * a.k + first] != e) ++first;
-    v = __builtin_fmaf(a.weights ? a.weights[t * a.k + j] : 1.f, a.y[(int64_t)(t * a.k + first) * a.d + c], v);
+    const float* y = a.y + (int64_t)(t * a.k + first) * a.d + c;
+    float sum = *y;
+    for (int p = 1; p < a.pieces; ++p) sum += y[(int64_t)p * a.tokens * a.k * a.d];
+    v = __builtin_fmaf(a.weights ? a.weights[t * a.k + j] : 1.f, sum, v);
   }
   static_cast<T*>(a.out)[t * a.ld_out + c] = (T)v;
 }
 
+// Work-groups of a product whose wavefronts have 16 rows each, if they are enough for that.
+bool whole_rows(int rows, int n, int experts) { return (int64_t)ceil_div(rows, 16) * std::min(n, experts) >= 256 * kWaves; }
+// Into how many pieces the second product's width is cut: a work-group waits for its weights stretch by stretch, so four to a compute unit are wanted.
+int pieces_of(int n, int experts, int d, int ff) {
+  if (!whole_rows(d, n, experts)) return 1;
+  const int64_t groups = (int64_t)ceil_div(ceil_div(d, 16), kWaves) * std::min(n, experts);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(4, ceil_div(ff, 2 * kStretch)), 1024 / groups));
+}
 template <typename Source, int HIDDEN, bool GATED>
-int launch_product(LayerArgs a, hipStream_t stream) {
+int launch_product(LayerArgs a, int pieces, hipStream_t stream) {
   const int tiles = ceil_div(a.rows, 16), experts = std::min(a.n, a.experts);
   a.by_expert = a.n > a.experts;
-  if ((int64_t)tiles * experts >= 256 * kWaves) hipLaunchKernelGGL((layer8_product_kernel<Source, HIDDEN, GATED, true>), dim3(ceil_div(tiles, kWaves), experts), dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((layer8_product_kernel<Source, HIDDEN, GATED, false>), dim3(tiles, experts), dim3(kThreads), 0, stream, a);
+  a.piece = ceil_div(ceil_div(a.width, kStretch), pieces) * (kStretch / kBlock8);
+  if (whole_rows(a.rows, a.n, a.experts)) hipLaunchKernelGGL((layer8_product_kernel<Source, HIDDEN, GATED, true>), dim3(ceil_div(tiles, kWaves), experts, pieces), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((layer8_product_kernel<Source, HIDDEN, GATED, false>), dim3(tiles, experts, pieces), dim3(kThreads), 0, stream, a);
   NMT_LAUNCH_CHECK();
   return NMT_OK;
 }
@@ -352,15 +364,16 @@ int launch_layer(const nmt_expert_layer8* p, hipStream_t stream) {
   a.scales = p->d_up_scales, a.ld_scales = p->ld_up_scales, a.stride_scales = p->stride_up_scales, a.rows = p->ff, a.width = p->d;
   const bool gate = p->act == NMT_ACT_SILU_GATE;
   int rc;
-  if (p->d % 8) rc = gate ? launch_product<Rows<T, PARTS, true>, HIDDEN, true>(a, stream) : launch_product<Rows<T, PARTS, true>, HIDDEN, false>(a, stream);
-  else rc = gate ? launch_product<Rows<T, PARTS, false>, HIDDEN, true>(a, stream) : launch_product<Rows<T, PARTS, false>, HIDDEN, false>(a, stream);
+  if (p->d % 8) rc = gate ? launch_product<Rows<T, PARTS, true>, HIDDEN, true>(a, 1, stream) : launch_product<Rows<T, PARTS, true>, HIDDEN, false>(a, 1, stream);
+  else rc = gate ? launch_product<Rows<T, PARTS, false>, HIDDEN, true>(a, 1, stream) : launch_product<Rows<T, PARTS, false>, HIDDEN, false>(a, 1, stream);
   if (rc != NMT_OK) return rc;
   a.x = hidden, a.ld_x = a.ld_hidden, a.codes = static_cast<const uint8_t*>(p->d_down), a.ld = p->ld_down, a.stride = p->stride_down;
   a.scales = p->d_down_scales, a.ld_scales = p->ld_down_scales, a.stride_scales = p->stride_down_scales, a.out = y, a.rows = p->d, a.width = p->ff;
-  if (const int rc2 = launch_product<Parts<HIDDEN>, 0, false>(a, stream); rc2 != NMT_OK) return rc2;
+  const int pieces = pieces_of(n, p->experts, p->d, p->ff);
+  if (const int rc2 = launch_product<Parts<HIDDEN>, 0, false>(a, pieces, stream); rc2 != NMT_OK) return rc2;
   SumArgs s = {};
   s.y = y, s.weights = p->d_weights, s.ids = p->d_expert, s.add = p->d_add, s.out = p->d_out, s.ld_add = p->ld_add, s.ld_out = p->ld_out;
-  s.tokens = p->tokens, s.k = p->k, s.experts = p->experts, s.d = p->d;
+  s.tokens = p->tokens, s.k = p->k, s.experts = p->experts, s.d = p->d, s.pieces = pieces;
   hipLaunchKernelGGL(layer8_sum_kernel<T>, dim3(ceil_div(p->d, kThreads), p->tokens), dim3(kThreads), 0, stream, s);
   NMT_LAUNCH_CHECK();
   return NMT_OK;
@@ -378,7 +391,7 @@ int check_layer(const char* who, int tokens, int k, int experts, int d, int ff) 
 
 extern "C" int64_t nmt_op_expert_layer8_scratch(int32_t tokens, int32_t k, int32_t experts, int32_t d, int32_t ff) {
   if (const int rc = check_layer("nmt_op_expert_layer8_scratch", tokens, k, experts, d, ff); rc != NMT_OK) return rc;
-  return hidden_floats(tokens * k, ff) + (int64_t)tokens * k * d;
+  return hidden_floats(tokens * k, ff) + (int64_t)tokens * k * d * (tokens ? pieces_of(tokens * k, experts, d, ff) : 1);
 }
 
 extern "C" int nmt_op_expert_layer8(const nmt_expert_layer8* p, void* stream_) {
