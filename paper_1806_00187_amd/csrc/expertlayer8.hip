@@ -11,10 +11,10 @@ namespace {
 
 constexpr int kMaxTokens = 64, kMaxChoices = 64, kMaxExperts = 1024, kMaxWidth = 1 << 20;
 constexpr int kThreads = 512, kWaves = 8;
-constexpr int kMost = 16;      // choices of a matrix instruction
+constexpr int kSets = 2;       // sets of 16 choices, a matrix instruction's, that are in work at a time
 // Codes go into the products 2^17 times smaller, and scales as much larger: so the sum of a block's 128 products, each of up to 448 times an input, is finite where the inputs are.
 constexpr float kDown = 0x1p17f;
-constexpr int kStretch = 512;  // of the width, in LDS at a time
+constexpr int kStretch = 256;  // of the width, in LDS at a time
 
 struct LayerArgs {
   const void* x;         // [tokens, d] rows of the layer's type, or hidden [parts, choices, width rounded up to 16] in bf16
@@ -139,7 +139,7 @@ struct Block {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int k = b * kBlock8 + 64 * half + 16 * group;
-        w[h][half] = __builtin_nontemporal_load(reinterpret_cast<const code4_t*>(row + (k < a.width ? k : 0)));  // (16 bytes with a code of the row in them)
+        w[h][half] = *reinterpret_cast<const code4_t*>(row + (k < a.width ? k : 0));  // (16 bytes with a code of the row in them)
       }
       // 16 rows from a multiple of 16 on share a scale, other 16 may have two
       const float* at = scales + b * a.ld_scales;
@@ -167,28 +167,36 @@ struct Block {
       }
     }
   }
-  // in(half, q): the inputs of eight codes from 64 half + 16 (L >> 4) + 8 q on.
-  template <typename F>
-  __device__ __forceinline__ void add(floatx4 (&acc)[HALVES], F in) const {
-    floatx4 t[HALVES];
+  // in(half, q, n): the inputs of eight codes from 64 half + 16 (L >> 4) + 8 q on, of the n-th 16 columns.
+  template <int N, typename F>
+  __device__ __forceinline__ void add(floatx4 (&acc)[N][HALVES], F in) const {
+    floatx4 t[N][HALVES];
 #pragma unroll
-    for (int h = 0; h < HALVES; ++h) t[h] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) t[n][h] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const Input<PARTS> x = in(half, q);
+        bf16x8_t m[HALVES];
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) {
-          const bf16x8_t m = widen8(w[h][half][2 * q], w[h][half][2 * q + 1], 1.f / kDown);
+        for (int h = 0; h < HALVES; ++h) m[h] = widen8(w[h][half][2 * q], w[h][half][2 * q + 1], 1.f / kDown);
 #pragma unroll
-          for (int p = PARTS - 1; p >= 0; --p) t[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(m, x.part[p], t[h], 0, 0, 0);
+        for (int n = 0; n < N; ++n) {
+          const Input<PARTS> x = in(half, q, n);
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) t[n][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(m[h], x.part[p], t[n][h], 0, 0, 0);
         }
       }
 #pragma unroll
-    for (int h = 0; h < HALVES; ++h)
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[h][e] = __builtin_fmaf(t[h][e], scale[h][e] * kDown, acc[h][e]);
+      for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[n][h][e] = __builtin_fmaf(t[n][h][e], scale[h][e] * kDown, acc[n][h][e]);
   }
 };
 
@@ -201,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, ROWS ? 4 : 2) layer8_product_kernel(
   constexpr bool UP = HIDDEN > 0;
   constexpr int PARTS = Source::kParts, HALVES = GATED ? 2 : 1, PITCH = kStretch + 8, BLOCKS = kStretch / kBlock8;
   __shared__ int32_t list[kMaxTokens], found;
-  __shared__ __attribute__((aligned(16))) __bf16 xs[ROWS ? PARTS : 1][ROWS ? kMost : 1][ROWS ? PITCH : 8];
+  __shared__ __attribute__((aligned(16))) __bf16 xs[ROWS ? PARTS : 1][ROWS ? 16 * kSets : 1][ROWS ? PITCH : 8];
   __shared__ float join[ROWS ? 1 : kWaves][HALVES][4][64];
   touch(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane >> 4;
@@ -214,75 +222,11 @@ __global__ void __launch_bounds__(kThreads, ROWS ? 4 : 2) layer8_product_kernel(
   const uint8_t* codes = a.codes + expert * a.stride;
   const float* scales = a.scales + expert * a.stride_scales;
   const int all = (a.width + kBlock8 - 1) / kBlock8, first = UP ? 0 : (int)blockIdx.z * a.piece, blocks = UP ? all : min(all, first + a.piece);
-  for (int c0 = 0; c0 < count; c0 += kMost) {
-    const int cols = min(count - c0, kMost), col = lane & 15, choice = list[min(c0 + col, count - 1)];
-    floatx4 acc[HALVES];
-#pragma unroll
-    for (int h = 0; h < HALVES; ++h) acc[h] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if constexpr (ROWS) {
-      for (int b0 = first; b0 < blocks; b0 += BLOCKS) {
-        Block<PARTS, HALVES> w[BLOCKS];
-#pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) w[i].ask(a, codes, scales, min(row0, a.rows - 1) & ~15, min(b0 + i, blocks - 1));
-        __syncthreads();  // (the last stretch is done with)
-        for (int i = threadIdx.x; i < cols * (kStretch / 8); i += kThreads) {
-          const int c = i / (kStretch / 8), k = i % (kStretch / 8) * 8, at = b0 * kBlock8 + k;
-          Source x;
-          x.set(a, list[c0 + c], UP);
-          x.ask(a, at);
-          const Input<PARTS> in = x.get(a, at);
-#pragma unroll
-          for (int p = 0; p < PARTS; ++p) *reinterpret_cast<bf16x8_t*>(&xs[p][c][k]) = in.part[p];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) {
-          if (b0 + i >= blocks) break;
-          w[i].cut(a, b0 + i);
-          w[i].add(acc, [&](int half, int q) {
-            Input<PARTS> in;  // (columns without a choice hold whatever was there: nothing of theirs is written)
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p) in.part[p] = *reinterpret_cast<const bf16x8_t*>(&xs[p][col][i * kBlock8 + 64 * half + 16 * group + 8 * q]);
-            return in;
-          });
-        }
-      }
-      if (row0 >= a.rows) continue;
-    } else {
-      for (int b = first + wave; b < blocks; b += kWaves) {
-        const int at = b * kBlock8 + 16 * group;
-        Block<PARTS, HALVES> w;
-        w.ask(a, codes, scales, row0, b);
-        Source x[2][2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            x[half][q].set(a, choice, UP);
-            x[half][q].ask(a, at + 64 * half + 8 * q);
-          }
-        w.cut(a, b);
-        w.add(acc, [&](int half, int q) { return x[half][q].get(a, at + 64 * half + 8 * q); });
-      }
-      __syncthreads();  // (the last choices' sums are read)
-#pragma unroll
-      for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) join[wave][h][e][lane] = acc[h][e];
-      __syncthreads();
-      if (wave > 0) continue;
-#pragma unroll
-      for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v = join[0][h][e][lane];
-#pragma unroll
-          for (int w = 1; w < kWaves; ++w) v += join[ROWS ? 0 : w][h][e][lane];
-          acc[h][e] = v;
-        }
-    }
-    if (col >= cols) continue;
-    const int row = row0 + 4 * group;
+  // What comes of 16 columns, from the c0-th choice on.
+  auto finish = [&](const floatx4 (&acc)[HALVES], int c0) {
+    const int col = c0 + (lane & 15), row = row0 + 4 * group;
+    if (col >= count) return;
+    const int choice = list[col];
     if constexpr (UP) {
       float v[4];
       __bf16 part[HIDDEN][4];
@@ -302,6 +246,87 @@ __global__ void __launch_bounds__(kThreads, ROWS ? 4 : 2) layer8_product_kernel(
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (row + e < a.rows) a.out[((int64_t)blockIdx.z * a.n + choice) * a.rows + row + e] = acc[0][e];
+    }
+  };
+  if constexpr (ROWS) {
+    for (int c0 = 0; c0 < count; c0 += 16 * kSets) {
+      const int cols = min(count - c0, 16 * kSets);
+      floatx4 acc[kSets][HALVES], (&acc_one)[1][HALVES] = reinterpret_cast<floatx4(&)[1][HALVES]>(acc);
+#pragma unroll
+      for (int n = 0; n < kSets; ++n)
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) acc[n][h] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int b0 = first; b0 < blocks; b0 += BLOCKS) {
+        Block<PARTS, HALVES> w[BLOCKS];
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) w[i].ask(a, codes, scales, min(row0, a.rows - 1) & ~15, min(b0 + i, blocks - 1));
+        __syncthreads();  // (the last stretch is done with)
+        for (int i = threadIdx.x; i < cols * (kStretch / 8); i += kThreads) {
+          const int c = i / (kStretch / 8), k = i % (kStretch / 8) * 8, at = b0 * kBlock8 + k;
+          Source x;
+          x.set(a, list[c0 + c], UP);
+          x.ask(a, at);
+          const Input<PARTS> in = x.get(a, at);
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) *reinterpret_cast<bf16x8_t*>(&xs[p][c][k]) = in.part[p];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+          if (b0 + i >= blocks) break;
+          auto from = [&](int half, int q, int n) {
+            Input<PARTS> in;  // (columns without a choice hold whatever was there: nothing of theirs is written)
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) in.part[p] = *reinterpret_cast<const bf16x8_t*>(&xs[p][16 * n + (lane & 15)][i * kBlock8 + 64 * half + 16 * group + 8 * q]);
+            return in;
+          };
+          w[i].cut(a, b0 + i);
+          if (cols > 16) w[i].add(acc, from);
+          else w[i].add(acc_one, from);
+        }
+      }
+      if (row0 < a.rows)
+#pragma unroll
+        for (int n = 0; n < kSets; ++n) finish(acc[n], c0 + 16 * n);
+    }
+  } else {
+    for (int c0 = 0; c0 < count; c0 += 16) {
+      const int choice = list[min(c0 + (lane & 15), count - 1)];
+      floatx4 acc[1][HALVES];
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) acc[0][h] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int b = first + wave; b < blocks; b += kWaves) {
+        const int at = b * kBlock8 + 16 * group;
+        Block<PARTS, HALVES> w;
+        w.ask(a, codes, scales, row0, b);
+        Source x[2][2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            x[half][q].set(a, choice, UP);
+            x[half][q].ask(a, at + 64 * half + 8 * q);
+          }
+        w.cut(a, b);
+        w.add(acc, [&](int half, int q, int) { return x[half][q].get(a, at + 64 * half + 8 * q); });
+      }
+      __syncthreads();  // (the last choices' sums are read)
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) join[wave][h][e][lane] = acc[0][h][e];
+      __syncthreads();
+      if (wave > 0) continue;
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float v = join[0][h][e][lane];
+#pragma unroll
+          for (int w = 1; w < kWaves; ++w) v += join[ROWS ? 0 : w][h][e][lane];
+          acc[0][h][e] = v;
+        }
+      finish(acc[0], c0);
     }
   }
 }
