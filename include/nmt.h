@@ -491,7 +491,7 @@ int nmt_adamw_step(const nmt_adamw* plan, double lr, double beta1, double beta2,
  * Matrices held in 8 bits.  A matrix [rows, d] is codes in OCP e4m3 (4 exponent and 3 mantissa bits, no infinity), one byte each, rows `ld` bytes apart, and
  * fp32 scales: value = code * scale.  128 elements of a row share a scale (the last block of a row may be shorter), scale (row r, block b) at b * ld_scales + r:
  * the scales of one block of columns lie side by side.  Or, `square`, 128 x 128 elements share one: that of rows 128 q ... and block b at b * ld_scales + q.
- * Bytes behind a row's last code are neither written nor looked at.
+ * Bytes behind a row's last code are neither written nor used.  Scratch belongs to one call at a time: calls that may overlap, captured ones among them, take one each.
  * ------------------------------------------------------------------------------------------ */
 
 /* x (fp16, bf16 or fp32, any distance between rows, any address) into 8 bits.  scale = the block's largest magnitude / 448, code = x / scale, nearest, ties to
@@ -541,6 +541,8 @@ typedef struct nmt_gemm8 {
 } nmt_gemm8;
 int64_t nmt_op_gemm8_scratch(int32_t M, int32_t N, int32_t K, int32_t batch, int32_t ranges);
 int nmt_op_gemm8(const nmt_gemm8* a /*host*/, void* stream);
+/* Host only.  Debug export: the edge of the tiles that such a call is cut into and its pieces along k, for tests that are to reach every form. */
+int nmt_debug_gemm8_form(int32_t M, int32_t N, int32_t K, int32_t batch, int32_t ranges, int32_t type, int32_t b_square, int32_t* tile, int32_t* splits);
 
 /* A sparse layer as a whole over few tokens (at most 64; more: nmt_op_expert_dispatch, nmt_op_gemm8, nmt_op_expert_combine), as when one token of each sentence is at hand:
  *   hidden[t, j] = act(up[expert[t, j]] x[t]),  out[t] = add[t] + sum over j of weights[t, j] * down[expert[t, j]] hidden[t, j].

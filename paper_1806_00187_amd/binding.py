@@ -150,6 +150,7 @@ _SIGNATURES = {
     "nmt_op_norm8": (C.c_int, [_P, _P]),
     "nmt_op_gemm8_scratch": (_I64, [_I32, _I32, _I32, _I32, _I32]),
     "nmt_op_gemm8": (C.c_int, [_P, _P]),
+    "nmt_debug_gemm8_form": (C.c_int, [_I32, _I32, _I32, _I32, _I32, _I32, _I32, C.POINTER(_I32), C.POINTER(_I32)]),
     "nmt_op_expert_layer8_scratch": (_I64, [_I32, _I32, _I32, _I32, _I32]),
     "nmt_op_expert_layer8": (C.c_int, [_P, _P]),
     "nmt_adamw_step": (C.c_int, [_P, C.c_double, C.c_double, C.c_double, C.c_double, _I32, _F, _P, _P]),
@@ -884,6 +885,13 @@ def nmt_op_gemm8_scratch(M, N, K, batch=1, ranges=False):
     if n < 0:
         _check(int(n))
     return n
+
+
+def nmt_debug_gemm8_form(M, N, K, dtype, batch=1, ranges=False, b_square=True):
+    """(edge of the tiles, pieces along k) of such a call of nmt_op_gemm8."""
+    lib, tile, splits = _lib or load(), C.c_int32(), C.c_int32()
+    _check(lib.nmt_debug_gemm8_form(M, N, K, batch, 1 if ranges else 0, _type_code(dtype, "nmt_debug_gemm8_form"), 1 if b_square else 0, C.byref(tile), C.byref(splits)))
+    return tile.value, splits.value
 
 
 def nmt_op_gemm8(a, a_scales, b, b_scales, c, bias=None, add=None, ranges=None, scratch=None, stream=None):

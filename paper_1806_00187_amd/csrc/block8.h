@@ -70,8 +70,11 @@ struct Eight {
       for (int e = 0; e < 8; ++e) v[e] = e < d ? row[e] : T(0);
     }
   }
-  __device__ __forceinline__ void get(float (&x)[8], int c, int d) const {
-    if (RAGGED) {
+  // What was loaded, where it belongs.
+  __device__ __forceinline__ vec settled(int c, int d) const {
+    if constexpr (!RAGGED) {
+      return v;
+    } else {
       struct Words {
         uint32_t w[WORDS];
       };
@@ -91,13 +94,13 @@ struct Eight {
 #pragma unroll
         for (int i = 0; i < WORDS; ++i) t.w[i] = __builtin_amdgcn_alignbit(i + 1 < WORDS ? t.w[(i + 1) % WORDS] : 0u, t.w[i], by);
       }
-      const vec moved = __builtin_bit_cast(vec, t);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (float)moved[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+      return __builtin_bit_cast(vec, t);
     }
+  }
+  __device__ __forceinline__ void get(float (&x)[8], int c, int d) const {
+    const vec t = settled(c, d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)t[e];
   }
   // Of the n (0 to 8) that are there.
   static __device__ __forceinline__ void store(T* to, const vec& t, int n) {

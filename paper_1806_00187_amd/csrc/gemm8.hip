@@ -48,13 +48,13 @@ __device__ __forceinline__ Gemm8Args arguments() {
 #endif
 }
 // One wave instruction: lane L's SIZE bytes, `at` bytes from base on, land at lds + SIZE L; zeros where `at` is kOob.  Written as an instruction because the compiler holds every read of LDS up
-// until all such requests have arrived; whoever reads what this brings waits for it (arrived()).
+// until all such requests have arrived; whoever reads what this brings waits for it (arrived()).  The waits are those that the compiler would put behind a vector instruction that has written one of the scalars.
 template <int SIZE>
 __device__ __forceinline__ void request_to_lds(uint64_t base, uint32_t lds, uint32_t at) {
   typedef uint32_t rsrc_t __attribute__((ext_vector_type(4)));
   const rsrc_t s = {(uint32_t)base, (uint32_t)(base >> 32), kOob, 0x00020000u};  // (no address has more than 48 bits)
-  if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(s), "s"(lds) : "memory");
-  else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(at), "s"(s), "s"(lds) : "memory");
+  if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(s), "s"(lds) : "memory");
+  else asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(at), "s"(s), "s"(lds) : "memory");
 }
 __device__ __forceinline__ uint64_t scalar(const void* p) {
   auto one = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
@@ -765,6 +765,15 @@ extern "C" int64_t nmt_op_gemm8_scratch(int32_t M, int32_t N, int32_t K, int32_t
   int splits = 0;
   for (int kind = 0; kind < 3; ++kind) splits = std::max(splits, plan(M, N, K, batch, ranges != 0, kind == 0, kind == 1).splits);
   return splits > 1 ? (int64_t)splits * batch * M * N : 0;
+}
+
+extern "C" int nmt_debug_gemm8_form(int32_t M, int32_t N, int32_t K, int32_t batch, int32_t ranges, int32_t type, int32_t b_square, int32_t* tile, int32_t* splits) {
+  const char* who = "nmt_debug_gemm8_form";
+  if (const int rc = check_sizes(who, M, N, K, batch); rc != NMT_OK) return rc;
+  NMT_REQUIRE(row_type_ok(type) && tile && splits, "%s: bad argument", who);
+  const Plan p = plan(M, N, K, batch, ranges != 0, type == NMT_F32, b_square != 0);
+  *tile = p.tile, *splits = p.splits;
+  return NMT_OK;
 }
 
 extern "C" int nmt_op_gemm8(const nmt_gemm8* p, void* stream_) {

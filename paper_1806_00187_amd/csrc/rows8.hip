@@ -31,23 +31,37 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
   const int64_t r = r0 + 8 * group, c = c0 + 8 * lane16;
   const int rows = (int)min((int64_t)a.rows - r, (int64_t)8), cols = (int)max(min((int64_t)a.d - c, (int64_t)8), (int64_t)0);  // of this thread's (rows may be negative)
   const T* x = static_cast<const T*>(a.x);
-  float v[8][8];
-  {
-    Eight<T, !COLS> t[8];
+  // (kept as they came, and made numbers where they are used: 64 registers less for rows of 16 bits)
+  Eight<T, !COLS> t[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t[i].load(x + min(r + i, (int64_t)a.rows - 1) * a.ld_x, (int)c, a.d);
+  for (int i = 0; i < 8; ++i) t[i].load(x + min(r + i, (int64_t)a.rows - 1) * a.ld_x, (int)c, a.d);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      t[i].get(v[i], (int)c, a.d);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = i < rows ? v[i][e] : 0.f;
-    }
+  for (int i = 0; i < 8; ++i) {
+    t[i].v = t[i].settled((int)c, a.d);
+    if (i >= rows) t[i].v = typename Eight<T, !COLS>::vec{};
   }
+  auto row_of = [&](int i, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)t[i].v[e];
+  };
+  auto column_of = [&](int e, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)t[i].v[e];
+  };
+  auto apart = [&] {  // (what was made of them is not kept)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(t[i].v));
+  };
   Scale8 whole = {0.f, 0.f};
   if (a.square) {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, magnitude8(v[i]));
+    for (int i = 0; i < 8; ++i) {
+      float v[8];
+      row_of(i, v);
+      top = max(top, magnitude8(v));
+    }
+    apart();
     top = lanes16_max(top);
     if (lane16 == 0) tops[0][group] = top;
     __syncthreads();
@@ -64,38 +78,44 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       Scale8 s = whole;
+      float v[8];
+      row_of(i, v);
       if (!a.square) {
-        s = scale8(lanes16_max(magnitude8(v[i])));
+        s = scale8(lanes16_max(magnitude8(v)));
         if (lane16 == 0 && i < rows) a.scales[(c0 >> 7) * a.ld_scales + r + i] = s.scale;
       }
       if (i < rows)
-        store8<!COLS>(a.codes + (r + i) * a.ld_codes + c, codes8(v[i][0], v[i][1], v[i][2], v[i][3], s.back), codes8(v[i][4], v[i][5], v[i][6], v[i][7], s.back), cols);
+        store8<!COLS>(a.codes + (r + i) * a.ld_codes + c, codes8(v[0], v[1], v[2], v[3], s.back), codes8(v[4], v[5], v[6], v[7], s.back), cols);
     }
+    apart();
   }
   if (a.codes_t) {
     if (!a.square) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, magnitude8(v[i][e]));
+        float v[8];
+        column_of(e, v);
+        uint32_t top = magnitude8(v);
         const auto rows16 = __builtin_amdgcn_permlane16_swap(top, top, false, false);
         top = max(rows16[0], rows16[1]);
         const auto halves = __builtin_amdgcn_permlane32_swap(top, top, false, false);
         top = max(halves[0], halves[1]);
         if ((threadIdx.x & 63) < 16) tops[wave][8 * lane16 + e] = top;
       }
+      apart();
       __syncthreads();
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       Scale8 s = whole;
+      float v[8];
+      column_of(e, v);
       if (!a.square) {
         const int at = 8 * lane16 + e;
         s = scale8(max(max(tops[0][at], tops[1][at]), max(tops[2][at], tops[3][at])));
         if (group == 0 && e < cols) a.scales_t[(r0 >> 7) * a.ld_scales_t + c + e] = s.scale;
       }
-      const uint32_t lo = codes8(v[0][e], v[1][e], v[2][e], v[3][e], s.back), hi = codes8(v[4][e], v[5][e], v[6][e], v[7][e], s.back);
+      const uint32_t lo = codes8(v[0], v[1], v[2], v[3], s.back), hi = codes8(v[4], v[5], v[6], v[7], s.back);
       turn[8 * lane16 + e][group ^ lane16] = (uint64_t)hi << 32 | lo;
     }
     __syncthreads();

@@ -72,6 +72,17 @@ def test_gemm_wants_the_scratch_it_asks_for():
             A.nmt_op_gemm8_scratch(*bad)
 
 
+def test_gemm_forms_are_named_and_bad_ones_refused():
+    assert A.nmt_debug_gemm8_form(1, 1, 1, torch.float16) == (64, 1)
+    assert A.nmt_debug_gemm8_form(1 << 20, 1 << 12, 1 << 10, torch.float16) == (256, 1)
+    assert A.nmt_debug_gemm8_form(1 << 20, 1 << 12, 1 << 10, torch.float16, b_square=False)[0] == 128
+    for bad in ((-1, 8, 8), (8, 8, 8, torch.float16, 1025)):
+        with pytest.raises(A.NmtError):
+            A.nmt_debug_gemm8_form(*bad[:3], *(bad[3:] or [torch.float16]))
+    with pytest.raises(A.NmtError):
+        A.nmt_debug_gemm8_form(8, 8, 8, torch.float64)
+
+
 def layer(**kw):
     base = dict(tokens=4, k=2, experts=8, d=200, ff=300, type=A.NMT_F16, act=A.NMT_ACT_SILU_GATE, ld_x=200, ld_add=200, ld_out=200, ld_up=208, stride_up=208 * 600,
                 ld_up_scales=5, stride_up_scales=10, ld_down=304, stride_down=304 * 200, ld_down_scales=2, stride_down_scales=6, d_x=P, d_expert=P, d_weights=P,

@@ -293,6 +293,49 @@ def test_gemm_of_many_tiles_or_long_rows(M, N, K):
     check_gemm(M, N, K, F32, (False, False), add=True)
 
 
+# one tile after the other, tiles with an addend, tiles of contractions that are cut up, in every size of tile
+FORMS = [(4400, 4355, 129, F16, (False, True), False, (256, 1)), (4400, 4400, 300, BF16, (False, True), False, (256, 1)), (4400, 4355, 512, F16, (True, True), True, (256, 1)),
+         (4099, 4400, 128, BF16, (False, True), False, (256, 1)), (1024, 4096, 26001, BF16, (False, True), True, (256, 4)), (2100, 2111, 1000, F16, (False, True), True, (128, 1)),
+         (2100, 2111, 640, BF16, (False, False), False, (128, 1)), (1000, 1000, 13001, F16, (False, False), True, (128, 4)), (2100, 2111, 300, F32, (True, False), True, (128, 1)),
+         (1024, 4096, 26001, F32, (False, False), True, (128, 2)), (700, 777, 500, BF16, (False, True), False, (64, 1)), (700, 130, 30001, F32, (False, True), True, (64, 12))]
+
+
+@pytest.mark.parametrize("M,N,K,dtype,squares,add,form", FORMS, ids=lambda v: str(v).replace("torch.", ""))
+def test_gemm_in_every_form(M, N, K, dtype, squares, add, form):
+    assert A.nmt_debug_gemm8_form(M, N, K, dtype, b_square=squares[1]) == form
+    check_gemm(M, N, K, dtype, squares, bias=True, add=add, pad=16, ld=3, off=1, in_place=add)
+
+
+def test_gemm_of_a_batch_and_of_experts_in_large_tiles():
+    M, N, K, batch = 2100, 2000, 300, 4
+    assert A.nmt_debug_gemm8_form(M, N, K, F16, batch) == (256, 1)
+    g = [eight(M, K, False, 40 + e) for e in range(batch)], [eight(N, K, True, 50 + e) for e in range(batch)]
+    ld = ceil(K, 16) * 16
+    def stack(parts, rows):
+        raw = torch.full((batch, rows, ld), 0x7F, dtype=torch.uint8, device=DEV)
+        for e, (codes, _) in enumerate(parts):
+            raw[e, :, :K] = codes.view(torch.uint8)
+        return raw.view(E4M3)[:, :, :K], torch.stack([s for _, s in parts])
+    (a, sa), (b, sb) = stack(g[0], M), stack(g[1], N)
+    bias = torch.randn(batch, N, generator=gen(3), device=DEV).to(F16)
+    c = torch.empty(batch, M, N, dtype=F16, device=DEV)
+    A.nmt_op_gemm8(a, sa, b, sb, c, bias=bias, scratch=scratch_for(M, N, K, batch))
+    for e in range(batch):
+        check_product(c[e], a[e], sa[e], b[e], sb[e], F16, bias[e], None, e)
+    counts = [3000, 0, 2501, 4000]
+    rows = sum(counts)
+    assert A.nmt_debug_gemm8_form(rows, N, K, F16, batch, True)[0] == 256
+    a, sa = eight(rows, K, False, 60)
+    n = torch.tensor(counts, device=DEV)
+    ranges = torch.stack([n.cumsum(0) - n, n], 1).int()
+    c, uc = guarded(rows, N, F16, torch.full((rows, N), 3.0), N + 1, 1)
+    A.nmt_op_gemm8(a, sa, b, sb, c, bias=bias, ranges=ranges)
+    assert uc()
+    for e, (first, count) in enumerate(ranges.tolist()):
+        if count:
+            check_product(c[first:first + count], a[first:first + count], sa[:, first:first + count], b[e], sb[e], F16, bias[e], None, e)
+
+
 def test_gemm_of_nothing():
     a, sa = torch.empty(40, 0, dtype=torch.uint8, device=DEV).view(E4M3), torch.empty(0, 40, device=DEV)
     bias, add = torch.randn(40, generator=gen(1), device=DEV), torch.randn(40, 40, generator=gen(2), device=DEV)
@@ -522,6 +565,57 @@ def test_graphs_streams_and_the_same_bits_again():
     torch.cuda.synchronize()
     for name, p, q in zip(names, bits(eager), bits(other)):
         assert torch.equal(p, q), name
+
+
+def test_matrices_beyond_32_bits():
+    """More than 2^32 elements and bytes: what lies behind them is read and written where it belongs."""
+    rows, d, last = 70001, 65552, 300
+    x = torch.zeros(rows, d, dtype=F16, device=DEV)
+    x[-last:] = torch.randn(last, d, generator=gen(61), device=DEV)
+    x[:2] = 1
+    new = lambda n, m: torch.empty(n, ceil(m, 16) * 16, dtype=torch.uint8, device=DEV).view(E4M3)[:, :m]  # noqa: E731
+    codes, scales, codes_t, scales_t = new(rows, d), torch.empty(ceil(d), rows, device=DEV), new(d, rows), torch.empty(ceil(rows), d, device=DEV)
+    A.nmt_op_quantize8(x, codes, scales, codes_t, scales_t)
+    check_codes(x[-last:], codes[-last:], scales[:, -last:], False, "codes")
+    whole = rows // 128 * 128 - 128      # (the last blocks of rows that are whole, and what is left)
+    check_codes(x[whole:, -last:].t(), codes_t[-last:, whole:], scales_t[whole // 128:, -last:], False, "codes_t")
+    assert (codes[:2].float() == 448).all() and not codes[2:rows - last:997].view(torch.uint8).any()
+    del x, codes_t, scales_t
+    b, sb = eight(40, d, True, 62)
+    c = torch.empty(rows, 40, device=DEV)
+    A.nmt_op_gemm8(codes, scales, b, sb, c, scratch=scratch_for(rows, 40, d))
+    check_product(c[-last:], codes[-last:], scales[:, -last:], b, sb, F32)
+    del codes, scales
+    n = 65600
+    a, sa = eight(rows, 96, False, 63)
+    b, sb = eight(n, 96, True, 64)
+    c = torch.empty(rows, n, dtype=F16, device=DEV)
+    A.nmt_op_gemm8(a, sa, b, sb, c, scratch=scratch_for(rows, n, 96))
+    first = n // 128 * 128 - 384
+    for r in (slice(0, 200), slice(rows - 200, rows)):
+        check_product(c[r, first:], a[r], sa[:, r], b[first:], sb[:, first // 128:], F16)
+        check_product(c[r, :256], a[r], sa[:, r], b[:256], sb[:, :2], F16)
+    del c
+    rows, d = 270001, 16384
+    x = torch.zeros(rows, d, dtype=BF16, device=DEV)
+    x[-5:] = torch.randn(5, d, generator=gen(65), device=DEV)
+    codes, scales = new(rows, d), torch.empty(ceil(d), rows, device=DEV)
+    A.nmt_op_norm8(x, None, None, codes, scales, torch.ones(d, dtype=BF16, device=DEV))
+    want = R.norm(x[-5:].to(D), "rms", 1e-5)[0]
+    got, step = decode(codes[-5:], scales[:, -5:]), spread(scales[:, -5:], 5, d, False)
+    q = want.abs() / step
+    within(got, want, (R.e4m3_half_step(q * (1 + 100 * U32)) + 200 * U32 * q) * step, "norm")
+    del x, codes, scales
+    # experts whose weights lie more than 2^32 bytes apart
+    apart = (1 << 32) + 4096
+    _, _, _, (up, su), (down, sd) = layer_inputs(3, 1, 2, 64, 48, F16, "relu", 66)
+    far = torch.empty(apart + up[0].numel(), dtype=torch.uint8, device=DEV).as_strided((2, 48, 64), (apart, 64, 1)).view(E4M3)
+    far.view(torch.uint8).copy_(up.view(torch.uint8))
+    x, ids = torch.randn(3, 64, generator=gen(67), device=DEV).to(F16), torch.tensor([[0], [1], [1]], dtype=torch.int32, device=DEV)
+    near, out, scratch = torch.empty_like(x), torch.empty_like(x), torch.empty(A.nmt_op_expert_layer8_scratch(3, 1, 2, 64, 48), device=DEV)
+    A.nmt_op_expert_layer8(x, ids, None, up, su, down, sd, near, scratch)
+    A.nmt_op_expert_layer8(x, ids, None, far, su, down, sd, out, scratch)
+    assert torch.equal(near, out) and near.any()
 
 
 def test_a_block_in_8_bits_goes_forwards_and_backwards():
