@@ -469,15 +469,17 @@ NMT_NORM_LAYER, NMT_NORM_RMS, NMT_ONE_GATE = 0, 1, 2 ** 31 - 1
 _MOST = 2 ** 31 - 1
 _KINDS = {"layer": NMT_NORM_LAYER, "rms": NMT_NORM_RMS}
 _TYPES = {}          # torch dtypes -> type codes; filled with _FLOAT and _INT when torch is there (load())
-_FLOAT = _INT = _E4M3 = _torch = _raw_stream = None
+_FLOAT = _INT = _E4M3 = _torch = _raw_stream = _current_device = None
 
 
 def _torch_types():
-    global _FLOAT, _INT, _E4M3, _torch, _raw_stream
+    global _FLOAT, _INT, _E4M3, _torch, _raw_stream, _current_device
     import torch
     _torch = torch
     # (what torch.cuda.current_stream looks up, without the Stream object around it: 0.1 us instead of 1)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+    # (what torch.cuda.current_device asks, without looking whether the GPU is in use yet: there are tensors on it)
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _TYPES.update({torch.float16: NMT_F16, torch.bfloat16: NMT_BF16, torch.float32: NMT_F32})
     _FLOAT, _INT, _E4M3 = torch.float32, torch.int32, torch.float8_e4m3fn
 
@@ -529,7 +531,7 @@ def _call(fn, device, stream, *args, out=None):
     if stream is None:
         stream = _raw_stream(device)
     last = (stream,) if out is None else (stream, C.byref(out))
-    if device == _torch.cuda.current_device():
+    if device == _current_device():
         rc = fn(*args, *last)
     else:
         with _torch.cuda.device(device):
@@ -858,6 +860,8 @@ def nmt_op_norm8(x, y, h, codes, scales, gain, shift=None, n=None, stats=None, k
 def _stack(t, batch, rows, d, dtype, device, what):
     """(address, distance between rows, distance between matrices) of a [rows, d] tensor, or of a [batch, rows, d] one."""
     strides, shape = t.stride(), t.shape
+    if batch == 1 and shape == (rows, d) and strides[1] == 1 and strides[0] >= d and rows > 1 and t.dtype is dtype and t.get_device() == device:
+        return t.data_ptr(), strides[0], 0
     if t.dtype is dtype and t.get_device() == device and ((shape == (rows, d) and batch == 1) or shape == (batch, rows, d)):
         ld, step = strides[-2:]
         if rows <= 1:
@@ -871,7 +875,8 @@ def _stack(t, batch, rows, d, dtype, device, what):
 
 def _scale_lines(scales, rows, what):
     """Whether these are the scales of 128 x 128 elements each, and how many lie side by side."""
-    lines = scales.shape[-1] if scales.dim() in (2, 3) else -1
+    shape = scales.shape
+    lines = shape[-1] if len(shape) in (2, 3) else -1
     if lines == rows:
         return 0, rows
     if lines != -(-rows // 128):
@@ -898,15 +903,18 @@ def nmt_op_gemm8(a, a_scales, b, b_scales, c, bias=None, add=None, ranges=None, 
     """c = a b^T + bias + add: a [M, K] and b [N, K] in 8 bits, c and add [M, N], bias [N]; or a, b, c, add and their scales with a dimension of products in front (bias then [batch, N]).
     ranges [experts, 2]: a, c and add are [M, .], expert e's rows those of its range, b [experts, N, K] and bias [experts, N]."""
     lib, who = _lib or load(), "nmt_op_gemm8"
-    if c is None or c.dim() not in (2, 3) or a is None or a.dim() not in (2, 3) or b is None or b.dim() not in (2, 3):
+    if c is None or a is None or b is None:
+        _refuse(f"{who}: a, b and c are tensors of two or three dimensions")
+    c_shape, a_shape = c.shape, a.shape
+    if len(c_shape) not in (2, 3) or len(a_shape) not in (2, 3):
         _refuse(f"{who}: a, b and c are tensors of two or three dimensions")
     device, dtype = c.get_device(), c.dtype
-    *many, M, N = c.shape
-    K = a.shape[-1]
+    *many, M, N = c_shape
+    K = a_shape[-1]
     batch = own = many[0] if many else 1        # (own: products that have an a and a c of their own)
     ranges_ = add_ = bias_ = scratch_ = ld_add = stride_add = stride_bias = held = 0
     if ranges is not None:
-        if many or a.dim() == 3:
+        if many or len(a_shape) == 3:
             _refuse(f"{who}: experts' rows lie in one matrix")
         batch = b.shape[0] if b.dim() == 3 else 1
         ranges_ = _vector(ranges, 2 * batch, _INT, device, "ranges")
