@@ -1,8 +1,10 @@
 // A sparse layer over few tokens, its experts' weights held in 8 bits with a scale for each 128 x 128:
 //   hidden[t, j] = act(up[e(t, j)] x[t]),  out[t] = add[t] + sum over j of weights[t, j] down[e(t, j)] hidden[t, j].
-// Bound by the weights of the experts that have a token, which are read once.  Two products of the same form and a sum: a work-group takes an expert's choices and 16 rows (or four
+// Bound by the weights of the experts that have a token, which are read once.  Two products of the same form and a sum: a work-group takes an expert's choices and 16 rows (or eight
 // times 16) of its weight; the matrix instruction's other operand are up to 16 choices' inputs.  Codes are exact in bf16; inputs are split into as
-// many bf16 parts as hold them: bf16 one, fp16 two, fp32 three; so the products are those of the inputs as they are.
+// many bf16 parts as hold them: bf16 one, fp16 two, fp32 three; so the products are those of the inputs as they are.  Hidden is kept in two parts (three for fp32): off by 2^-18 (2^-27) of itself.
+// Measured: 33 tokens, 4 of 64 experts, 1024 x 4096 silu gate, bf16 149 to 158 us, 4.8 TB/s of weights; 64 tokens, 2 of 128, 640 x 1280 42 us, 3.2 TB/s; one token, 2 of 8, 512 x 2048 10.8 us in a graph, which is three launches
+// that wait for each other (4.5, 5 and 2): each a chain of choices, addresses, weights and sums.  The sum in the second product's last work-group instead of a launch: 13 us in a graph, and 198 for the 33 tokens.
 #include "block8.h"
 
 #include <algorithm>
@@ -11,10 +13,10 @@ namespace {
 
 constexpr int kMaxTokens = 64, kMaxChoices = 64, kMaxExperts = 1024, kMaxWidth = 1 << 20;
 constexpr int kThreads = 512, kWaves = 8;
-constexpr int kSets = 2;       // sets of 16 choices, a matrix instruction's, that are in work at a time
+constexpr int kSets = 2;       // sets of 16 choices, a matrix instruction's, that are in work at a time (one: 33 tokens 170 us instead of 157)
 // Codes go into the products 2^17 times smaller, and scales as much larger: so the sum of a block's 128 products, each of up to 448 times an input, is finite where the inputs are.
 constexpr float kDown = 0x1p17f;
-constexpr int kStretch = 256;  // of the width, in LDS at a time
+constexpr int kStretch = 256;  // of the width, in LDS at a time (512, which leaves room for half as many work-groups: 33 tokens 208 us instead of 158)
 
 struct LayerArgs {
   const void* x;         // [tokens, d] rows of the layer's type, or hidden [parts, choices, width rounded up to 16] in bf16
@@ -357,11 +359,15 @@ __global__ void __launch_bounds__(kThreads) layer8_sum_kernel(const SumArgs a) {
   static_cast<T*>(a.out)[t * a.ld_out + c] = (T)v;
 }
 
-// Work-groups of a product whose wavefronts have 16 rows each, if they are enough for that.
-bool whole_rows(int rows, int n, int experts) { return (int64_t)ceil_div(rows, 16) * std::min(n, experts) >= 256 * kWaves; }
-// Into how many pieces the second product's width is cut: a work-group waits for its weights stretch by stretch, so four to a compute unit are wanted.
+// Whether a product's wavefronts have 16 rows each (ROWS).  They read a weight once for 32 choices, without them it is once for 16; but they must be enough: eight to a compute unit for the first product, four for
+// the second, whose width can be cut.  With and without, microseconds of the layer: 33 tokens, 4 of 64 experts, 1024 x 4096 157, 236; 64 tokens, 8 of 16, 512 x 2048 (32 choices of an expert) 60, 70;
+// 8 tokens, 2 of 64, 1024 x 4096 (1024 wavefronts for the second product) 32, 36; but one token, 4 of 16, 2048 x 4096 36, 28; 2 of 8, 512 x 2048 15, 11.
+bool whole_rows(int rows, int n, int experts, bool up) {
+  return (int64_t)ceil_div(rows, 16) * std::max(std::min(n, experts), n / 16) >= (up ? 256 * kWaves : 128 * kWaves);
+}
+// Into how many pieces the second product's width is cut: a work-group waits for its weights stretch by stretch, so four to a compute unit are wanted (the 33 tokens: 158 us, 163 in one piece).
 int pieces_of(int n, int experts, int d, int ff) {
-  if (!whole_rows(d, n, experts)) return 1;
+  if (!whole_rows(d, n, experts, false)) return 1;
   const int64_t groups = (int64_t)ceil_div(ceil_div(d, 16), kWaves) * std::min(n, experts);
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(4, ceil_div(ff, 2 * kStretch)), 1024 / groups));
 }
@@ -370,7 +376,7 @@ int launch_product(LayerArgs a, int pieces, hipStream_t stream) {
   const int tiles = ceil_div(a.rows, 16), experts = std::min(a.n, a.experts);
   a.by_expert = a.n > a.experts;
   a.piece = ceil_div(ceil_div(a.width, kStretch), pieces) * (kStretch / kBlock8);
-  if (whole_rows(a.rows, a.n, a.experts)) hipLaunchKernelGGL((layer8_product_kernel<Source, HIDDEN, GATED, true>), dim3(ceil_div(tiles, kWaves), experts, pieces), dim3(kThreads), 0, stream, a);
+  if (whole_rows(a.rows, a.n, a.experts, HIDDEN > 0)) hipLaunchKernelGGL((layer8_product_kernel<Source, HIDDEN, GATED, true>), dim3(ceil_div(tiles, kWaves), experts, pieces), dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL((layer8_product_kernel<Source, HIDDEN, GATED, false>), dim3(tiles, experts, pieces), dim3(kThreads), 0, stream, a);
   NMT_LAUNCH_CHECK();
   return NMT_OK;

@@ -354,6 +354,8 @@ extern "C" int nmt_op_norm8(const nmt_norm8* p, void* stream_) {
   ROWS8_LD(p->d_n, p->rows, p->ld_n, p->d, "n");
   ROWS8_LD(p->d_codes, p->rows, p->ld_codes, p->d, "codes");
   ROWS8_LD(p->d_scales, ceil_div(p->d, kBlock8), p->ld_scales, p->rows, "scales");
+  NMT_REQUIRE(p->rows <= 1 || ((!p->d_h || p->d_h != p->d_x || p->ld_h == p->ld_x) && (!p->d_n || p->d_n != p->d_y || p->ld_n == p->ld_y)),
+              "%s: what is written in place has the distance of what was read", who);
   Norm8Args a = {};
   a.rows = p->rows, a.d = p->d, a.kind = p->kind, a.eps = p->eps, a.resid_scale = p->resid_scale;
   a.ld_x = p->ld_x, a.ld_y = p->ld_y, a.ld_h = p->ld_h, a.ld_n = p->ld_n, a.ld_codes = p->ld_codes, a.ld_scales = p->ld_scales;

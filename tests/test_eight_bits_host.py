@@ -38,7 +38,7 @@ def norm(**kw):
 
 @pytest.mark.parametrize("bad", [dict(rows=-1), dict(rows=2 ** 31 - 1), dict(d=0), dict(d=16385), dict(type=3), dict(kind=2), dict(eps=0.0), dict(eps=float("nan")),
                                  dict(resid_scale=float("inf")), dict(ld_x=299), dict(ld_y=299), dict(ld_h=299), dict(ld_n=299), dict(ld_codes=299), dict(ld_scales=3),
-                                 dict(d_x=None), dict(d_gain=None), dict(d_codes=None), dict(d_scales=None), dict(d_y=None), dict(d_y=None, d_h=None, resid_scale=0.5)])
+                                 dict(d_x=None), dict(d_gain=None), dict(d_codes=None), dict(d_scales=None), dict(d_y=None), dict(d_y=None, d_h=None, resid_scale=0.5), dict(ld_h=301), dict(ld_n=301)])
 def test_norm_refuses(bad):
     refused(A.load().nmt_op_norm8(C.byref(norm(**bad)), None), says="nmt_op_norm8")
 

@@ -491,7 +491,8 @@ def test_layer_with_dropped_and_double_choices():
     check_layer(4, 2, 3, 64, 80, F16, "relu", none=1.1, add=True)
 
 
-@pytest.mark.parametrize("tokens,k,E,d,ff", [(3, 2, 8, 1024, 2048), (40, 4, 16, 512, 1024), (64, 2, 4, 300, 5000), (16, 2, 64, 256, 2000)])
+@pytest.mark.parametrize("tokens,k,E,d,ff", [(3, 2, 8, 1024, 2048), (40, 4, 16, 512, 1024), (64, 2, 4, 300, 5000), (16, 2, 64, 256, 2000),
+                                             (64, 8, 16, 520, 700), (8, 2, 64, 1030, 300)])
 def test_layer_of_many_work_groups(tokens, k, E, d, ff):
     check_layer(tokens, k, E, d, ff, F16, "silu_gate")
 
