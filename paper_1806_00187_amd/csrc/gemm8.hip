@@ -300,13 +300,13 @@ struct Product {
 // other; then comes the barrier behind which the stage is free and the next one is there, and the last G strips are multiplied column by column, so that one of B's fragments after the other is done
 // with and can be fetched for the next block long before it is needed.  What a matrix instruction leaves is multiplied by its scales and added up LAG instructions later, which is the
 // vector units' work beside the matrix units'.  The requests for the block after next are spread over the last strips.
-// BFINE: B's rows have a scale each; else the wavefront's columns share one.
+// BFINE: B's rows have a scale each; else the wavefront's columns share one.  (Tiles of 256 x 256 leave registers for a LAG of 2 then: 8192^3 540 us, with 3 770.)
 template <int BM, int BN, int NW, bool BFINE>
 struct Strips : Product<BM, BN, NW> {
   using P = Product<BM, BN, NW>;
   using typename P::OpA;
   using typename P::OpB;
-  static constexpr int TM = P::TM, TN = P::TN, G = TM < 3 ? TM : 3, ROWS = TM - G, SLOTS = TM * TN, LAG = 3, RING = 4;
+  static constexpr int TM = P::TM, TN = P::TN, G = TM < 3 ? TM : 3, ROWS = TM - G, SLOTS = TM * TN, LAG = BFINE && TM == 8 ? 2 : 3, RING = 4;
   static constexpr bool PER_STRIP = !BFINE && TM % 4 == 0;  // (of the strips in work at a time no two are the same modulo 4)
   static_assert(SLOTS % RING == 0, "");
   static_assert(P::WN <= BK, "a wavefront's columns share a scale");
@@ -690,14 +690,17 @@ __global__ void __launch_bounds__(256) gemm8_sums_kernel(const Gemm8Args g) {
 }
 
 // How a product is cut up: tiles of 256 x 256, 128 x 128 or 64 x 64, of which a compute unit holds one, two or four, and pieces along k.  What it takes is estimated from what was measured, microseconds: a
-// block of k with that many tiles on a compute unit, what a tile takes besides, and the sums of pieces.  Of 42 products (5 to 52701
-// rows, 512 to 52701 k, fp32 and bf16 results) timed in all forms 34 take the fastest, six one that is up to 11 % slower, two (6000 x 2900 x 1000 bf16, 777 x 5000 x 1000 fp32) one that is 24 % slower.  What the forms
-// are for, microseconds: 8192 x 8192 x 512 in tiles of 256 52; 3584 x 2048 x 512 of 256, 128 and 64 16, 10, 14; 300 x 1024 x 1024 20, 12, 8; 512 x 512 x 52701 whole and in 16 pieces of tiles of 128 367, 41.
+// block of k with that many tiles on a compute unit, what a tile takes besides, and the sums of pieces.  Of 65 products (5 to 52701 rows, 512 to 52701 k, fp32 and bf16 results, B's scales by squares and by
+// rows) timed in all forms 52 take the fastest, eleven one that is up to 11 % slower, two (6000 x 2900 x 1000 bf16, 777 x 5000 x 1000 fp32) one that is 24 % slower.  What the forms are for,
+// microseconds: 8192^3 in tiles of 256 and 128 480, 600 (B's rows with a scale each 540, 660); 3584 x 2048 x 512 of 256, 128 and 64 16, 10, 14; 300 x 1024 x 1024 20, 12, 8; 512 x 512 x 52701 whole and in 16 pieces,
+// of 128, 367, 41.
 struct Form {
   int tile, held;
   double block[4], besides;
 };
 constexpr Form kNarrow[] = {{256, 1, {1.6}, 5.0}, {128, 2, {0.9, 1.22}, 3.5}, {64, 4, {0.56, 0.66, 0.85, 1.1}, 2.5}};
+// (B's rows with a scale each)
+constexpr Form kFine[] = {{256, 1, {1.85}, 13.0}, {128, 2, {0.94, 1.27}, 3.5}, {64, 4, {0.6, 0.7, 0.9, 1.15}, 2.5}};
 constexpr Form kWide[] = {{128, 2, {1.36, 2.1}, 3.5}, {64, 4, {0.65, 0.8, 1.1, 1.4}, 2.5}};
 constexpr double kSums = 4.0, kSumsRate = 4e6;  // microseconds; bytes of pieces, written and read, in a microsecond
 struct Plan {
@@ -721,8 +724,7 @@ Plan plan(int M, int N, int K, int batch, bool ranges, bool wide, bool b_square)
     if (wide)
       for (const Form& f : kWide) look(f, splits);
     else
-      for (const Form& f : kNarrow)
-        if (f.tile < 256 || b_square) look(f, splits);
+      for (const Form& f : b_square ? kNarrow : kFine) look(f, splits);
   }
   return best;
 }
@@ -735,12 +737,13 @@ int launch_tiles(Gemm8Args g, hipStream_t stream) {
   g.tiles_m = (int)tiles_m, g.by_n = divisor((uint32_t)tiles_n), g.by_tiles = divisor((uint32_t)(tiles_m * tiles_n)), g.by_splits = divisor((uint32_t)g.splits);
   g.by_patch = divisor((uint32_t)(kPatch * tiles_n)), g.by_rows = divisor(kPatch), g.by_last = divisor((uint32_t)std::max<int64_t>(1, tiles_m % kPatch));
   // Tiles of 256 x 256: a work-group on each compute unit takes one after the other, where the requests of two blocks are of one tile or of two.
-  const bool turns = BM == 256 && g.splits == 1 && g.K > BK && !g.add;
+  const bool turns = BM == 256 && g.shift_b && g.splits == 1 && g.K > BK && !g.add;
   const int64_t launched = turns ? std::min<int64_t>(groups, device_info().cus / 8 * 8) : groups;
   g.launched = (uint32_t)launched;
   const dim3 grid((uint32_t)std::min<int64_t>(launched, kGridX), (uint32_t)((launched + kGridX - 1) / kGridX)), threads(64 * NW);
   if constexpr (BM == 256) {
-    if (turns && g.type == NMT_F16) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, false, half_t>), grid, threads, 0, stream, g);
+    if (!g.shift_b) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, true, false, void>), grid, threads, 0, stream, g);
+    else if (turns && g.type == NMT_F16) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, false, half_t>), grid, threads, 0, stream, g);
     else if (turns) hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, false, bf16_t>), grid, threads, 0, stream, g);
     else hipLaunchKernelGGL((gemm8_kernel<BM, BN, NW, false, false, void>), grid, threads, 0, stream, g);
   } else if (!WIDE && g.shift_b) {

@@ -297,7 +297,8 @@ def test_gemm_of_many_tiles_or_long_rows(M, N, K):
 FORMS = [(4400, 4355, 129, F16, (False, True), False, (256, 1)), (4400, 4400, 300, BF16, (False, True), False, (256, 1)), (4400, 4355, 512, F16, (True, True), True, (256, 1)),
          (4099, 4400, 128, BF16, (False, True), False, (256, 1)), (1024, 4096, 26001, BF16, (False, True), True, (256, 4)), (2100, 2111, 1000, F16, (False, True), True, (128, 1)),
          (2100, 2111, 640, BF16, (False, False), False, (128, 1)), (1000, 1000, 13001, F16, (False, False), True, (128, 4)), (2100, 2111, 300, F32, (True, False), True, (128, 1)),
-         (1024, 4096, 26001, F32, (False, False), True, (128, 2)), (700, 777, 500, BF16, (False, True), False, (64, 1)), (700, 130, 30001, F32, (False, True), True, (64, 12))]
+         (1024, 4096, 26001, F32, (False, False), True, (128, 2)), (700, 777, 500, BF16, (False, True), False, (64, 1)), (700, 130, 30001, F32, (False, True), True, (64, 12)),
+         (4096, 4099, 3001, BF16, (False, False), True, (128, 1)), (4096, 4090, 3001, BF16, (False, False), True, (256, 1)), (1024, 4096, 26001, F16, (True, False), True, (256, 4))]
 
 
 @pytest.mark.parametrize("M,N,K,dtype,squares,add,form", FORMS, ids=lambda v: str(v).replace("torch.", ""))
