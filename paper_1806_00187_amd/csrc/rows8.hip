@@ -22,7 +22,8 @@ struct QuantArgs {
 };
 
 // A work-group takes 128 x 128 elements, a thread 8 rows of 8 columns of them: 16 lanes hold 128 of a row, which share a scale, and a column's 128 are spread over 16
-// groups of lanes.  Codes of columns turn round in LDS, 8 rows of one column to a word of 8 bytes; words of a column are swapped about by the column, so that
+// groups of lanes.  Measured: 52701 x 1024 bf16 as it lies 26.6 us, 6.1 TB/s, its transpose 31 us, 5.2; 26001 x 1024 fp16 both 24 us, 4.5 TB/s; 4096 x 1024 fp32, squares, both 6.0.  Tiles of columns wait for all their rows and
+// for LDS; more work-groups to a compute unit than the two or three that registers allow spilled and were slower.  Codes of columns turn round in LDS, 8 rows of one column to a word of 8 bytes; words of a column are swapped about by the column, so that
 // the 16 lanes of a row write to different banks.
 // COLS: all 128 columns are there.
 template <typename T, bool COLS>
@@ -162,6 +163,8 @@ struct Norm8Args {
 };
 typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
 
+// A row is read once into registers, and everything is formed there.  Measured: 52701 x 1024 bf16 with a sum 67 us, 5.6 TB/s; 13000 x 2048 fp16 30, 6.3; 6000 x 4096 fp32 59, 5.4; 2000 x 16384 bf16 39, 5.8; 20000 x 1001 fp16 25, 5.6; 1531 x
+// 777 fp32 6.9; 5 x 512 fp16 2.2.
 // LANES lanes of each of WAVES wavefronts hold a row, VECS times eight elements each: 16 lanes hold the 128 that share a scale.
 template <typename T, int LANES, int VECS, int WAVES, bool RAGGED>
 __global__ void __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) norm8_kernel(const Norm8Args a) {
