@@ -7,8 +7,8 @@
 //
 // Bound by the matrix units and the card's power: 8192^3 with 16-bit results 480 us, 2300 TFLOP/s, the matrix units at work in 60 % of the cycles of a clock that falls to 1.8 GHz (the library's product of the
 // same codes without scales of blocks 360 us); 52701 x 4096 x 1024 236 us; 52012 rows of 128 experts, 1024 x 1024, 93 us.  Short sizes wait for memory and LDS once per block of k: 3584 x 2048 x 512 10 us, 5 x 2048 x 512 5 us.
-// fp32 results: 8192^3 1000 us, 1100 TFLOP/s (bf16 library product 790); 1024 x 4096 x 26001 230 us and the sums of its two pieces 13.  Without the widening of A's codes this would take 660, so more of a tile per wavefront would
-// help, but registers hold no more.
+// fp32 results: 8192^3 1000 us, 1100 TFLOP/s (bf16 library product 790); 1024 x 4096 x 26001 230 us and the sums of its two pieces 13.  The widening itself is 55 us of the 1000; the same instructions with A's operand
+// held constant take 750: most of the rest is what changing operands cost, in power.
 #include "block8.h"
 
 #include <algorithm>
