@@ -337,6 +337,26 @@ def test_gemm_of_a_batch_and_of_experts_in_large_tiles():
             check_product(c[first:first + count], a[first:first + count], sa[:, first:first + count], b[e], sb[e], F16, bias[e], None, e)
 
 
+def test_gemm_of_experts_whose_rows_have_a_scale_each_in_large_tiles():
+    counts, N, K = [7000, 0, 5288], 4090, 3000
+    rows = sum(counts)
+    assert A.nmt_debug_gemm8_form(rows, N, K, BF16, len(counts), True, b_square=False) == (256, 1)
+    a, sa = eight(rows, K, False, 61)
+    each = [eight(N, K, False, 70 + e) for e in range(len(counts))]
+    raw = torch.full((len(counts), N, ceil(K, 16) * 16), 0x7F, dtype=torch.uint8, device=DEV)
+    for e, (codes, _) in enumerate(each):
+        raw[e, :, :K] = codes.view(torch.uint8)
+    b, sb = raw.view(E4M3)[:, :, :K], torch.stack([s for _, s in each])
+    n = torch.tensor(counts, device=DEV)
+    ranges = torch.stack([n.cumsum(0) - n, n], 1).int()
+    c, uc = guarded(rows, N, BF16, torch.full((rows, N), 3.0), N + 1, 1)
+    A.nmt_op_gemm8(a, sa, b, sb, c, ranges=ranges)
+    assert uc()
+    for e, (first, count) in enumerate(ranges.tolist()):
+        if count:
+            check_product(c[first:first + count], a[first:first + count], sa[:, first:first + count], b[e], sb[e], BF16, None, None, e)
+
+
 def test_gemm_of_nothing():
     a, sa = torch.empty(40, 0, dtype=torch.uint8, device=DEV).view(E4M3), torch.empty(0, 40, device=DEV)
     bias, add = torch.randn(40, generator=gen(1), device=DEV), torch.randn(40, 40, generator=gen(2), device=DEV)
