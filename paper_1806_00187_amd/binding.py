@@ -862,7 +862,7 @@ def _stack(t, batch, rows, d, dtype, device, what):
     strides, shape = t.stride(), t.shape
     if batch == 1 and shape == (rows, d) and strides[1] == 1 and strides[0] >= d and rows > 1 and t.dtype is dtype and t.get_device() == device:
         return t.data_ptr(), strides[0], 0
-    if t.dtype is dtype and t.get_device() == device and ((shape == (rows, d) and batch == 1) or shape == (batch, rows, d)):
+    if t.dtype is dtype and t.get_device() == device and (shape == (batch, rows, d) or (batch == 1 and shape == (rows, d))):
         ld, step = strides[-2:]
         if rows <= 1:
             ld = d
