@@ -7,7 +7,7 @@
 namespace {
 
 constexpr int kMaxRows = 0x7FFFFFFF - 65536, kMaxCols = 16384;
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kGridX = 1 << 22;  // work-groups in a row of the grid: one has less than 2^32 threads
 
 // ---- a matrix into 8 bits --------------------------------------------------------------------------
@@ -21,23 +21,23 @@ struct QuantArgs {
   Divisor col_tiles;
 };
 
-// A work-group takes 128 x 128 elements, a thread 8 rows of 8 columns of them: 16 lanes hold 128 of a row, which share a scale, and a column's 128 are spread over 16
-// groups of lanes.  Measured: 52701 x 1024 bf16 as it lies 26.6 us, 6.1 TB/s, its transpose 31 us, 5.2; 26001 x 1024 fp16 both 24 us, 4.5 TB/s; 4096 x 1024 fp32, squares, both 6.0.  Tiles of columns wait for all their rows and
-// for LDS; more work-groups to a compute unit than the two or three that registers allow spilled and were slower.  Codes of columns turn round in LDS, 8 rows of one column to a word of 8 bytes; words of a column are swapped about by the column, so that
-// the 16 lanes of a row write to different banks.
+// A work-group takes 128 x 128 elements, a thread 4 rows of 8 columns of them: 16 lanes hold 128 of a row, which share a scale, and a column's 128 are spread over 32
+// groups of lanes.  (8 rows to a thread: three work-groups of half as many wavefronts to a compute unit, 26001 x 1024 24 us instead of 22.)  Codes of columns turn round in LDS, 4 rows of one column to a word; words of a column are
+// swapped about by fours, by the column, so that the 16 lanes of a row write to different banks and a column's 16 codes lie side by side.
+// Measured: 52701 x 1024 bf16 as it lies 25.4 us, 6.4 TB/s, its transpose 28, 5.8; 26001 x 1024 fp16 both 21.9, 4.9; 26001 x 4096 91; 4096 x 1024 fp32, squares, both 6.0.  Columns wait for all rows of a tile and twice for LDS.
 // COLS: all 128 columns are there.
 template <typename T, bool COLS>
-__device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, int64_t c0, uint64_t (&turn)[128][16], uint32_t (&tops)[4][128]) {
+__device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, int64_t c0, uint32_t (&turn)[128][32], uint32_t (&tops)[8][128], float (&backs)[128]) {
   const int lane16 = threadIdx.x & 15, group = threadIdx.x >> 4, wave = threadIdx.x >> 6;
-  const int64_t r = r0 + 8 * group, c = c0 + 8 * lane16;
-  const int rows = (int)min((int64_t)a.rows - r, (int64_t)8), cols = (int)max(min((int64_t)a.d - c, (int64_t)8), (int64_t)0);  // of this thread's (rows may be negative)
+  const int64_t r = r0 + 4 * group, c = c0 + 8 * lane16;
+  const int rows = (int)min((int64_t)a.rows - r, (int64_t)4), cols = (int)max(min((int64_t)a.d - c, (int64_t)8), (int64_t)0);  // of this thread's (rows may be negative)
   const T* x = static_cast<const T*>(a.x);
   // (kept as they came, and made numbers where they are used: 64 registers less for rows of 16 bits)
-  Eight<T, !COLS> t[8];
+  Eight<T, !COLS> t[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) t[i].load(x + min(r + i, (int64_t)a.rows - 1) * a.ld_x, (int)c, a.d);
+  for (int i = 0; i < 4; ++i) t[i].load(x + min(r + i, (int64_t)a.rows - 1) * a.ld_x, (int)c, a.d);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 4; ++i) {
     t[i].v = t[i].settled((int)c, a.d);
     if (i >= rows) t[i].v = typename Eight<T, !COLS>::vec{};
   }
@@ -45,19 +45,19 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = (float)t[i].v[e];
   };
-  auto column_of = [&](int e, float (&v)[8]) {
+  auto column_of = [&](int e, float (&v)[4]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)t[i].v[e];
+    for (int i = 0; i < 4; ++i) v[i] = (float)t[i].v[e];
   };
   auto apart = [&] {  // (what was made of them is not kept)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(t[i].v));
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(t[i].v));
   };
   Scale8 whole = {0.f, 0.f};
   if (a.square) {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       float v[8];
       row_of(i, v);
       top = max(top, magnitude8(v));
@@ -68,7 +68,7 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
     __syncthreads();
     top = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, tops[0][i]);
+    for (int i = 0; i < 32; ++i) top = max(top, tops[0][i]);
     whole = scale8(top);
     if (threadIdx.x == 0) {
       if (a.codes) a.scales[(c0 >> 7) * a.ld_scales + (r0 >> 7)] = whole.scale;
@@ -77,7 +77,7 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
   }
   if (a.codes) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       Scale8 s = whole;
       float v[8];
       row_of(i, v);
@@ -94,7 +94,7 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
     if (!a.square) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float v[8];
+        float v[4];
         column_of(e, v);
         uint32_t top = magnitude8(v);
         const auto rows16 = __builtin_amdgcn_permlane16_swap(top, top, false, false);
@@ -105,34 +105,38 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
       }
       apart();
       __syncthreads();
+      // a column's scale is formed once, by one thread
+      const int col = threadIdx.x;
+      if (col < kBlock8) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) top = max(top, tops[w][col]);
+        const Scale8 s = scale8(top);
+        if (c0 + col < a.d) a.scales_t[(r0 >> 7) * a.ld_scales_t + c0 + col] = s.scale;
+        backs[col] = s.back;
+      }
+      __syncthreads();
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      Scale8 s = whole;
-      float v[8];
+      float v[4];
       column_of(e, v);
-      if (!a.square) {
-        const int at = 8 * lane16 + e;
-        s = scale8(max(max(tops[0][at], tops[1][at]), max(tops[2][at], tops[3][at])));
-        if (group == 0 && e < cols) a.scales_t[(r0 >> 7) * a.ld_scales_t + c + e] = s.scale;
-      }
-      const uint32_t lo = codes8(v[0], v[1], v[2], v[3], s.back), hi = codes8(v[4], v[5], v[6], v[7], s.back);
-      turn[8 * lane16 + e][group ^ lane16] = (uint64_t)hi << 32 | lo;
+      turn[8 * lane16 + e][group ^ (lane16 & 7) << 2] = codes8(v[0], v[1], v[2], v[3], a.square ? whole.back : backs[8 * lane16 + e]);
     }
     __syncthreads();
     // a column's 128 codes lie with 8 lanes, 16 each
     const int at = threadIdx.x & 7;
     const int64_t row = r0 + 16 * at;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int col = (threadIdx.x >> 3) + 32 * i, by = col >> 3;
-      const uint64_t w0 = turn[col][(2 * at) ^ by], w1 = turn[col][(2 * at + 1) ^ by];
+    for (int i = 0; i < 2; ++i) {
+      const int col = (threadIdx.x >> 3) + 64 * i;
+      const code4_t w = *reinterpret_cast<const code4_t*>(&turn[col][4 * (at ^ (col >> 3 & 7))]);
       if (c0 + col >= a.d) continue;
       uint8_t* to = a.codes_t + (c0 + col) * a.ld_codes_t + row;
       if (row + 16 <= a.rows) {
-        *reinterpret_cast<code4_any*>(to) = code4_any{(uint32_t)w0, (uint32_t)(w0 >> 32), (uint32_t)w1, (uint32_t)(w1 >> 32)};
+        *reinterpret_cast<code4_any*>(to) = (code4_any)w;
       } else {
-        for (int e = 0; row + e < a.rows; ++e) to[e] = (uint8_t)((e < 8 ? w0 : w1) >> 8 * (e & 7));
+        for (int e = 0; row + e < a.rows; ++e) to[e] = (uint8_t)((e < 8 ? e < 4 ? w[0] : w[1] : e < 12 ? w[2] : w[3]) >> 8 * (e & 3));
       }
     }
   }
@@ -140,15 +144,16 @@ __device__ __forceinline__ void quantize_tile(const QuantArgs& a, int64_t r0, in
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) quantize8_kernel(const QuantArgs a) {
-  __shared__ uint64_t turn[128][16];
-  __shared__ uint32_t tops[4][128];
+  __shared__ __attribute__((aligned(16))) uint32_t turn[128][32];
+  __shared__ uint32_t tops[8][128];
+  __shared__ __attribute__((aligned(16))) float backs[128];
   const int64_t tile = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   if (tile >= a.tiles) return;
   uint32_t col;
   const uint32_t row = div_mod((uint32_t)tile, a.col_tiles, col);
   const int64_t r0 = (int64_t)row * kBlock8, c0 = (int64_t)col * kBlock8;
-  if (c0 + kBlock8 <= a.d) quantize_tile<T, true>(a, r0, c0, turn, tops);
-  else quantize_tile<T, false>(a, r0, c0, turn, tops);
+  if (c0 + kBlock8 <= a.d) quantize_tile<T, true>(a, r0, c0, turn, tops, backs);
+  else quantize_tile<T, false>(a, r0, c0, turn, tops, backs);
 }
 
 // ---- the norm ----------------------------------------------------------------------------------------
