@@ -163,9 +163,11 @@ __device__ __forceinline__ bool place(const Gemm8Args& g, uint32_t id, int BM, i
   }
   p.split = 0;
   const int lane = threadIdx.x & 63, per = (g.batch + 63) / 64;
+  // (cut at both ends: what lies below row 0 is no part of the count; no sum leaves 32 bits)
   auto range = [&](int e, int& first, int& count) {
-    first = max(0, min(g.ranges[2 * e], g.M));
-    count = max(0, min(g.ranges[2 * e + 1], g.M - first));
+    const int from = g.ranges[2 * e], rows = g.ranges[2 * e + 1];
+    first = max(0, min(from, g.M));
+    count = max(0, min(max(rows, 0) + min(from, 0), g.M - first));
   };
   uint32_t mine = 0;
   int first, count;

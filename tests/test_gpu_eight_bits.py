@@ -433,6 +433,61 @@ def test_gemm_of_experts(counts, square, N, K):
     assert (c[2:M - 1] == 3).all() and uc()
 
 
+def experts_weights(E, N, K, square, seed):
+    """[E, N, K] codes in a buffer of no numbers, and their scales."""
+    each = [eight(N, K, square, seed + e % 5) for e in range(E)]
+    raw = torch.full((E, N, ceil(K, 16) * 16), 0x7F, dtype=torch.uint8, device=DEV)
+    for e, (codes, _) in enumerate(each):
+        raw[e, :, :K] = codes.view(torch.uint8)
+    return raw.view(E4M3)[:, :, :K], torch.stack([s for _, s in each])
+
+
+def check_ranges(M, N, K, ranges, dtype, square=True, bias=True, add=False, in_place=False):
+    """Rows of each range that lie in [0, M) are the product's, all others are left as they were."""
+    E = len(ranges)
+    a, sa = eight(M, K, False, 80)
+    b, sb = experts_weights(E, N, K, square, 81)
+    g = gen(82)
+    bias = torch.randn(E, N, generator=g, device=DEV).to(dtype) if bias else None
+    old, plus = (4 * torch.randn(M, N, generator=g, device=DEV).to(dtype) for _ in range(2))
+    c, uc = guarded(M, N, dtype, old, N + 3, 1)
+    plus = old if in_place else plus
+    A.nmt_op_gemm8(a, sa, b, sb, c, bias=bias, add=(c if in_place else plus) if add else None, ranges=torch.tensor(ranges, dtype=torch.int32, device=DEV),
+                   scratch=scratch_for(M, N, K, E, True))
+    torch.cuda.synchronize()
+    assert uc()
+    left = torch.ones(M, dtype=torch.bool, device=DEV)
+    for e, (first, count) in enumerate(ranges):
+        r = slice(max(first, 0), max(0, min(first + max(count, 0), M)))
+        if r.start < r.stop:
+            assert left[r].all(), "ranges overlap"
+            left[r] = False
+            check_product(c[r], a[r], sa[:, r], b[e], sb[e], dtype, bias[e] if bias is not None else None, plus[r] if add else None, (e, first, count))
+    assert torch.equal(c[left], old[left])
+
+
+# a part of the rows: ranges of all of them less the part's start, so that some begin before row 0 and some end behind the last
+PARTS = [(200, 70, 300, F16, True, 64), (700, 300, 200, BF16, False, 64), (700, 300, 200, F32, True, 64), (3000, 2000, 300, BF16, True, 128), (3000, 2000, 300, F32, False, 128),
+         (9000, 2000, 300, F16, True, 256), (9000, 2000, 300, F16, False, 128)]
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("M,N,K,dtype,square,tile", PARTS, ids=lambda v: str(v).replace("torch.", ""))
+def test_gemm_of_experts_whose_ranges_reach_past_both_ends(M, N, K, dtype, square, tile, add):
+    counts = [M // 3, M // 2 + 11, 0, M // 4 + 3, M]
+    assert A.nmt_debug_gemm8_form(M, N, K, dtype, len(counts), True, b_square=square)[0] == tile
+    for start in (M // 3 - 3, M // 3 + 7, 1):   # (three rows of the first expert, none, all but one)
+        firsts = [sum(counts[:e]) - start for e in range(len(counts))]
+        check_ranges(M, N, K, list(zip(firsts, counts)), dtype, square, bias=not add, add=add, in_place=add and start == 1)
+
+
+def test_gemm_of_experts_ranges_of_any_integers():
+    low, high = -2 ** 31, 2 ** 31 - 1
+    ranges = [(-7, 10), (3, 20), (-7, 7), (-7, 5), (23, -4), (30, 0), (-5, -5), (low, high), (low, low), (high, high), (high, 5), (95, high), (50, 1)]
+    for dtype in TYPES:
+        check_ranges(100, 40, 200, ranges, dtype, add=dtype is F32)
+
+
 # ---- the sparse layer ------------------------------------------------------------------------------
 def layer_inputs(tokens, k, E, d, ff, dtype, act, seed, none=0.0, twice=False):
     g = gen(seed)
