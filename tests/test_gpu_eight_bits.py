@@ -595,6 +595,60 @@ def test_layer_of_infinities_and_huge_inputs():
     assert torch.isfinite(huge[0]).all() and float((huge[0] - ref[0]).norm() / ref[0].norm()) < 1e-5
 
 
+def plain_layer(x, ids, weights, up, su, down, sd, act):
+    """The layer in 64 bits, and a bound of fp32's roundings (no additions, all choices there)."""
+    tokens, d = x.shape
+    ff = down.shape[2]
+    want, bound = (torch.zeros(tokens, d, dtype=D, device=DEV) for _ in range(2))
+    for t, row in enumerate(ids.tolist()):
+        for j, e in enumerate(row):
+            X, U, V = x[t].to(D), decode(up[e], su[e]), decode(down[e], sd[e])
+            g, eg = U @ X, (d + ceil(d) + 8) * U32 * (U.abs() @ X.abs())
+            if act == "relu":
+                h, eh = g.clamp(min=0), eg
+            else:
+                s = torch.sigmoid(g[:ff])
+                h = s * g[:ff] * g[ff:]
+                eh = 1.1 * eg[:ff] * g[ff:].abs() + s * g[:ff].abs() * eg[ff:] + 16 * U32 * h.abs()   # (exponential, sum, quotient and product: 11 of them at most)
+            eh = eh + h.abs() * (2.0 ** -18 if x.dtype is not F32 else 2.0 ** -27)
+            want[t] += float(weights[t, j]) * (V @ h)
+            bound[t] += float(weights[t, j]) * (V.abs() @ eh + (ff + ceil(ff) + 8 + ids.shape[1]) * U32 * (V.abs() @ h.abs()))
+    return want, bound
+
+
+# (sizes of which one product, the other or none gives every wavefront rows of its own)
+@pytest.mark.parametrize("act", ["relu", "silu_gate"])
+@pytest.mark.parametrize("tokens,k,E,d,ff", [(5, 2, 4, 300, 200), (16, 2, 64, 256, 2000), (64, 8, 16, 520, 700)])
+def test_layer_of_scales_near_the_end_of_the_range(tokens, k, E, d, ff, act):
+    """Scales from 2^111 on, as weights of 2^120 have them: finite where the sums are, and nothing comes of inputs that are zero."""
+    x, ids, weights, (up, su), (down, sd) = layer_inputs(tokens, k, E, d, ff, F32, act, 37)
+    scratch = torch.empty(A.nmt_op_expert_layer8_scratch(tokens, k, E, d, ff), device=DEV)
+    # scales from 2^110 to 2^114; hidden values of some 2^32, 2^64 behind the gate; and back
+    down_by = 32 if act == "relu" else 64
+    x *= 2.0 ** -90
+    x[1], x[2:, :128] = 0, 0
+    x[0, :128] *= 2.0 ** -20
+    su, sd = su * 2.0 ** 122, sd * 2.0 ** -down_by
+    su[:, 0] = 2.0 ** 119       # (only token 0 has anything there)
+    assert float(su[:, 1:].max()) > 2.0 ** 111 > float(su.min())
+    out = torch.full_like(x, 7.0)
+    A.nmt_op_expert_layer8(x, ids, weights, up, su, down, sd, out, scratch, act=act)
+    want, bound = plain_layer(x, ids, weights, up, su, down, sd, act)
+    assert (out[1] == 0).all()
+    within(out, want, bound + half_step(F32) * want.abs(), "out of large up")
+    # the second product's
+    x = torch.randn(tokens, d, generator=gen(38), device=DEV) * 2.0 ** (-40 if act == "relu" else -30)
+    x[1] = 0
+    su = su * 2.0 ** -122
+    su[:, 0] = su[:, -1]
+    for exponent in (100, 118):
+        sd = torch.full_like(sd, 2.0 ** exponent)
+        A.nmt_op_expert_layer8(x, ids, weights, up, su, down, sd, out, scratch, act=act)
+        want, bound = plain_layer(x, ids, weights, up, su, down, sd, act)
+        assert (out[1] == 0).all()
+        within(out, want, bound + half_step(F32) * want.abs(), ("out of large down", exponent))
+
+
 # ---- as they are used ------------------------------------------------------------------------------
 def test_graphs_streams_and_the_same_bits_again():
     """Every operator captured, and replayed with eager calls and other inputs between: each replay gives the eager call's bits."""
