@@ -519,7 +519,8 @@ typedef struct nmt_norm8 {
 int nmt_op_norm8(const nmt_norm8* a /*host*/, void* stream);
 
 /* C[M, N] = A B^T + bias + add for A [M, K] and B [N, K] in 8 bits: products of codes are summed in fp32 over each block of 128 k and times its scales added up in fp32, in increasing k
- * (a long contraction of a small C in pieces, in a fixed order), rounded once to `type`.  For results of 16 bits the matrix instruction adds eight products of codes at a time, to 13 bits below the largest one's power of two
+ * (a long contraction of a small C in pieces, in a fixed order), rounded once to `type`.  A block's two scales are multiplied by each other first: one may be as large as the other is small, but their product is to
+ * be 0 or a normal number of fp32.  (Beyond fp32 what comes of the block is infinite, or NaN where its sum is 0; below 2^-126 it is off by up to 2^-125.)  For results of 16 bits the matrix instruction adds eight products of codes at a time, to 13 bits below the largest one's power of two
  * (some 1.5e-5 of a result, at most 2^-10 of the sum of the terms' magnitudes); for fp32 results every product counts in full.  a_square, b_square: whether 128 x 128 elements share a scale.  d_bias [N] and d_add [M, N], of C's type, may be
  * NULL; d_add may be d_c with the same distances.  y = x W^T: A = x, B = W; the input's gradient: A = dy, B = W transposed; the weight's: A = dy transposed, B = x transposed.
  * batch products lie stride_* apart (bytes of A and B, elements of the others; 0: the same for all; of C not).

@@ -380,6 +380,36 @@ def test_gemm_scales_of_one_row_do_not_reach_another():
     assert torch.equal(c, want)
 
 
+# (tiles of every size, one after the other or not, with squares or rows of B, pieces along k)
+SCALED = [(70, 90, 300, F16, True), (70, 90, 300, F32, False), (2100, 2111, 300, BF16, False), (2100, 2111, 300, F32, True), (4400, 4355, 300, BF16, True), (4096, 4090, 3001, BF16, False),
+          (700, 130, 30001, F32, True)]
+
+
+@pytest.mark.parametrize("M,N,K,dtype,square", SCALED, ids=lambda v: str(v).replace("torch.", ""))
+def test_gemm_of_scales_whose_product_is_a_normal_number(M, N, K, dtype, square):
+    """Neither scale is met by the sums alone: one may be as large as the other is small."""
+    (a, sa), (b, sb) = eight(M, K, False, 90), eight(N, K, square, 91)
+    c = torch.empty(M, N, dtype=dtype, device=DEV)
+    # scales of eight(): exp(randn) / 64, 2^-15 to 2^3; sums of a block: less than 2^25
+    for up, down in ((112, -112), (-106, 106)) + (((60, 36), (-50, -46)) if dtype is not F16 else ()):
+        scratch = scratch_for(M, N, K)
+        A.nmt_op_gemm8(a, sa * 2.0 ** up, b, sb * 2.0 ** down, c, scratch=scratch)
+        check_product(c, a, sa * 2.0 ** up, b, sb * 2.0 ** down, dtype, what=(up, down))
+
+
+def test_gemm_of_scales_whose_product_is_next_to_nothing():
+    """Such a product of scales is off by 2^-150 at most, and a block's sum is less than 2^25."""
+    for dtype, square in ((F32, False), (F32, True), (BF16, True), (BF16, False)):
+        (a, sa), (b, sb) = eight(70, 300, False, 92), eight(90, 300, square, 93)
+        sa, sb = sa * 2.0 ** -90, sb * 2.0 ** -40
+        c = torch.empty(70, 90, dtype=dtype, device=DEV)
+        A.nmt_op_gemm8(a, sa, b, sb, c)
+        X, W = decode(a, sa), decode(b, sb)
+        want, mag = X @ W.t(), X.abs() @ W.abs().t()
+        cut = 0.0 if dtype is F32 else 2.0 ** -10
+        within(c, want, half_step(dtype) * want.abs() + (cut + 320 * U32) * mag + 3 * 2.0 ** -125, dtype)
+
+
 @pytest.mark.parametrize("batch,M,N,K", [(1, 30, 40, 128), (3, 100, 70, 256), (7, 64, 65, 384), (40, 200, 300, 128), (2, 300, 200, 5120)])
 def test_gemm_of_a_batch(batch, M, N, K):
     """Weight gradients of experts with room for K rows each: matrices side by side in columns."""
