@@ -226,6 +226,18 @@ def test_norm_of_zeros_and_of_no_numbers():
     assert torch.isfinite(codes[4:].float()).all()
 
 
+# widths of every form, whole and with a part of eight, and rows that are more than there is room for at a time: a worker has several, and the next one is asked for beside this one's stores
+MANY = [(270001, 100), (140001, 200), (70001, 512), (70001, 777), (33001, 2048), (33001, 1100), (17001, 2100), (9001, 4104), (9001, 5001), (1201, 8200), (1201, 9001), (1100, 16384)]
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("rows,d", MANY)
+def test_norm_of_several_rows_to_a_worker(rows, d, kind):
+    for dtype in TYPES if d > 8192 else (F16,):
+        check_norm(rows, d, dtype, kind, 0.9)
+        check_norm(rows, d, dtype, kind, 0.9, ld=d + 3, off=1, in_place=True)
+
+
 # ---- products --------------------------------------------------------------------------------------
 def eight(rows, d, square, seed, pad=0, shift_rows=0):
     """Codes [rows, d] in a buffer of no numbers, rows at multiples of 16 bytes, and scales."""
