@@ -369,6 +369,53 @@ def test_gemm_of_experts_whose_rows_have_a_scale_each_in_large_tiles():
             check_product(c[first:first + count], a[first:first + count], sa[:, first:first + count], b[e], sb[e], BF16, None, None, e)
 
 
+# (K of a part of a block, of a part of 16 codes, of one code more, in one piece and in several)
+ENDS = FORMS + [(100, 70, 129, F16, (False, True), False, (64, 1)), (100, 70, 143, BF16, (False, False), False, (64, 1)), (100, 70, 2000, F32, (False, True), False, (64, 8))]
+
+
+@pytest.mark.parametrize("M,N,K,dtype,squares,add,form", ENDS, ids=lambda v: str(v).replace("torch.", ""))
+def test_gemm_counts_the_ends_of_rows_and_of_pieces(M, N, K, dtype, squares, add, form):
+    """A few columns of k make up nearly all of a result: the first and the last, those next to a border of 16, of blocks or of pieces.  Any of them is some 2^-4 of most results, which are
+    bound to 2^-10 of the sum of their terms' magnitudes and a rounding."""
+    tile, splits = A.nmt_debug_gemm8_form(M, N, K, dtype, b_square=squares[1])
+    assert (tile, splits) == form
+    piece = ceil(ceil(K), splits) * 128
+    ends = {0, 1, K - 1, K // 16 * 16 - 1, K // 16 * 16, (K - 1) // 128 * 128, (K - 1) // 128 * 128 - 1} | {p * piece + i for p in range(1, splits) for i in (-1, 0)}
+    ends = torch.tensor(sorted(k for k in ends if 0 <= k < K), device=DEV)
+    (a, sa), (b, sb) = eight(M, K, squares[0], 94), eight(N, K, squares[1], 95)
+    for t, seed in ((a, 96), (b, 97)):
+        v = (t.float() / 2.0 ** 12).to(E4M3)
+        g = gen(seed)
+        v[:, ends] = ((64 + 384 * torch.rand(t.shape[0], len(ends), generator=g, device=DEV)) * (1 - 2 * torch.randint(0, 2, (t.shape[0], len(ends)), generator=g, device=DEV))).to(E4M3)
+        t.view(torch.uint8).copy_(v.view(torch.uint8))
+    sa.fill_(1 / 64), sb.fill_(1 / 32)
+    c = torch.empty(M, N, dtype=dtype, device=DEV)
+    A.nmt_op_gemm8(a, sa, b, sb, c, scratch=scratch_for(M, N, K))
+    check_product(c, a, sa, b, sb, dtype)
+
+
+@pytest.mark.parametrize("large", [0, 5, 31, 63, 77, 127])
+def test_gemm_of_16_bit_results_drops_what_lies_13_bits_below_the_largest_of_eight(large):
+    """One large product, the same with the other sign 64 further on, and a small one in every other place: that 13 bits below counts everywhere; half of it does where neither of the large ones is among its
+    eight.  For fp32 results everything counts."""
+    away = (large + 64) % 128
+    places = torch.tensor([k for k in range(128) if k not in (large, away)], device=DEV)
+    b, one, ones = torch.ones(16, 128, device=DEV).to(E4M3), torch.ones(1, 16, device=DEV), torch.ones(1, 126, device=DEV)
+
+    def result(small, dtype):
+        a = torch.zeros(126, 128, device=DEV)
+        a[:, large], a[:, away] = 256, -256
+        a[torch.arange(126, device=DEV), places] = small
+        c = torch.empty(126, 16, dtype=dtype, device=DEV)
+        A.nmt_op_gemm8(a.to(E4M3), ones, b, one, c)
+        assert (c == c[:, :1]).all()
+        return c[:, 0].float()
+    for dtype in (F16, BF16):
+        assert (result(2.0 ** -5, dtype) == 2.0 ** -5).all()
+        assert int((result(2.0 ** -6, dtype) != 2.0 ** -6).sum()) == 14
+    assert (result(2.0 ** -9, F32) == 2.0 ** -9).all()
+
+
 def test_gemm_of_nothing():
     a, sa = torch.empty(40, 0, dtype=torch.uint8, device=DEV).view(E4M3), torch.empty(0, 40, device=DEV)
     bias, add = torch.randn(40, generator=gen(1), device=DEV), torch.randn(40, 40, generator=gen(2), device=DEV)
@@ -438,6 +485,28 @@ def test_gemm_of_a_batch(batch, M, N, K):
     # one A for all
     A.nmt_op_gemm8(fa[0].expand(batch, M, K), ta[0].expand(batch, K // 128, M), fb, tb, c, scratch=scratch_for(M, N, K, batch))
     check_product(c[batch - 1], fa[0], ta[0], fb[batch - 1], tb[batch - 1], F16)
+
+
+@pytest.mark.parametrize("square", [False, True])
+@pytest.mark.parametrize("batch,M,N,K,dtype,tile", [(3, 100, 70, 256, BF16, 64), (3, 100, 70, 200, F32, 64), (2, 300, 200, 5120, F32, 64), (2, 300, 200, 5120, BF16, 64), (5, 1100, 1000, 300, F32, 128),
+                                                    (5, 1100, 1000, 300, BF16, 128), (4, 2100, 2000, 400, BF16, 256)], ids=lambda v: str(v).replace("torch.", ""))
+def test_gemm_of_a_batch_of_any_type(batch, M, N, K, dtype, tile, square):
+    """Each with its own a, b, bias and addend, in place; rows and matrices further apart than they are long."""
+    if tile == 256 and not square:
+        tile = 128     # (rows of B with a scale each)
+    assert A.nmt_debug_gemm8_form(M, N, K, dtype, batch, b_square=square)[0] == tile
+    (a, sa), (b, sb) = experts_weights(batch, M, K, False, 83), experts_weights(batch, N, K, square, 84)
+    g = gen(85)
+    bias = torch.randn(batch, N, generator=g, device=DEV).to(dtype)
+    old = (4 * torch.randn(batch, M, N, generator=g, device=DEV)).to(dtype)
+    c, uc = guarded(batch * (M + 1), N, dtype, None, N + 5, 1)
+    c = c.as_strided((batch, M, N), ((M + 1) * (N + 5), N + 5, 1))
+    c.copy_(old)
+    A.nmt_op_gemm8(a, sa, b, sb, c, bias=bias, add=c, scratch=scratch_for(M, N, K, batch))
+    torch.cuda.synchronize()
+    assert uc()
+    for e in range(batch):
+        check_product(c[e], a[e], sa[e], b[e], sb[e], dtype, bias[e], old[e], e)
 
 
 COUNTS = [[0, 5, 0, 1, 200, 0], [64, 64], [300], [0, 0], [1] * 70, [129, 0, 257, 128, 3], [0] * 500 + [17] + [0] * 400 + [90]]
