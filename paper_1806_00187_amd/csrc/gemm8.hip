@@ -54,6 +54,7 @@ __device__ __forceinline__ Gemm8Args arguments() {
 }
 // One wave instruction: lane L's SIZE bytes, `at` bytes from base on, land at lds + SIZE L; zeros where `at` is kOob.  Written as an instruction because the compiler holds every read of LDS up
 // until all such requests have arrived; whoever reads what this brings waits for it (arrived()).  The waits are those that the compiler would put behind a vector instruction that has written one of the scalars.
+// m0 is one of the registers that the compiler reserves and takes no word of a change of: nothing else in these kernels may use it, which is checked on the built library.
 template <int SIZE>
 __device__ __forceinline__ void request_to_lds(uint64_t base, uint32_t lds, uint32_t at) {
   typedef uint32_t rsrc_t __attribute__((ext_vector_type(4)));
