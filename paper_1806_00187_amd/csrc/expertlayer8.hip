@@ -365,13 +365,13 @@ __global__ void __launch_bounds__(kThreads) layer8_sum_kernel(const SumArgs a) {
 // the second, whose width can be cut.  With and without, microseconds of the layer: 33 tokens, 4 of 64 experts, 1024 x 4096 157, 236; 64 tokens, 8 of 16, 512 x 2048 (32 choices of an expert) 60, 70;
 // 8 tokens, 2 of 64, 1024 x 4096 (1024 wavefronts for the second product) 32, 36; but one token, 4 of 16, 2048 x 4096 36, 28; 2 of 8, 512 x 2048 15, 11.
 bool whole_rows(int rows, int n, int experts, bool up) {
-  return (int64_t)ceil_div(rows, 16) * std::max(std::min(n, experts), n / 16) >= (up ? 256 * kWaves : 128 * kWaves);
+  return (int64_t)ceil_div(rows, 16) * std::max(std::min(n, experts), n / 16) >= (int64_t)device_info().cus * kWaves / (up ? 1 : 2);
 }
 // Into how many pieces the second product's width is cut: a work-group waits for its weights stretch by stretch, so four to a compute unit are wanted (the 33 tokens: 158 us, 163 in one piece).
 int pieces_of(int n, int experts, int d, int ff) {
   if (!whole_rows(d, n, experts, false)) return 1;
   const int64_t groups = (int64_t)ceil_div(ceil_div(d, 16), kWaves) * std::min(n, experts);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(4, ceil_div(ff, 2 * kStretch)), 1024 / groups));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(4, ceil_div(ff, 2 * kStretch)), 4ll * device_info().cus / groups));
 }
 template <typename Source, int HIDDEN, bool GATED>
 int launch_product(LayerArgs a, int pieces, hipStream_t stream) {
