@@ -549,8 +549,9 @@ int nmt_debug_gemm8_form(int32_t M, int32_t N, int32_t K, int32_t batch, int32_t
 /* A sparse layer as a whole over few tokens (at most 64; more: nmt_op_expert_dispatch, nmt_op_gemm8, nmt_op_expert_combine), as when one token of each sentence is at hand:
  *   hidden[t, j] = act(up[expert[t, j]] x[t]),  out[t] = add[t] + sum over j of weights[t, j] * down[expert[t, j]] hidden[t, j].
  * act NMT_ACT_RELU: up [experts, ff, d], max(., 0).  NMT_ACT_SILU_GATE: up [experts, 2 ff, d], g / (1 + exp(-g)) * u of its rows r (g) and ff + r (u).  down [experts, d, ff].  Weights in 8 bits with
- * square scales, experts stride_* apart (bytes; floats of the scales), rows at multiples of 16 bytes.  x, add and out are of `type`; products, hidden and sums fp32, with the inputs as they are (not in
- * 8 bits), out rounded once.  d_expert [tokens, k]: a value outside [0, experts) is none and adds nothing, whatever its weight; only experts that are chosen are read.
+ * square scales, experts stride_* apart (bytes; floats of the scales), rows at multiples of 16 bytes.  x, add and out are of `type`; products are of the inputs as they are (not in
+ * 8 bits), sums fp32, out rounded once.  hidden goes from one product to the next rounded to within 2^-17 of itself (fp32: as it is).  What of x or hidden is below 2^-80, and what a block of 128 adds below 2^-109, may count with
+ * fewer bits.  d_expert [tokens, k]: a value outside [0, experts) is none and adds nothing, whatever its weight; only experts that are chosen are read.
  * d_weights fp32 [tokens, k], NULL: 1.  d_add may be NULL, or d_out with the same distance.
  * d_scratch: 16-byte aligned, scratch_floats >= nmt_op_expert_layer8_scratch.  k <= 64, experts <= 1024, d and ff <= 2^20. */
 #define NMT_ACT_RELU 0

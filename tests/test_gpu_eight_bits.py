@@ -721,10 +721,35 @@ def plain_layer(x, ids, weights, up, su, down, sd, act):
                 s = torch.sigmoid(g[:ff])
                 h = s * g[:ff] * g[ff:]
                 eh = 1.1 * eg[:ff] * g[ff:].abs() + s * g[:ff].abs() * eg[ff:] + 16 * U32 * h.abs()   # (exponential, sum, quotient and product: 11 of them at most)
-            eh = eh + h.abs() * (2.0 ** -18 if x.dtype is not F32 else 2.0 ** -27)
+            eh = eh + h.abs() * (0.0 if x.dtype is F32 else 2.0 ** -17)
             want[t] += float(weights[t, j]) * (V @ h)
             bound[t] += float(weights[t, j]) * (V.abs() @ eh + (ff + ceil(ff) + 8 + ids.shape[1]) * U32 * (V.abs() @ h.abs()))
     return want, bound
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_layer_hands_hidden_on_as_it_says(dtype):
+    """One hidden value less another that is near it: their difference shows how many bits of them went on."""
+    d = ff = 128
+    g = gen(39)
+    # hidden[0] and [1]: an input and what bf16 keeps of it, times a scale of 21 bits
+    x = torch.zeros(64, d, device=DEV)
+    x[:, 0] = 1 + torch.rand(64, generator=g, device=DEV)
+    x[:, 1] = x[:, 0].bfloat16().float()
+    x = x.to(dtype)
+    up = torch.zeros(1, ff, d, device=DEV)
+    up[0, 0, 0], up[0, 1, 1] = 1, 1
+    scale = torch.ones(1, 1, 1, device=DEV) * (1 + 2.0 ** -16 + 2.0 ** -20)
+    down = torch.zeros(1, d, ff, device=DEV)
+    down[0, :, 0], down[0, :, 1] = 1, -1
+    ids, one = torch.zeros(64, 1, dtype=torch.int32, device=DEV), torch.ones(1, 1, 1, device=DEV)
+    out, scratch = torch.empty_like(x), torch.empty(A.nmt_op_expert_layer8_scratch(64, 1, 1, d, ff), device=DEV)
+    A.nmt_op_expert_layer8(x, ids, None, up.to(E4M3), scale, down.to(E4M3), one, out, scratch)
+    # the scale's product rounds once, the difference of two is exact where they are near each other
+    h = (x[:, :2].to(D) * scale.to(D)[0, 0]).float().to(D)
+    want = (h[:, 0] - h[:, 1])[:, None].expand(64, d)
+    off = 0.0 if dtype is F32 else 2.0 ** -17
+    within(out, want, half_step(dtype) * want.abs() + off * (h[:, 0] + h[:, 1])[:, None], "out")
 
 
 # (sizes of which one product, the other or none gives every wavefront rows of its own)
