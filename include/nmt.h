@@ -526,7 +526,8 @@ int nmt_op_norm8(const nmt_norm8* a /*host*/, void* stream);
  * batch products lie stride_* apart (bytes of A and B, elements of the others; 0: the same for all; of C not).
  * d_ranges NULL: `batch` products of M x N x K each.  Otherwise d_ranges [batch, 2] (nmt_op_expert_dispatch): expert e's rows are the ranges[e, 1] rows of A, of the scales and of C from ranges[e, 0] on, M is
  * the number of rows of A and C in all, its B, scales of B and bias lie e strides on, the other strides are not used, and a_square is 0.  Rows that no expert has are left as they
- * were; ranges do not overlap, and what of them lies outside [0, M) is cut off.
+ * were; ranges do not overlap, and what of them lies outside [0, M) is cut off.  Ranges are of A's rows, never of k: the weights' gradients of experts are a batch, each expert's rows with room of their own
+ * (a multiple of 128, and the rows behind an expert's last zero), since 128 rows that share a scale would reach from one expert into the next.
  * Rows of A and B begin at multiples of 16 bytes; C, bias and add have any address that their type allows and any distance.  K = 0: bias + add.  batch <= 1024; lda, ldb <= 2^22.
  * d_scratch: 16-byte aligned, scratch_floats >= nmt_op_gemm8_scratch(M, N, K, batch, ranges != NULL), which may be 0. */
 typedef struct nmt_gemm8 {
