@@ -1,10 +1,11 @@
 // A sparse layer over few tokens, its experts' weights held in 8 bits with a scale for each 128 x 128:
 //   hidden[t, j] = act(up[e(t, j)] x[t]),  out[t] = add[t] + sum over j of weights[t, j] down[e(t, j)] hidden[t, j].
-// Bound by the weights of the experts that have a token, which are read once for each 32 choices of an expert (16, where a work-group has 16 rows).  Two products of the same form and a sum: a work-group takes an expert's choices and 16 rows (or eight
-// times 16) of its weight; the matrix instruction's other operand are up to 16 choices' inputs.  Codes are exact in bf16; inputs are split into as
-// many bf16 parts as hold them: bf16 one, fp16 two, fp32 three; so the products are those of the inputs as they are.  Hidden goes on in two parts, off by
-// up to 2^-17 of itself beside results that are rounded by up to 2^-11 (fp16) or 2^-8 (bf16), or, for fp32, in three, which hold it: in three parts the 33 tokens below take 158 us instead of 147, 64 tokens, 8 of 16 experts, 57 instead of 53.
-// Measured: 33 tokens, 4 of 64 experts, 1024 x 4096 silu gate, bf16 149 to 158 us, 4.8 TB/s of weights; 64 tokens, 2 of 128, 640 x 1280 42 us, 3.2 TB/s; one token, 2 of 8, 512 x 2048 10.8 us in a graph, which is three launches
+// Bound by the weights of the experts that have a token, which are read once for each 32 choices of an expert (16, where a work-group has 16 rows).  Two products of the same form and a sum: a
+// work-group takes an expert's choices and 16 rows (or eight times 16) of its weight; the matrix instruction's other operand are up to 16 choices' inputs.  Codes are exact in bf16; inputs are split into as
+// many bf16 parts as hold them: bf16 one, fp16 two, fp32 three; so the products are those of the inputs as they are.  Hidden goes on in two parts, off by up to 2^-17 of itself beside results that are rounded by up
+// to 2^-11 (fp16) or 2^-8 (bf16), or, for fp32, in three, which hold it: in three for all types the 33 tokens below take 158 us instead of 147, 64 tokens, 8 of 16 experts, 57 instead of 53.
+// Measured: 33 tokens, 4 of 64 experts, 1024 x 4096 silu gate, bf16 147 to 153 us, 4.6 to 4.8 TB/s of weights; 64 tokens, 2 of 128, 640 x 1280 ReLU 42 us, 3.2 TB/s; 64 tokens, 8 of 16, 512 x 2048 ReLU fp16 54 us,
+// 0.6 TB/s, where each work-group walks all choices for its own and reads weights once more for an expert's last ones; one token, 2 of 8, 512 x 2048 10.8 us in a graph, which is three launches
 // that wait for each other (4.5, 5 and 2): each a chain of choices, addresses, weights and sums.  The sum in the second product's last work-group instead of a launch: 13 us in a graph, and 198 for the 33 tokens.
 #include "block8.h"
 

@@ -5,9 +5,9 @@
 // normally distributed codes, at most 2^-10 of the sum of the terms' magnitudes, beside which results are rounded to 16 bits (by up to 2^-11, 2^-8).  Results in fp32 are to be better than that: their codes go through the bf16
 // instruction, at half the rate, which adds up in fp32 what are exact products.
 //
-// Bound by the matrix units and the card's power: 8192^3 with 16-bit results 480 us, 2300 TFLOP/s, the matrix units at work in 60 % of the cycles of a clock that falls to 1.8 GHz (the library's product of the
-// same codes without scales of blocks 360 us); 52701 x 4096 x 1024 236 us; 52012 rows of 128 experts, 1024 x 1024, 93 us.  Short sizes wait for memory and LDS once per block of k: 3584 x 2048 x 512 10 us, 5 x 2048 x 512 5 us.
-// fp32 results: 8192^3 1000 us, 1100 TFLOP/s (bf16 library product 790); 1024 x 4096 x 26001 230 us and the sums of its two pieces 13.  The widening itself is 55 us of the 1000; the same instructions with A's operand
+// Bound by the matrix units and the card's power: 8192^3 with 16-bit results 466 to 480 us, 2300 TFLOP/s, the matrix units at work in 60 % of the cycles of a clock that falls to 1.8 GHz (the library's product of the
+// same codes without scales of blocks 360 us); 52701 x 4096 x 1024 236 to 248 us; 52012 rows of 128 experts, 1024 x 1024, 88 to 103 us.  Short sizes wait for memory and LDS once per block of k: 3584 x 2048 x 512 10 us, 5 x 2048 x 512 5 us.
+// fp32 results: 8192^3 1000 to 1060 us, 1040 to 1100 TFLOP/s (bf16 library product 790); 1024 x 4096 x 26001 230 us and the sums of its two pieces 13; with 16-bit results, B's rows with a scale each, 140 in all.  The widening itself is 55 us of the 1000; the same instructions with A's operand
 // held constant take 750: most of the rest is what changing operands cost, in power.
 #include "block8.h"
 

@@ -168,7 +168,7 @@ struct Norm8Args {
 };
 typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-// A row is read once into registers, and everything is formed there.  Measured: 52701 x 1024 bf16 with a sum 67 us, 5.6 TB/s; 13000 x 2048 fp16 30, 6.3; 6000 x 4096 fp32 59, 5.4; 2000 x 16384 bf16 39, 5.8; 20000 x 1001 fp16 25, 5.6; 1531 x
+// A row is read once into registers, and everything is formed there.  Measured: 52701 x 1024 bf16 with a sum 67 us, 5.6 TB/s; 13000 x 2048 fp16 30, 6.3; 6000 x 4096 fp32 55 to 59, 5.4 to 5.8; 2000 x 16384 bf16 39, 5.8; 20000 x 1001 fp16 25, 5.6; 1531 x
 // 777 fp32 6.9; 5 x 512 fp16 2.2.
 // LANES lanes of each of WAVES wavefronts hold a row, VECS times eight elements each: 16 lanes hold the 128 that share a scale.
 template <typename T, int LANES, int VECS, int WAVES, bool RAGGED>
