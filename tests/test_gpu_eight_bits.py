@@ -458,15 +458,17 @@ def test_gemm_of_scales_whose_product_is_a_normal_number(M, N, K, dtype, square)
 
 def test_gemm_of_scales_whose_product_is_next_to_nothing():
     """Such a product of scales is off by 2^-150 at most, and a block's sum is less than 2^25."""
-    for dtype, square in ((F32, False), (F32, True), (BF16, True), (BF16, False)):
+    # (some 2^-127, of which sums of 2^17 and more make normal numbers that are far from the bound, and 2^-142)
+    for dtype, square, down in ((t, q, x) for t in (F32, BF16) for q in (False, True) for x in (-25, -40)):
         (a, sa), (b, sb) = eight(70, 300, False, 92), eight(90, 300, square, 93)
-        sa, sb = sa * 2.0 ** -90, sb * 2.0 ** -40
+        sa, sb = sa * 2.0 ** -90, sb * 2.0 ** down
         c = torch.empty(70, 90, dtype=dtype, device=DEV)
         A.nmt_op_gemm8(a, sa, b, sb, c)
         X, W = decode(a, sa), decode(b, sb)
         want, mag = X @ W.t(), X.abs() @ W.abs().t()
         cut = 0.0 if dtype is F32 else 2.0 ** -10
-        within(c, want, half_step(dtype) * want.abs() + (cut + 320 * U32) * mag + 3 * 2.0 ** -125, dtype)
+        within(c, want, half_step(dtype) * want.abs() + (cut + 320 * U32) * mag + 3 * 2.0 ** -125, (dtype, down))
+        assert down < -30 or float(c.abs().max()) > 2.0 ** -115
 
 
 @pytest.mark.parametrize("batch,M,N,K", [(1, 30, 40, 128), (3, 100, 70, 256), (7, 64, 65, 384), (40, 200, 300, 128), (2, 300, 200, 5120)])
